@@ -315,6 +315,112 @@ int sts_op_attn_prefill_form(const float* q, const float* k, const float* v, flo
 int sts_op_attn_decode(const float* q, const float* k, const float* v, float* out, int32_t n, const int32_t* ctx,
                        int32_t n_q, int32_t n_kv, int32_t d, int32_t chunk_pages);
 
+/* ---- operators on device data, for a step that answers one prompt many times: places for the new tokens, rotary positions and
+ * the append to the pages, attention over a prefix that requests share, log probabilities of what was sampled. As in
+ * sts_op_gemm_noalloc all pointers but those to the descriptions are DEVICE pointers of the caller's, valid until the work has run;
+ * the kernels are queued on `stream` (a hipStream_t, NULL = the null stream of the current device), on whose device the data lies,
+ * and the call returns without waiting. Nothing is allocated, nothing is kept between calls, all of it can be captured into a graph.
+ * Pages hold 16 tokens, batches up to 4096 requests. Lengths, tables and tokens lie on the device, so the host checks sizes,
+ * strides and alignment (STS_EINVAL, nothing queued) and the kernels check what they read: none follows a page, place or token
+ * number out of its range. Arrays that are written must not overlap others unless stated. */
+enum { STS_F32 = 0, STS_BF16 = 1, STS_F16 = 2 };
+
+/* Block tables and places of a step's new rows (what the engine's calls make on the host for their own sequences, Section 3.5.1).
+ * Request i holds cached[i] tokens and gets added[i] more; the pages it needs come off the end of free_pages[0 .. n_free) in the
+ * requests' order and are entered into its table. Rows are the added tokens, request after request. */
+typedef struct {
+  int32_t n_requests, max_pages;        /* entries of a table row that may be used */
+  int32_t max_rows;                     /* length of requests, positions and places */
+  int32_t free_capacity;                /* length of free_pages */
+  int64_t table_stride;                 /* entries from a table row to the next, >= max_pages */
+  const int32_t *cached, *added;        /* [n_requests] */
+  const int32_t *free_pages, *n_free;   /* [free_capacity]; [1] */
+  int32_t* tables;                      /* [n_requests][table_stride]: entries of new pages are written, no others */
+  int32_t* lens;                        /* [n_requests]: cached + added */
+  int32_t* row_starts;                  /* [n_requests + 1]: first row of each request, and the number of rows */
+  int32_t *requests, *positions;        /* [max_rows]: of each row; behind the last row left as they were */
+  int32_t* places;                      /* [max_rows]: page * 16 + slot of each row; behind the last row -1 */
+  int32_t* n_free_left;                 /* [1]: the free pages that are left (not in place of n_free) */
+  int32_t* status;                      /* [1]: STS_OK; STS_EINVAL (a negative length, a count of free pages out of range); STS_ENOMEM (too few free
+                                           pages, rows, or entries of a table row). Not STS_OK: the step has no rows (row_starts 0, places -1, lens =
+                                           cached, n_free_left = n_free) and the tables are left as they were */
+} sts_block_tables;
+int sts_op_block_tables(const sts_block_tables* a, void* stream);
+
+/* Rotary positions. Pair i < rotary_dim / 2 of a head turns by position * f_i, elements from rotary_dim on pass. f_i by `scaling`, with
+ * w_i = theta^(-2 i / rotary_dim) and turns_i = original_len * w_i / 2 pi:
+ *   PLAIN   w_i
+ *   LINEAR  w_i / factor
+ *   BASE    w_i of the base theta * factor^(rotary_dim / (rotary_dim - 2))
+ *   BANDS   from w_i / factor (turns_i <= low) to w_i (turns_i >= high), in between in proportion to turns_i
+ *   RAMP    from w_i (i <= a) to w_i / factor (i >= b), in between in proportion to i; a and b are the pair numbers, rounded outwards, that make
+ *           `high` and `low` turns over original_len: rotary_dim ln(original_len / (turns 2 pi)) / (2 ln theta)
+ * magnitude: factor of cosine and sine (0: 1). */
+enum { STS_ROPE_PLAIN = 0, STS_ROPE_LINEAR, STS_ROPE_BASE, STS_ROPE_BANDS, STS_ROPE_RAMP };
+typedef struct {
+  int32_t rotary_dim;                   /* even, 2 to 256 */
+  int32_t interleaved;                  /* pairs (2 i, 2 i + 1) instead of (i, i + rotary_dim / 2) */
+  int32_t scaling, original_len;
+  float theta, factor, low, high, magnitude;
+} sts_rope;
+/* Host only, no GPU state: f_i, rotary_dim / 2 of them. */
+int sts_rope_frequencies(const sts_rope* rope, double* out);
+/* Rows of Q and K, heads behind each other; strides in elements from row to row. Q rows are turned into q_out, K rows into k_out
+ * (may be NULL with a pool) and the pool, V rows into the pool. q_out = q and k_out = k, with equal strides, turn rows in place. */
+typedef struct {
+  int32_t dtype;                        /* STS_F32 (no pool), STS_BF16, STS_F16 */
+  int32_t rows, n_q, n_kv, d;           /* n_q or n_kv may be 0 (their pointers are then not read) */
+  int32_t pool_pages;
+  const void* q; int64_t q_stride; void* q_out; int64_t q_out_stride;
+  const void* k; int64_t k_stride; void* k_out; int64_t k_out_stride;
+  const void* v; int64_t v_stride;
+  void* pool;                           /* one layer's pool in the library's layout, [pool_pages][n_kv][K: 16 x d | V^T: d x 16] (d 64 or 128), or NULL */
+  const int32_t* positions;             /* [rows] */
+  const int32_t* places;                /* [rows]: page * 16 + slot, different for each row; a row whose place is not in the pool is not appended */
+} sts_rope_rows;
+int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* stream);
+
+/* Decode attention (one query row a request) for groups of requests whose contexts begin with the same pages. Requests
+ * group_starts[g] .. group_starts[g + 1] - 1 are group g; the whole pages among the first shared_lens[g] tokens of their contexts, as far as
+ * all of them hold them, are read through the first one's table, once for all. The caller sees to it that their tables agree there.
+ * shared_lens 0, a group of one, or group_starts that do not lead from 0 to n_requests in order: nothing is shared, the result is the same.
+ * A context of length 0 gives zeros and an lse of -inf; one that is negative or longer than max_pages, or whose table names a page
+ * outside the pool, gives NaN. What lies in a page behind its context is not looked at.
+ * The plan is made from the lengths once a step and serves all layers: sts_op_attn_shared_plan, then sts_op_attn_shared for each layer on the
+ * same stream (or ordered behind it) with the same description. Calls that may run at the same time need workspaces of their own. */
+typedef struct {
+  int32_t dtype;                        /* STS_BF16 or STS_F16: of q, pool and out */
+  int32_t n_requests, n_groups;         /* n_groups 0: nothing is shared, group_starts and shared_lens are not read */
+  int32_t n_q, n_kv, d;                 /* n_q / n_kv up to 32, n_kv up to 512, d 64 or 128 */
+  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read */
+  int64_t table_stride;                 /* >= max_pages */
+  const int32_t *tables, *lens;         /* [n_requests][table_stride]; [n_requests]: tokens to attend to, the new one included */
+  const int32_t *group_starts, *shared_lens;   /* [n_groups + 1]; [n_groups] */
+  void* workspace; int64_t workspace_bytes;    /* 256-byte aligned, sts_attn_shared_workspace bytes */
+} sts_attn_batch;
+/* Host only, no GPU state: bytes of workspace; -1 for sizes out of range. */
+int64_t sts_attn_shared_workspace(int32_t n_requests, int32_t n_q, int32_t n_kv, int32_t d);
+int sts_op_attn_shared_plan(const sts_attn_batch* b, void* stream);
+/* q and out [n_requests][n_q * d], strides in elements; pool: one layer's, 16-byte aligned; lse [n_requests][n_q] or NULL: natural logarithm of the
+ * sum of exponentials of the scaled scores. scale 0: 1 / sqrt(d). */
+int sts_op_attn_shared(const sts_attn_batch* b, const void* q, int64_t q_stride, const void* pool, void* out, int64_t out_stride, float* lse, float scale, void* stream);
+
+/* Log probabilities of given tokens, entropies, and the most likely tokens, of rows of logits. Each output may be NULL.
+ * Logits may be -inf (no probability); a row of nothing else has log probabilities and lse -inf and entropy 0. A row with +inf or NaN has
+ * NaN for all of them; in the order of its tokens NaN counts as -inf. */
+typedef struct {
+  int32_t dtype, rows, vocab, top_k;    /* rows up to 65535, top_k 0 to 32 and at most vocab */
+  int64_t row_stride;                   /* elements from row to row */
+  const void* logits;                   /* aligned to its elements */
+  const int32_t* tokens;                /* [rows]; one outside [0, vocab): log probability NaN, rank -1. NULL: no tokens */
+  float *logprob, *entropy, *lse;       /* [rows], in nats */
+  int32_t* rank;                        /* [rows]: tokens before the given one, larger logits first, then lower numbers (0: the greedy choice; a NaN logit: -1) */
+  float* top_logprob; int32_t* top_token;      /* [rows][top_k], in that order */
+  void* workspace; int64_t workspace_bytes;    /* 16-byte aligned, sts_op_logprobs_workspace bytes (0 where there are many rows) */
+} sts_logprobs;
+int64_t sts_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t top_k);
+int sts_op_logprobs(const sts_logprobs* a, void* stream);
+
 /* ---- performance estimator (Section 3.2) — host only, integer arithmetic.
  * Wave quantisation (Section 2.2.1): g workgroups on n units, b workgroups per unit. */
 int sts_wave_quant(int64_t g, int64_t n, int64_t b, int64_t* waves, int64_t* tail, int64_t* idle_num, int64_t* idle_den);

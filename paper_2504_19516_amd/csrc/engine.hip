@@ -17,12 +17,14 @@
 #include <string>
 #include <vector>
 
+#include "device_ops.h"
 #include "kernels.h"
 #include "sts.h"
 
 using namespace sts;
 
 static std::atomic<int> g_hip_err{0};   // either phase's control thread may record an error
+void sts::record_hip_error(hipError_t e) { g_hip_err = (int)e; }
 #define HIPCK(x)                                                 \
   do {                                                           \
     hipError_t e_ = (x);                                         \

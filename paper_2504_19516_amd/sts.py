@@ -22,6 +22,10 @@ GEMM_CFGS = {"128x128": 0, "64x256": 1, "64x128": 2, "256x256": 3, "128x256": 4,
 INF_NS = 1 << 60
 
 
+DTYPES = {"f32": 0, "bf16": 1, "f16": 2}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
 class StsError(RuntimeError):
     def __init__(self, code, what):
         self.code = code
@@ -84,6 +88,40 @@ class ReplayStats(C.Structure):
                                           "n_tpot", "n_slo_ok", "n_decisions")]
 
 
+def _fields(kind, names):
+    return [(n, kind) for n in names.split()]
+
+
+class BlockTables(C.Structure):
+    """sts_block_tables; pointers are device addresses (ints), None for NULL."""
+    _fields_ = _fields(C.c_int32, "n_requests max_pages max_rows free_capacity") + _fields(C.c_int64, "table_stride") + _fields(
+        C.c_void_p, "cached added free_pages n_free tables lens row_starts requests positions places n_free_left status")
+
+
+class Rope(C.Structure):
+    """sts_rope; scaling: one of ROPE_SCALINGS' values."""
+    _fields_ = _fields(C.c_int32, "rotary_dim interleaved scaling original_len") + _fields(C.c_float, "theta factor low high magnitude")
+
+
+class RopeRows(C.Structure):
+    """sts_rope_rows"""
+    _fields_ = _fields(C.c_int32, "dtype rows n_q n_kv d pool_pages") + [
+        ("q", C.c_void_p), ("q_stride", C.c_int64), ("q_out", C.c_void_p), ("q_out_stride", C.c_int64), ("k", C.c_void_p), ("k_stride", C.c_int64), ("k_out", C.c_void_p),
+        ("k_out_stride", C.c_int64), ("v", C.c_void_p), ("v_stride", C.c_int64)] + _fields(C.c_void_p, "pool positions places")
+
+
+class AttnBatch(C.Structure):
+    """sts_attn_batch"""
+    _fields_ = _fields(C.c_int32, "dtype n_requests n_groups n_q n_kv d pool_pages max_pages") + _fields(C.c_int64, "table_stride") + _fields(
+        C.c_void_p, "tables lens group_starts shared_lens workspace") + _fields(C.c_int64, "workspace_bytes")
+
+
+class Logprobs(C.Structure):
+    """sts_logprobs"""
+    _fields_ = _fields(C.c_int32, "dtype rows vocab top_k") + _fields(C.c_int64, "row_stride") + _fields(
+        C.c_void_p, "logits tokens logprob entropy lse rank top_logprob top_token workspace") + _fields(C.c_int64, "workspace_bytes")
+
+
 EXPORTS = [
     "sts_strerror", "sts_last_hip_error", "sts_init", "sts_destroy", "sts_release_streams", "sts_load_weights", "sts_read_weights",
     "sts_seq_create", "sts_seq_free", "sts_seq_length", "sts_seq_truncate", "sts_seq_reserve", "sts_pages_free", "sts_seq_set_block_table",
@@ -94,7 +132,8 @@ EXPORTS = [
     "sts_probe_copy", "sts_profile_observe", "sts_op_gemm", "sts_op_attn_prefill", "sts_op_attn_prefill_form", "sts_attn_prefill_plan", "sts_op_attn_decode", "sts_wave_quant",
     "sts_profile_parse", "sts_profile_load", "sts_profile_dump", "sts_profile_free", "sts_latency_query",
     "sts_latency_roofline", "sts_sched_decide", "sts_sched_replay", "sts_max_pages_per_seq_limit", "sts_decode_chunk_plan", "sts_decode_gemm_plan", "sts_decode_layer_plan", "sts_decode_layer_all_rows", "sts_decode_gemm_all_rows", "sts_probe_read", "sts_set_stream_model", "sts_profile_stream_model", "sts_op_gemm_noalloc", "sts_op_gemm_cols", "sts_weight_packed_index", "sts_probe_gemm", "sts_set_tile_model",
-    "sts_profile_tile_model",
+    "sts_profile_tile_model", "sts_op_block_tables", "sts_rope_frequencies", "sts_op_rope", "sts_attn_shared_workspace", "sts_op_attn_shared_plan",
+    "sts_op_attn_shared", "sts_op_logprobs_workspace", "sts_op_logprobs",
 ]
 
 
@@ -106,6 +145,10 @@ def lib():
         _lib = C.CDLL(LIB_PATH)
         _lib.sts_strerror.restype = C.c_char_p
         _lib.sts_kernel_name.restype = C.c_char_p
+        _lib.sts_op_logprobs_workspace.restype = C.c_int64
+        _lib.sts_attn_shared_workspace.restype = C.c_int64
+        # called once a layer: converting by declared types takes a third of the time that wrapping each argument does
+        _lib.sts_op_attn_shared.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c_void_p]
     return _lib
 
 
@@ -425,6 +468,46 @@ def op_attn_decode(q, k, v, ctx, chunk_pages):
     _ck(lib().sts_op_attn_decode(_p(q, C.c_float), _p(k, C.c_float), _p(v, C.c_float), _p(out, C.c_float), n, _p(ctx),
                                  n_q, k.shape[1], d, chunk_pages), "sts_op_attn_decode")
     return out
+
+
+# Operators on device data: descriptions hold device addresses (ints; a torch tensor's data_ptr()), the kernels are queued on `stream` (a
+# hipStream_t value, None or 0 = the null stream) and not waited for. A process that also uses torch imports torch first: the library then
+# shares its HIP runtime, and with it streams and graphs.
+def op_block_tables(a: BlockTables, stream=None):
+    _ck(lib().sts_op_block_tables(C.byref(a), C.c_void_p(stream)), "sts_op_block_tables")
+
+
+def rope_frequencies(rope: Rope):
+    """Radians a token of each pair; host only."""
+    out = np.empty(max(1, rope.rotary_dim // 2), np.float64)
+    _ck(lib().sts_rope_frequencies(C.byref(rope), _p(out)), "sts_rope_frequencies")
+    return out
+
+
+def op_rope(rope: Rope, a: RopeRows, stream=None):
+    _ck(lib().sts_op_rope(C.byref(rope), C.byref(a), C.c_void_p(stream)), "sts_op_rope")
+
+
+def attn_shared_workspace(n_requests, n_q, n_kv, d):
+    """Bytes of workspace of a batch; host only."""
+    return lib().sts_attn_shared_workspace(n_requests, n_q, n_kv, d)
+
+
+def op_attn_shared_plan(b: AttnBatch, stream=None):
+    _ck(lib().sts_op_attn_shared_plan(C.byref(b), C.c_void_p(stream)), "sts_op_attn_shared_plan")
+
+
+def op_attn_shared(b: AttnBatch, q, q_stride, pool, out, out_stride, lse=None, scale=0.0, stream=None):
+    _ck(lib().sts_op_attn_shared(C.byref(b), q, q_stride, pool, out, out_stride, lse, scale, stream), "sts_op_attn_shared")
+
+
+def op_logprobs_workspace(dtype, rows, vocab, top_k):
+    """Bytes of workspace (dtype: a value of DTYPES); host only."""
+    return lib().sts_op_logprobs_workspace(dtype, rows, vocab, top_k)
+
+
+def op_logprobs(a: Logprobs, stream=None):
+    _ck(lib().sts_op_logprobs(C.byref(a), C.c_void_p(stream)), "sts_op_logprobs")
 
 
 def release_streams():
