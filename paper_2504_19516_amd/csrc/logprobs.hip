@@ -5,16 +5,16 @@
 // and the top k in that same order (value descending, then index ascending).
 //
 // One pass over the logits, in units of log2: y = x log2(e) - M, with M = m log2(e) as it rounds, is one fused multiply-add, p = 2^y.
-// M stands in for m to the end, so its rounding cancels. Logits beyond 2^100 (a row masked throughout with the type's lowest value)
-// would leave fp32's range there: they take y = (x - m) log2(e). Every lane keeps its own running maximum, sum and weighted sum, and
+// M stands in for m to the end, so its rounding cancels. A maximum beyond 2^100 (a row masked throughout with the type's lowest value)
+// would leave fp32's range there: it takes y = x - m, which is 0 or below -2^77. Every lane keeps its own running maximum, sum and weighted sum, and
 // they meet once at the end. A row is cut into parts (one workgroup each) when there are few rows;
 // a second kernel joins the parts.
 //
-// Top k: a wave keeps a bound below which nothing can be among its k best, and passes elements above it on to a list in LDS. The bound
-// comes from the lanes' running maxima, which are there anyway: they are different elements, so the k-th largest of the 64 is a lower
-// bound of the wave's k-th best. Some k (1 + ln n) elements of a row in random order pass. A full list is cut to its k best, which
-// makes the bound exact; from then on equals do not pass, because a wave goes through its elements in ascending order. So no order of
-// the logits and no number of equal ones makes a wave pass on more than a list per batch of its lanes' elements.
+// Top k: while the row streams by, each lane only notes the largest element of every group of its own (32 elements or more) in LDS. The lanes'
+// largest are different elements, so the k-th largest of them bounds the k-th best from below; few groups reach the bound (some k), and
+// their elements are read again, compared with it, and sorted by compare-exchanges between lanes. Where more elements reach the bound than
+// the buffer holds (rows of equal values), the waves go through the part again, each with a sorted list of its 64 best and the bound that
+// its k-th best gives; equals do not pass that bound, because a wave goes through its elements in ascending order.
 #include <algorithm>
 
 #include "device_ops.h"
@@ -23,9 +23,11 @@ namespace sts {
 namespace {
 
 constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64;
-constexpr int LP_VECS = 8;                      // 16-byte vectors of a lane and batch
-constexpr int LP_LIST = 256;                    // entries of a wave's list
+constexpr int LP_ELEMS = 32;                    // elements of a lane and batch
 constexpr int LP_MAX_K = 32, LP_MAX_PARTS = 16;
+constexpr int LP_SLOTS = 8;                     // groups of a lane
+constexpr int LP_BUFFER = 256;                  // candidates of a part
+constexpr int LP_WORKGROUPS = 1024;             // wanted: four a CU, see logprob_parts
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr double LN2 = 0.69314718055994530942;
 
@@ -56,29 +58,73 @@ __device__ __forceinline__ void join_sums(RowSums& a, const RowSums& b) {
   a.above += b.above;
 }
 
-// The k largest of `count` keys in LDS, in their order, to the front of the list. For one wave. Keys differ from each other.
-__device__ __forceinline__ void keep_best(unsigned long long* list, int count, int k) {
+// Exchange with the lane whose number differs in one bit, without a trip through LDS.
+template <int M>
+__device__ __forceinline__ unsigned xor_lane(unsigned v) {
+  auto dpp = [](unsigned x, auto ctrl) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, true); };
+  if constexpr (M == 1) return dpp(v, std::integral_constant<int, 0xB1>{});
+  if constexpr (M == 2) return dpp(v, std::integral_constant<int, 0x4E>{});
+  if constexpr (M == 4) return dpp(dpp(v, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1B>{});     // 7 - i, then i ^ 3
+  if constexpr (M == 8) return dpp(v, std::integral_constant<int, 0x128>{});                                              // turned by 8 of 16
+  if constexpr (M == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  if constexpr (M == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+template <int M> __device__ __forceinline__ float xor_lane(float v) { return __uint_as_float(xor_lane<M>(__float_as_uint(v))); }
+template <int M> __device__ __forceinline__ unsigned long long xor_lane(unsigned long long v) {
+  return (unsigned long long)xor_lane<M>((unsigned)(v >> 32)) << 32 | xor_lane<M>((unsigned)v);
+}
+template <typename T, typename F>
+__device__ __forceinline__ T all_lanes(T v, F f) {
+  v = f(v, xor_lane<1>(v)); v = f(v, xor_lane<2>(v)); v = f(v, xor_lane<4>(v));
+  v = f(v, xor_lane<8>(v)); v = f(v, xor_lane<16>(v)); v = f(v, xor_lane<32>(v));
+  return v;
+}
+// One step of a sorting network: lanes M apart keep the larger key in the lane where `larger` holds.
+template <int M>
+__device__ __forceinline__ void exchange(unsigned long long& key, bool larger) {
+  const unsigned long long other = xor_lane<M>(key);
+  if ((other > key) == larger) key = other;
+}
+// A bitonic run of 64 keys into descending order.
+__device__ __forceinline__ void settle(unsigned long long& key) {
   const int lane = threadIdx.x & 63;
-  constexpr int PER = LP_LIST / 64;
-  unsigned long long mine[PER];
-  int before[PER];
-#pragma unroll
-  for (int j = 0; j < PER; j++) {
-    mine[j] = lane + 64 * j < count ? list[lane + 64 * j] : 0;
-    before[j] = 0;
+  exchange<32>(key, !(lane & 32)); exchange<16>(key, !(lane & 16)); exchange<8>(key, !(lane & 8));
+  exchange<4>(key, !(lane & 4)); exchange<2>(key, !(lane & 2)); exchange<1>(key, !(lane & 1));
+}
+// 64 keys into ascending order.
+__device__ __forceinline__ void sort_up(unsigned long long& key) {
+  const int lane = threadIdx.x & 63;
+  auto up = [&](int size) { return (lane & size) == 0; };          // this lane's run of `size` goes up
+#define STEP(size, m) exchange<m>(key, ((lane & m) != 0) == up(size))
+  STEP(2, 1);
+  STEP(4, 2); STEP(4, 1);
+  STEP(8, 4); STEP(8, 2); STEP(8, 1);
+  STEP(16, 8); STEP(16, 4); STEP(16, 2); STEP(16, 1);
+  STEP(32, 16); STEP(32, 8); STEP(32, 4); STEP(32, 2); STEP(32, 1);
+  STEP(64, 32); STEP(64, 16); STEP(64, 8); STEP(64, 4); STEP(64, 2); STEP(64, 1);
+#undef STEP
+}
+// The 64 best of a descending list and of 64 further keys, in descending order.
+__device__ __forceinline__ void merge_64(unsigned long long& best, unsigned long long more) {
+  sort_up(more);
+  best = more > best ? more : best;
+  settle(best);
+}
+// The 32 best of `n` descending lists of 32 keys each, in descending order (lanes 0 to 31).
+__device__ __forceinline__ unsigned long long merge_lists(const unsigned long long (*lists)[LP_MAX_K], int n) {
+  const int lane = threadIdx.x & 63;
+  unsigned long long key = lane < 32 ? lists[0][lane] : 0;
+  for (int i = 1; i < n; i++) {
+    if (lane >= 32) key = lists[i][63 - lane];
+    settle(key);
   }
-  for (int i = 0; i < count; i++) {
-    const unsigned long long other = list[i];
-#pragma unroll
-    for (int j = 0; j < PER; j++) before[j] += other > mine[j];
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-#pragma unroll
-  for (int j = 0; j < PER; j++)
-    if (lane + 64 * j < count && before[j] < k) list[before[j]] = mine[j];
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+  return key;
 }
 
 struct LogprobsCall {
@@ -100,12 +146,9 @@ __device__ __forceinline__ RowResult finish_sums(const RowSums& t) {
 }
 __device__ __forceinline__ float logprob_of(float x, const RowResult& r) { return r.none ? -INFINITY : (float)((double)x - r.ref - r.lz); }
 
-template <typename T>
-__device__ __forceinline__ void write_row(const sts_logprobs& a, int row, const RowSums& t) {
-  const RowResult r = finish_sums(t);
-  const int tok = a.tokens ? a.tokens[row] : -1;
+// tok, x: the given token and its logit (NaN if there is none).
+__device__ __forceinline__ void write_row(const sts_logprobs& a, int row, const RowSums& t, const RowResult& r, int tok, float x) {
   const bool given = tok >= 0 && tok < a.vocab;
-  const float x = given ? (float)reinterpret_cast<const T*>(a.logits)[(long long)row * a.row_stride + tok] : NAN;
   if (a.logprob) a.logprob[row] = given ? logprob_of(x, r) : NAN;
   if (a.rank) a.rank[row] = x != x ? -1 : x == -INFINITY ? tok + t.above : t.above;
   if (a.entropy) a.entropy[row] = r.entropy;
@@ -117,219 +160,265 @@ __device__ __forceinline__ void write_top(const sts_logprobs& a, int row, int at
   if (a.top_logprob) a.top_logprob[i] = logprob_of(key_value((unsigned)(key >> 32)), r);
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsCall c) {
+__device__ __forceinline__ float below(float x) {                 // the next value below
+  return x == 0.f ? -__uint_as_float(1u) : key_value(value_key(x) - 1);
+}
+__device__ __forceinline__ void lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's 64 best of every fourth load of a part, in descending order, with a buffer of its own of 64 + 64 E keys.
+template <typename T, typename L>
+__device__ unsigned long long second_pass(unsigned long long* buffer, int n_vecs, int base, int i0, int i1, int k, L load) {
   constexpr int E = 16 / sizeof(T);
+  const int lane = threadIdx.x & 63;
+  unsigned long long best = 0, least = 0;        // the list, and its k-th key: what is not above it is not among the k best
+  int count = 0;
+  for (int q = (threadIdx.x & ~63) + lane; q - lane < n_vecs; q += LP_THREADS) {
+    const int at = base + q * E;
+    const vec16<T> v = load(at);
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+      const unsigned long long key = order_key((float)v[e], at + e);
+      const bool pass = key > least && at + e >= i0 && at + e < i1;
+      const unsigned long long mask = __ballot(pass);
+      if (pass) buffer[count + __popcll(mask & ((1ull << lane) - 1))] = key;
+      count += __popcll(mask);
+    }
+    lds_fence();
+    while (count >= 64) {
+      count -= 64;
+      merge_64(best, buffer[count + lane]);
+      least = (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(best >> 32), k - 1) << 32 | (unsigned)__builtin_amdgcn_readlane((int)best, k - 1);
+    }
+    lds_fence();
+  }
+  merge_64(best, lane < count ? buffer[lane] : 0);
+  return best;
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c) {
+  constexpr int E = 16 / sizeof(T), VECS = LP_ELEMS / E, BATCH = 64 * VECS;
   typedef vec16<T> V;
   const sts_logprobs& a = c.a;
-  __shared__ unsigned long long lists[TOP ? LP_WAVES : 1][TOP ? LP_LIST : 1];
+  constexpr int SECOND = 64 + 64 * E;            // keys that a wave's buffer holds in the second pass: almost a list, and what a load may pass on
+  union Scratch {
+    struct { unsigned long long buffer[LP_BUFFER]; float group_max[LP_SLOTS][LP_THREADS], lane_maxima[LP_THREADS]; } first;
+    unsigned long long second[LP_WAVES][SECOND];
+    char none;
+  };
+  __shared__ __align__(16) unsigned char scratch[TOP ? sizeof(Scratch) : 16];
+  __shared__ unsigned long long lists[TOP ? LP_WAVES : 1][LP_MAX_K];
+  auto& first = reinterpret_cast<Scratch*>(scratch)->first;
   __shared__ RowSums wave_sums[LP_WAVES];
-  __shared__ int counts[LP_WAVES];
+  __shared__ int candidates;
   const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T* x = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
   const int i0 = part * c.width, i1 = min(a.vocab, i0 + c.width), k = TOP ? a.top_k : 0;
   // vectors lie at 16-byte addresses: the first may begin before the part
-  const int lead = (int)(reinterpret_cast<uintptr_t>(x + i0) % 16 / sizeof(T));
-  const int base = i0 - lead;
+  const int base = i0 - (int)(reinterpret_cast<uintptr_t>(x + i0) % 16 / sizeof(T));
+  const int n_vecs = (i1 - base + E - 1) / E;
+  auto load = [&](int at) {                      // elements at .. at + E - 1, -inf outside the part
+    V v;
+    if (at >= i0 && at + E <= i1) v = *reinterpret_cast<const V*>(x + at);
+    else {
+#pragma unroll
+      for (int e = 0; e < E; e++) v[e] = at + e >= i0 && at + e < i1 ? x[at + e] : (T)-INFINITY;
+    }
+    return v;
+  };
+
+  V raw[VECS];
+  auto fetch = [&](int b) {
+#pragma unroll
+    for (int j = 0; j < VECS; j++) raw[j] = load(base + (b + j * 64 + lane) * E);
+  };
+  fetch(wave * BATCH);
   const int tok = a.tokens ? a.tokens[row] : -1;
   const float xt = tok >= 0 && tok < a.vocab ? (float)x[tok] : NAN;
-  // an element stands before the token if it is above `strict` -- or, at a lower index, above `loose`, the next value below. A token of
-  // -inf: its rank is its index plus the elements above -inf behind it
-  const float strict = xt;
-  float loose = key_value(value_key(xt) - 1);
-  if (xt == 0.f) loose = -__uint_as_float(1u);
-  if (xt == -INFINITY) loose = INFINITY;
-  if (xt != xt) loose = NAN;
+  // an element stands before the token if it is above xt -- or, at a lower index, above `loose`, the next value below. A token of -inf:
+  // its rank is its index plus the elements above -inf behind it
+  const float loose = xt != xt ? NAN : xt == -INFINITY ? INFINITY : below(xt);
+  if (TOP && tid == 0) candidates = 0;
 
   RowSums t{-INFINITY, 0.f, 0.f, 0};
-  float lane_max = -INFINITY;                    // of the wave's elements so far
-  float bound = -INFINITY;                       // elements above it are passed on
-  bool open = TOP;                               // there is no bound yet: all are
-  int count = 0, above = 0;                      // wave-uniform
-  unsigned long long* list = lists[TOP ? wave : 0];
-
-  const int n_vecs = (i1 - base + E - 1) / E;
-  constexpr int BATCH = 64 * LP_VECS;
-  for (int b = wave * BATCH; b < n_vecs; b += LP_WAVES * BATCH) {
-    float v[LP_VECS][E];
+  int above = 0;                                 // wave-uniform
+  float lane_max = -INFINITY, slot_max = -INFINITY;
+  // batches of a wave, and of a group
+  const int batches = max(0, (n_vecs - wave * BATCH + LP_WAVES * BATCH - 1) / (LP_WAVES * BATCH)), span = (batches + LP_SLOTS - 1) / LP_SLOTS;
+  int slot = 0, in_slot = 0;
+  for (int i = 0, b = wave * BATCH; i < batches; i++, b += LP_WAVES * BATCH) {
+    float v[VECS][E], mx = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < LP_VECS; j++) {
-      const int q = b + j * 64 + lane, at = base + q * E;
-      if (at >= i0 && at + E <= i1) {
-        const V w = *reinterpret_cast<const V*>(x + at);
+    for (int j = 0; j < VECS; j++)
 #pragma unroll
-        for (int e = 0; e < E; e++) v[j][e] = (float)w[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; e++) v[j][e] = at + e >= i0 && at + e < i1 ? (float)x[at + e] : -INFINITY;
+      for (int e = 0; e < E; e++) {
+        v[j][e] = (float)raw[j][e];
+        mx = fmaxf(mx, v[j][e]);
       }
-    }
-    float top[LP_VECS], mx = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < LP_VECS; j++) {
-      top[j] = v[j][0];
-#pragma unroll
-      for (int e = 1; e < E; e++) top[j] = fmaxf(top[j], v[j][e]);
-      mx = fmaxf(mx, top[j]);
-    }
-    // ---- sums
+    if (i + 1 < batches) fetch(b + LP_WAVES * BATCH);
     if (mx > t.m) {
       const float shift = log2_diff(t.m, mx), f = __builtin_amdgcn_exp2f(shift);
       t.s = t.z == 0.f ? 0.f : f * (t.s + shift * t.z);
       t.z *= f;
       t.m = mx;
     }
-    auto add = [&](auto y_of) {
+    const bool far = beyond(t.m);                // there other values are 2^77 and more away: x - m is as good as any multiple of it
+    const float scale = far ? 1.f : LOG2E, ref = t.m == -INFINITY ? 0.f : t.m * scale;
 #pragma unroll
-      for (int j = 0; j < LP_VECS; j++)
-#pragma unroll
-        for (int e = 0; e < E; e++) {
-          const float y = y_of(v[j][e]), p = __builtin_amdgcn_exp2f(y);
-          t.z += p;
-          t.s = fmaf(p, fmaxf(y, -200.f), t.s);  // p is 0 there; -inf * 0 is not
-        }
-    };
-    if (!__any(beyond(t.m))) {
-      const float ref = t.m == -INFINITY ? 0.f : t.m * LOG2E;
-      add([&](float x) { return fmaf(x, LOG2E, -ref); });
-    } else {
-      const float ref = t.m == -INFINITY ? 0.f : t.m, big = t.m * LOG2E;
-      const bool far = beyond(t.m);
-      add([&](float x) { return far ? (x - ref) * LOG2E : t.m == -INFINITY ? x : fmaf(x, LOG2E, -big); });
-    }
-    // ---- elements before the token
-#pragma unroll
-    for (int j = 0; j < LP_VECS; j++) {
-      const int at = base + (b + j * 64 + lane) * E;
-      const bool all_before = at + E <= tok, all_behind = at >= tok;
+    for (int j = 0; j < VECS; j++) {
+      // a vector lies before the token or behind it; the one around it counts as behind (mended below)
+      const float limit = base + (b + j * 64 + lane + 1) * E <= tok ? loose : xt;
 #pragma unroll
       for (int e = 0; e < E; e++) {
-        const float limit = all_before || (!all_behind && at + e < tok) ? loose : strict;
+        const float y = fmaf(v[j][e], scale, -ref), p = __builtin_amdgcn_exp2f(y);
+        t.z += p;
+        t.s = fmaf(p, fmaxf(y, -200.f), t.s);    // p is 0 there; -inf * 0 is not
         above += __popcll(__ballot(v[j][e] > limit));
       }
     }
-    // ---- candidates
     if constexpr (TOP) {
-      lane_max = fmaxf(lane_max, mx);
-      {
-        // the k-th largest of the lanes' maxima, its upper 16 bits
-        const unsigned mk = value_key(lane_max);
-        unsigned kth = 0;
-#pragma unroll
-        for (int bit = 31; bit >= 16; bit--) {
-          const unsigned cand = kth | 1u << bit;
-          if (__popcll(__ballot(mk >= cand)) >= k) kth = cand;
-        }
-        if (kth > value_key(-INFINITY)) {
-          const float at_least = key_value(kth), below = at_least == 0.f ? -__uint_as_float(1u) : key_value(kth - 1);
-          bound = open ? below : fmaxf(bound, below);
-          open = false;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < LP_VECS; j++) {
-        if (!__any(open || top[j] > bound)) continue;
-        const int at = base + (b + j * 64 + lane) * E;
-        bool cut = false;
-        for (int e = 0; e < E; e++) {
-          float xe = v[j][0];
-#pragma unroll
-          for (int u = 1; u < E; u++) xe = e == u ? v[j][u] : xe;
-          const bool pass = (open || xe > bound) && at + e >= i0 && at + e < i1;
-          const unsigned long long mask = __ballot(pass);
-          if (mask == 0) continue;
-          const int more = __popcll(mask);
-          if (count + more > LP_LIST) {
-            keep_best(list, count, k);
-            count = k;
-            cut = true;
-          }
-          if (pass) list[count + __popcll(mask & ((1ull << lane) - 1))] = order_key(xe, at + e);
-          count += more;
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-        }
-        if (cut || count > LP_LIST - 128) {
-          // the bound becomes the k-th best: everything up to this vector is in, and what comes has higher indices
-          keep_best(list, count, k);
-          count = min(count, k);
-          if (count < k) continue;
-          bound = key_value((unsigned)(list[k - 1] >> 32));
-          open = false;
-        }
+      slot_max = fmaxf(slot_max, mx);
+      if (++in_slot == span || i + 1 == batches) {
+        first.group_max[slot++][tid] = slot_max;
+        lane_max = fmaxf(lane_max, slot_max);
+        slot_max = -INFINITY;
+        in_slot = 0;
       }
     }
   }
-  t.above = 0;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    RowSums u{__shfl_xor(t.m, o, 64), __shfl_xor(t.z, o, 64), __shfl_xor(t.s, o, 64), 0};
-    join_sums(t, u);
+  // the elements before the token in its own vector
+  if (wave == 0 && tok >= i0 && tok < i1) {
+    const int at = base + (tok - base) / E * E + lane;
+    const float xe = at >= i0 && at < tok ? (float)x[at] : NAN;
+    above += __popcll(__ballot(xe > loose)) - __popcll(__ballot(xe > xt));
   }
+  // ---- the lanes' sums, the waves' sums and lists
+  const float m = all_lanes(t.m, [](float p, float q) { return fmaxf(p, q); });
+  const float shift = t.m == -INFINITY ? 0.f : log2_diff(t.m, m), f = t.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(shift);      // a lane without a maximum has sums of 0, or NaN
+  t.s = f * (t.s + (t.z == 0.f ? 0.f : shift * t.z));
+  t.s = all_lanes(t.s, [](float p, float q) { return p + q; });
+  t.z = all_lanes(t.z * f, [](float p, float q) { return p + q; });
+  t.m = m;
+  t.above = above;
+  if (lane == 0) wave_sums[wave] = t;
+  unsigned long long best = 0;                   // a descending list, a key a lane
   if constexpr (TOP) {
-    keep_best(list, count, k);
-    count = min(count, k);
+    first.lane_maxima[tid] = lane_max;
+    __syncthreads();
+    // the k-th largest of the lanes' maxima, its upper 16 bits; none where fewer than k lanes have seen anything above -inf
+    unsigned keys[LP_WAVES], kth = 0;
+#pragma unroll
+    for (int w = 0; w < LP_WAVES; w++) keys[w] = value_key(first.lane_maxima[w * 64 + lane]);
+#pragma unroll
+    for (int bit = 31; bit >= 16; bit--) {
+      const unsigned cand = kth | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int w = 0; w < LP_WAVES; w++) n += __popcll(__ballot(keys[w] >= cand));
+      if (n >= k) kth = cand;
+    }
+    const bool open = kth <= value_key(-INFINITY);
+    float bound = open ? -INFINITY : below(key_value(kth));
+    // Without a bound everything above -inf is a candidate, and the part's first 64 elements: among them are 32 of -inf, or more than k others
+    unsigned hits = 0;
+    for (int g = 0; g < slot; g++) hits |= (unsigned)(first.group_max[g][tid] > bound || (open && g == 0 && tid * E < 64 + E)) << g;
+    while (hits) {                               // lanes apart: their groups
+      const int g = __builtin_ctz(hits);
+      hits &= hits - 1;
+      for (int i = g * span; i < min(batches, (g + 1) * span); i++) {
+        const int b = wave * BATCH + i * LP_WAVES * BATCH;
+        V again[VECS];
+#pragma unroll
+        for (int j = 0; j < VECS; j++) again[j] = load(base + (b + j * 64 + lane) * E);
+        unsigned found = 0;                      // bit j E + e
+#pragma unroll
+        for (int j = 0; j < VECS; j++)
+#pragma unroll
+          for (int e = 0; e < E; e++) found |= (unsigned)((float)again[j][e] > bound || (open && b + j * 64 + lane < 64 + E)) << (j * E + e);
+        while (found) {                          // few: their values again, from L1
+          const int q = __builtin_ctz(found), at = base + (b + q / E * 64 + lane) * E + q % E;
+          found &= found - 1;
+          if (at < i0 || at >= i1) continue;
+          const float xe = (float)x[at];
+          if (!(xe > bound) && at >= i0 + 64) continue;
+          const int n = atomicAdd(&candidates, 1);
+          if (n < LP_BUFFER) first.buffer[n] = order_key(xe, at);
+        }
+      }
+    }
+    __syncthreads();
+    const int n = candidates;
+    if (n <= LP_BUFFER) {
+      if (wave != 0) return;
+      for (int i = 0; i < n; i += 64) merge_64(best, i + lane < n ? first.buffer[i + lane] : 0);
+    } else {
+      __syncthreads();                           // the second pass takes the scratch over
+      best = second_pass<T>(reinterpret_cast<Scratch*>(scratch)->second[wave], n_vecs, base, i0, i1, k, load);
+      if (lane < LP_MAX_K) lists[wave][lane] = best;
+      __syncthreads();
+      if (wave != 0) return;
+      best = merge_lists(lists, LP_WAVES);
+    }
+  } else {
+    __syncthreads();
+    if (wave != 0) return;
   }
-  if (lane == 0) {
-    t.above = above;
-    wave_sums[wave] = t;
-    counts[wave] = count;
-  }
-  __syncthreads();
-  if (tid >= 64) return;
   t = wave_sums[0];
 #pragma unroll
   for (int w = 1; w < LP_WAVES; w++) join_sums(t, wave_sums[w]);
-  int n = counts[0];
-  if constexpr (TOP) {
-    for (int w = 1; w < LP_WAVES; w++) {
-      const unsigned long long key = lane < counts[w] ? lists[w][lane] : 0;
-      if (lane < counts[w]) lists[0][n + lane] = key;
-      n += counts[w];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    keep_best(lists[0], n, k);
-    n = min(n, k);
-  }
   if (c.parts == 1) {
-    if (lane == 0) write_row<T>(a, row, t);
-    if constexpr (TOP) {
-      const RowResult r = finish_sums(t);
-      if (lane < k) write_top(a, row, lane, lists[0][lane], r);
-    }
+    const RowResult r = finish_sums(t);
+    if (lane == 0) write_row(a, row, t, r, tok, xt);
+    if constexpr (TOP) if (lane < k) write_top(a, row, lane, best, r);
   } else {
     const long long at = (long long)row * c.parts + part;
     if (lane == 0) c.sums[at] = t;
-    if constexpr (TOP) if (lane < k) c.keys[at * k + lane] = lane < n ? lists[0][lane] : 0;
+    if constexpr (TOP) if (lane < k) c.keys[at * k + lane] = best;
   }
 }
 
 // Joins the parts of a row.
-template <typename T>
+template <typename T, bool TOP>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(LogprobsCall c) {
-  __shared__ unsigned long long keys[LP_MAX_PARTS * LP_MAX_K];
+  static_assert(LP_MAX_PARTS == 4 * LP_WAVES, "four parts a wave");
+  __shared__ unsigned long long lists[TOP ? LP_MAX_PARTS : 1][LP_MAX_K], quarters[TOP ? LP_WAVES : 1][LP_MAX_K];
   const sts_logprobs& a = c.a;
-  const int row = blockIdx.x, tid = threadIdx.x, n = c.parts * a.top_k;
-  for (int i = tid; i < n; i += LP_THREADS) keys[i] = c.keys[(long long)row * n + i];
-  RowSums t = c.sums[(long long)row * c.parts];
-  for (int p = 1; p < c.parts; p++) join_sums(t, c.sums[(long long)row * c.parts + p]);
-  if (tid == 0) write_row<T>(a, row, t);
-  if (n == 0) return;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.top_k;
+  const int tok = a.tokens ? a.tokens[row] : -1;
+  const float xt = tok >= 0 && tok < a.vocab ? (float)reinterpret_cast<const T*>(a.logits)[(long long)row * a.row_stride + tok] : NAN;
+  RowSums t{-INFINITY, 0.f, 0.f, 0};
+  if (wave == 0 && lane < c.parts) t = c.sums[(long long)row * c.parts + lane];
+  unsigned long long best = 0;
+  if constexpr (TOP) {
+    for (int i = tid; i < LP_MAX_PARTS * LP_MAX_K; i += LP_THREADS) {
+      const int p = i / LP_MAX_K, j = i % LP_MAX_K;
+      lists[p][j] = p < c.parts && j < k ? c.keys[((long long)row * c.parts + p) * k + j] : 0;
+    }
+    __syncthreads();
+    best = merge_lists(lists + 4 * wave, 4);
+    if (lane < LP_MAX_K) quarters[wave][lane] = best;
+    __syncthreads();
+  }
+  if (wave != 0) return;
+#pragma unroll
+  for (int o = LP_MAX_PARTS / 2; o > 0; o >>= 1) join_sums(t, RowSums{__shfl_xor(t.m, o, 64), __shfl_xor(t.z, o, 64), __shfl_xor(t.s, o, 64), __shfl_xor(t.above, o, 64)});
+  t = RowSums{__shfl(t.m, 0, 64), __shfl(t.z, 0, 64), __shfl(t.s, 0, 64), __shfl(t.above, 0, 64)};
   const RowResult r = finish_sums(t);
-  __syncthreads();
-  for (int i = tid; i < n; i += LP_THREADS) {
-    const unsigned long long mine = keys[i];
-    int before = 0;
-    for (int j = 0; j < n; j++) before += keys[j] > mine;
-    if (mine != 0 && before < a.top_k) write_top(a, row, before, mine, r);
+  if (lane == 0) write_row(a, row, t, r, tok, xt);
+  if constexpr (TOP) {
+    best = merge_lists(quarters, LP_WAVES);
+    if (lane < k) write_top(a, row, lane, best, r);
   }
 }
 
-// Parts of a row: enough workgroups for four per CU, none shorter than a batch of each of its waves.
-int logprob_parts(int rows, int vocab, int bytes) {
-  const int batch = LP_WAVES * 64 * LP_VECS * (16 / bytes);
-  return std::max(1, std::min({(vocab + batch - 1) / batch, (1024 + rows - 1) / rows, LP_MAX_PARTS}));
+// Parts of a row: enough workgroups for four per CU, none shorter than a batch of each of its waves. Wanting 512 / 1024 / 2048 workgroups, 64
+// rows of 128256 fp32 logits with 5 alternatives took 19.7 / 16.8 / 17.0 us, 200 rows 41.7 / 34.4 / 43.6 (with the join 5 us more each).
+int logprob_parts(int rows, int vocab) {
+  constexpr int batch = LP_WAVES * 64 * LP_ELEMS;
+  return std::max(1, std::min({(vocab + batch - 1) / batch, (LP_WORKGROUPS + rows - 1) / rows, LP_MAX_PARTS}));
 }
 size_t workspace_of(int rows, int parts, int k) { return parts == 1 ? 0 : (size_t)rows * parts * (sizeof(RowSums) + (size_t)k * sizeof(unsigned long long)); }
 
@@ -337,7 +426,9 @@ template <typename T>
 hipError_t launch_logprobs(hipStream_t s, const LogprobsCall& c) {
   const dim3 grid(c.parts, c.a.rows);
   hipError_t e = c.a.top_k > 0 ? launch(logprobs_kernel<T, true>, grid, dim3(LP_THREADS), 0, s, c) : launch(logprobs_kernel<T, false>, grid, dim3(LP_THREADS), 0, s, c);
-  if (e == hipSuccess && c.parts > 1) e = launch(logprobs_join_kernel<T>, dim3(c.a.rows), dim3(LP_THREADS), 0, s, c);
+  if (e != hipSuccess || c.parts == 1) return e;
+  const dim3 rows(c.a.rows);
+  e = c.a.top_k > 0 ? launch(logprobs_join_kernel<T, true>, rows, dim3(LP_THREADS), 0, s, c) : launch(logprobs_join_kernel<T, false>, rows, dim3(LP_THREADS), 0, s, c);
   return e;
 }
 
@@ -348,7 +439,7 @@ using namespace sts;
 
 extern "C" int64_t sts_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t top_k) {
   if (dtype < STS_F32 || dtype > STS_F16 || rows < 0 || vocab < 1 || top_k < 0 || top_k > LP_MAX_K) return -1;
-  return rows == 0 ? 0 : (int64_t)workspace_of(rows, logprob_parts(rows, vocab, (int)dtype_bytes(dtype)), top_k);
+  return rows == 0 ? 0 : (int64_t)workspace_of(rows, logprob_parts(rows, vocab), top_k);
 }
 
 extern "C" int sts_op_logprobs(const sts_logprobs* a, void* stream) {
@@ -358,7 +449,7 @@ extern "C" int sts_op_logprobs(const sts_logprobs* a, void* stream) {
   if (!a->logits || !aligned(a->logits, size) || (a->rows > 1 && a->row_stride < a->vocab)) return STS_EINVAL;
   if (!a->tokens && (a->logprob || a->rank)) return STS_EINVAL;
   if ((a->top_logprob || a->top_token) && a->top_k == 0) return STS_EINVAL;
-  LogprobsCall c{*a, logprob_parts(a->rows, a->vocab, (int)size), 0, nullptr, nullptr};
+  LogprobsCall c{*a, logprob_parts(a->rows, a->vocab), 0, nullptr, nullptr};
   c.width = (a->vocab + c.parts - 1) / c.parts;
   const size_t need = workspace_of(a->rows, c.parts, a->top_k);
   if (need > 0 && (!a->workspace || !aligned(a->workspace, 16) || a->workspace_bytes < (int64_t)need)) return STS_EINVAL;
