@@ -391,8 +391,8 @@ int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* stream);
 typedef struct {
   int32_t dtype;                        /* STS_BF16 or STS_F16: of q, pool and out */
   int32_t n_requests, n_groups;         /* n_groups 0: nothing is shared, group_starts and shared_lens are not read */
-  int32_t n_q, n_kv, d;                 /* n_q / n_kv up to 32, n_kv up to 512, d 64 or 128 */
-  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read */
+  int32_t n_q, n_kv, d;                 /* n_q / n_kv up to 32, n_kv up to 256, d 64 or 128 */
+  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read; n_requests * max_pages up to 2^28 */
   int64_t table_stride;                 /* >= max_pages */
   const int32_t *tables, *lens;         /* [n_requests][table_stride]; [n_requests]: tokens to attend to, the new one included */
   const int32_t *group_starts, *shared_lens;   /* [n_groups + 1]; [n_groups] */

@@ -7,14 +7,15 @@
 //   m = max m_j,  l = sum l_j 2^(m_j - m),  o = sum o_j 2^(m_j - m) / l
 //
 // A segment is a token range with the rows that read it: the shared pages of a group with a tile of its requests, or the own pages of
-// one request. A request brings n_q / n_kv rows (the query heads of a KV head) to the products, so a tile of shared pages fills the matrix cores'
-// columns that a single request leaves empty. The plan, made once a step on the device from the lengths, lays the segments of a KV
-// head end to end, weighs them (pages, and the start and end of a segment), and cuts the line into equal shares, one for each workgroup
-// of a KV head: a long context is shared by many workgroups, short ones are strung together in one.
+// one request. A request brings n_q / n_kv rows (the query heads of a KV head) to the products, so a tile of shared pages fills the matrix
+// cores' columns that a single request leaves empty. There are two kinds:
+//   - up to 32 rows (narrow): one wave takes pages by itself, bound by memory;
+//   - up to 128 rows (wide): the four waves of a workgroup take 32 rows each and share the pages through LDS, bound by the matrix cores
+//     and by the exponentials beside them.
+// The plan, made once a step on the device from the lengths, divides the workgroups of a KV head between the kinds in proportion to their
+// work, lays each kind's segments end to end (pages, and the start and end of a segment counted as pages) and cuts each line into equal
+// shares, one for each workgroup or wave: a long context is shared by many, short ones are strung together.
 //
-// A workgroup's 4 waves take blocks of two pages (32 tokens) in turns, K rows global -> LDS without passing through registers, V^T
-// straight into the registers of its product, both two blocks ahead, as attn_decode.hip does and explains; the rows of the block's
-// product are here any (request, head) pairs instead of the heads of one request. The waves' partial results meet in LDS.
 #include <algorithm>
 
 #include "device_ops.h"
@@ -22,21 +23,25 @@
 namespace sts {
 namespace {
 
-constexpr int AS_ROWS = 32;                     // rows of a segment: columns of a product
+constexpr int AS_ROWS = 32;                     // rows of a narrow segment: columns of a product
+constexpr int AS_TILE = 128;                    // rows of a wide one
 constexpr int AS_SLOTS = 512;                   // workgroups of a launch: two on each CU
-constexpr int AS_PLAN_THREADS = 1024;
-// Weights: a page read, and the start and end of a segment, in sixteenths of a page.
-constexpr int AS_PAGE_COST = 16, AS_START_COST = 96, AS_MIN_SHARE = AS_START_COST + 8 * AS_PAGE_COST;
+constexpr int AS_PLAN_THREADS = 512;
+constexpr int AS_JOIN_ROWS = 1024;              // up to so many (request, head) pairs, four waves join each
+// Start and end of a wide and of a narrow segment, and the smallest shares beyond them, in pages. A page takes a workgroup about as long in
+// either kind.
+constexpr int AS_WIDE_START = 16, AS_NARROW_START = 2, AS_WIDE_LEAST = 8, AS_NARROW_LEAST = 4;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // A piece of a segment: rows row0 .. row0 + rows - 1 (request * heads of a group + head) over the pages [pg0, pg1) of a request's
-// table, tokens from len on left out. part: number of its first row's partial result, -1: it finishes its rows.
-struct Item { int row0, rows, request, pg0, pg1, len, part, slot; };
+// table, tokens from len on left out. part: number of its first row's partial result, -1: it finishes its rows. once: nobody else reads the pages.
+struct Item { int row0, rows, request, pg0, pg1, len, part, once; };
+struct Range { Item first; int next, end, pad[2]; };              // items of a wave: the first, and next .. end - 1; none if its rows are 0. The four of a workgroup with wide ones have the same
 // Where a request's partial results are: head h in p_part + j * p_step + h, j < p_count, and s_part + j * heads + h, j < s_count.
 // done: its one piece finishes it. len < 0: its length is out of range.
 struct Parts { int p_part, p_step, p_count, s_part, s_count, len, done, pad; };
 struct Plan {
-  int* slot_first;                               // [slots + 1]: first item of each
+  Range* ranges;                                 // [slots][4]
   Item* items;
   Parts* parts;                                  // [n_requests]
   f32x2* stats;                                  // [partial row][kv head]: maximum (log2 units), sum
@@ -44,8 +49,9 @@ struct Plan {
 };
 
 int slots_of(int n_kv) { return std::max(1, AS_SLOTS / n_kv); }
-int max_items(int n, int n_kv) { return 2 * n + slots_of(n_kv); }           // pieces: one a segment and one a cut
-int64_t max_part_rows(int n, int n_q, int n_kv) { return (int64_t)2 * n * (n_q / n_kv) + (int64_t)slots_of(n_kv) * AS_ROWS; }
+// A segment is one piece, and one more for every share that ends in it; shares are a workgroup's of 128 rows or a wave's of 32.
+int max_items(int n, int n_kv) { return 2 * n + 4 * slots_of(n_kv); }
+int64_t max_part_rows(int n, int n_q, int n_kv) { return (int64_t)2 * n * (n_q / n_kv) + (int64_t)slots_of(n_kv) * AS_TILE; }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 // The workspace's parts behind each other; returns its size.
@@ -54,7 +60,7 @@ size_t lay_out(unsigned char* base, int n, int n_q, int n_kv, int d, Plan* p) {
   auto take = [&](size_t bytes) { unsigned char* q = base + at; at += up256(bytes); return q; };
   const size_t rows = (size_t)max_part_rows(n, n_q, n_kv) * n_kv;
   Plan q;
-  q.slot_first = reinterpret_cast<int*>(take((slots_of(n_kv) + 1) * sizeof(int)));
+  q.ranges = reinterpret_cast<Range*>(take(slots_of(n_kv) * 4 * sizeof(Range)));
   q.items = reinterpret_cast<Item*>(take(max_items(n, n_kv) * sizeof(Item)));
   q.parts = reinterpret_cast<Parts*>(take(n * sizeof(Parts)));
   q.stats = reinterpret_cast<f32x2*>(take(rows * sizeof(f32x2)));
@@ -66,159 +72,227 @@ size_t lay_out(unsigned char* base, int n, int n_q, int n_kv, int d, Plan* p) {
 // ---- the plan: one workgroup
 struct PlanCall { int n, groups, heads, slots, max_pages; const int *lens, *group_starts, *shared_lens; Plan plan; };
 
-// Exclusive sums over the workgroup's threads, and the totals.
-__device__ __forceinline__ long long plan_scan(long long v, long long* waves, long long* total) {
+// Exclusive sums over the workgroup's threads, and the totals, of N values.
+template <int N>
+__device__ __forceinline__ void plan_scan(int (&v)[N], int (&total)[N], int (*waves)[AS_PLAN_THREADS / 64]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long long x = v;
+  int x[N];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) waves[wave] = x;
-  __syncthreads();
-  long long before = 0, all = 0;
+  for (int i = 0; i < N; i++) {
+    x[i] = v[i];
 #pragma unroll
-  for (int w = 0; w < AS_PLAN_THREADS / 64; w++) {
-    if (w < wave) before += waves[w];
-    all += waves[w];
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(x[i], o, 64);
+      if (lane >= o) x[i] += y;
+    }
+    if (lane == 63) waves[i][wave] = x[i];
   }
   __syncthreads();
-  *total = all;
-  return before + x - v;
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < AS_PLAN_THREADS / 64; w++) {
+      const int y = waves[i][w];
+      before += w < wave ? y : 0;
+      all += y;
+    }
+    total[i] = all;
+    v[i] = before + x[i] - v[i];
+  }
+  __syncthreads();
+}
+
+// A line of segments cut into shares. A segment lies from `at` on: its start, then its pages. Where a share ends in it, it is cut at a whole
+// block of pages; of the shares that it lies in, the first and the last may get none of them. Shares are longer than a start and a
+// block, so those in between get some.
+struct Line {
+  int share, start, granule;
+  float inverse;
+  __device__ __forceinline__ int share_of(int at) const {
+    int k = (int)((float)at * inverse);
+    while (k * share > at) k--;
+    while ((k + 1) * share <= at) k++;
+    return k;
+  }
+  // pages of the segment that lie in the shares up to k
+  __device__ __forceinline__ int up_to(int at, int pages, int k) const {
+    const int room = (k + 1) * share - at - start;
+    return room >= pages ? pages : max(room, 0) & ~(granule - 1);
+  }
+  // first share with pages of a segment, and how many shares have some
+  __device__ __forceinline__ void cut(int at, int pages, int* first, int* count) const {
+    *first = 0; *count = 0;
+    if (pages == 0) return;
+    int k0 = share_of(at), k1 = share_of(at + start + pages - 1);
+    if (k0 < k1 && up_to(at, pages, k0) == 0) k0++;
+    if (k0 < k1 && up_to(at, pages, k1 - 1) == pages) k1--;
+    *first = k0; *count = k1 - k0 + 1;
+  }
+};
+
+// The last of count ascending values at or before x (the first is).
+template <typename I>
+__device__ __forceinline__ int last_up_to(const I* list, int count, int x) {
+  int lo = 0, hi = count;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((int)list[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
 }
 
 __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanCall c) {
-  extern __shared__ int lds[];
-  __shared__ long long waves[AS_PLAN_THREADS / 64];
-  __shared__ int malformed;
-  const int n = c.n, tid = threadIdx.x, per_tile = AS_ROWS / c.heads;        // requests of a tile
-  int *start = lds, *pages = start + n + 1, *tile0 = pages + n;              // by group: first request, shared pages, first tile
-  int* slot_at = tile0 + n + 1;                  // [slots + 1]
+  constexpr int N = OP_MAX_REQUESTS;
+  // by group: first request, shared pages, first tile; by tile: place on the line of wide segments; by segment: place on the line of narrow
+  // ones, first item, first partial row
+  __shared__ unsigned short start[N + 1], tile0[N + 1], item0[2 * N + 1];
+  __shared__ int lens[N], pages[N], wide_at[N + 1], narrow_at[2 * N + 1], part0[2 * N], waves[2][AS_PLAN_THREADS / 64], malformed;
+  const int n = c.n, groups = c.groups, tid = threadIdx.x;
   if (tid == 0) malformed = 0;
+  for (int i = tid; i < n; i += AS_PLAN_THREADS) {               // -1: longer than its table, or negative
+    const int l = c.lens[i];
+    lens[i] = l < 0 || l > c.max_pages * (long long)OP_PAGE ? -1 : l;
+  }
   __syncthreads();
   // groups whose starts do not lead from 0 to n in order are left aside: every request then reads all its pages for itself
-  const int groups = c.groups;
   for (int g = tid; groups > 0 && g <= groups; g += AS_PLAN_THREADS) {
     const int s = c.group_starts[g];
-    start[g] = s;
     const bool ok = s >= 0 && s <= n && (g > 0 || s == 0) && (g < groups ? s <= c.group_starts[g + 1] : s == n);
+    start[g] = (unsigned short)(ok ? s : 0);
     if (!ok) malformed = 1;
     if (g < groups) pages[g] = max(c.shared_lens[g], 0) / OP_PAGE;
   }
-  auto len = [&](int r) {                        // -1: longer than its table, or negative
-    const int l = c.lens[r];
-    return l < 0 || l > c.max_pages * (long long)OP_PAGE ? -1 : l;
-  };
   __syncthreads();
   const bool shares = groups > 0 && !malformed;
-  auto group_of = [&](int r) {
-    int lo = 0, hi = groups;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (start[mid] <= r) lo = mid; else hi = mid;
-    }
-    return lo;
-  };
   // a group shares what its shortest member holds in whole pages
   if (shares)
-    for (int i = tid; i < n; i += AS_PLAN_THREADS) atomicMin(&pages[group_of(i)], max(len(i), 0) / OP_PAGE);
+    for (int i = tid; i < n; i += AS_PLAN_THREADS) {
+      int* p = &pages[last_up_to(start, groups, i)];
+      const int held = max(lens[i], 0) / OP_PAGE;
+      if (*reinterpret_cast<volatile int*>(p) > held) atomicMin(p, held);      // seldom: the caller knows what they share
+    }
   __syncthreads();
-  // tiles of each group
+  // requests of a tile: a group that fills more than the columns of one product takes wide ones
+  auto per_tile = [&](int members) { return (members * c.heads > AS_ROWS ? AS_TILE : AS_ROWS) / c.heads; };
+  auto tiles_of = [&](int g) {
+    const int members = start[g + 1] - start[g], per = per_tile(members);
+    return pages[g] > 0 ? (members + per - 1) / per : 0;
+  };
   const int gper = (groups + AS_PLAN_THREADS - 1) / AS_PLAN_THREADS, g0 = min(groups, tid * gper), g1 = min(groups, g0 + gper);
-  long long tiles = 0, all_tiles = 0;
+  int tiles[1] = {0}, all_tiles[1];
   for (int g = g0; g < g1; g++) {
     if (!shares || start[g + 1] - start[g] < 2) pages[g] = 0;
-    tiles += pages[g] > 0 ? (start[g + 1] - start[g] + per_tile - 1) / per_tile : 0;
+    tiles[0] += tiles_of(g);
   }
-  tiles = plan_scan(tiles, waves, &all_tiles);
+  plan_scan(tiles, all_tiles, waves);
   for (int g = g0; g < g1; g++) {
-    tile0[g] = (int)tiles;
-    tiles += pages[g] > 0 ? (start[g + 1] - start[g] + per_tile - 1) / per_tile : 0;
+    tile0[g] = (unsigned short)tiles[0];
+    tiles[0] += tiles_of(g);
   }
-  if (tid == 0) tile0[groups] = (int)all_tiles;
-  for (int k = tid; k <= c.slots; k += AS_PLAN_THREADS) slot_at[k] = 0x7FFFFFFF;
   __syncthreads();
 
   // segments: the tiles, then the requests' own pages
-  const int T = (int)all_tiles, segments = T + n;
-  struct Segment { int row0, rows, request, pg0, pg1, len; };
+  const int T = all_tiles[0], segments = T + n;
+  struct Segment { int row0, rows, request, pg0, pages, len; };
   auto segment = [&](int s) {
     Segment x;
     if (s < T) {
-      int lo = 0, hi = groups;                   // the last group whose first tile is at or before s; it has tiles
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tile0[mid] <= s) lo = mid; else hi = mid;
-      }
-      const int r0 = start[lo] + (s - tile0[lo]) * per_tile;
-      x = {r0 * c.heads, min(per_tile, start[lo + 1] - r0) * c.heads, start[lo], 0, pages[lo], pages[lo] * OP_PAGE};
+      const int g = last_up_to(tile0, groups, s);                 // the last of several with that first tile: it has tiles
+      const int per = per_tile(start[g + 1] - start[g]), r0 = start[g] + (s - tile0[g]) * per;
+      x = {r0 * c.heads, min(per, start[g + 1] - r0) * c.heads, start[g], 0, pages[g], pages[g] * OP_PAGE};
     } else {
-      const int r = s - T, l = max(len(r), 0);
-      x = {r * c.heads, c.heads, r, shares ? pages[group_of(r)] : 0, (l + OP_PAGE - 1) / OP_PAGE, l};
+      const int r = s - T, l = lens[r], shared = shares ? pages[last_up_to(start, groups, r)] : 0;
+      x = {r * c.heads, c.heads, r, shared, (max(l, 0) + OP_PAGE - 1) / OP_PAGE - shared, l};
     }
     return x;
   };
-  auto cost_of = [&](const Segment& x) { return x.pg1 > x.pg0 ? AS_START_COST + (long long)(x.pg1 - x.pg0) * AS_PAGE_COST : 0; };
+  auto is_narrow = [](const Segment& x) { return x.rows <= AS_ROWS; };
+  auto cost_of = [&](const Segment& x) { return x.pages > 0 ? x.pages + (is_narrow(x) ? AS_NARROW_START : AS_WIDE_START) : 0; };
   const int per = (segments + AS_PLAN_THREADS - 1) / AS_PLAN_THREADS, s0 = min(segments, tid * per), s1 = min(segments, s0 + per);
-  long long cost = 0, all_cost;
-  for (int s = s0; s < s1; s++) cost += cost_of(segment(s));
-  const long long cost0 = plan_scan(cost, waves, &all_cost);
-  const long long share = max((all_cost + c.slots - 1) / c.slots, (long long)AS_MIN_SHARE);
-  // f(slot, first page, last page) for the pieces of a segment that lies from `at` on the line
-  auto pieces = [&](const Segment& x, long long at, auto f) {
-    const long long end = at + cost_of(x);
-    if (end == at) return;
-    int from = x.pg0;
-    for (long long k = at / share; from < x.pg1; k++) {
-      const long long cut = (k + 1) * share;     // pages up to the end of slot k, whole blocks of two
-      const long long up = (cut - at - AS_START_COST) / AS_PAGE_COST;
-      int to = cut >= end ? x.pg1 : x.pg0 + (int)max(up, 0ll) / 2 * 2;
-      to = min(max(to, from), x.pg1);
-      if (to > from) f((int)k, from, to);
-      from = to;
-    }
-  };
-  long long at = cost0, count = 0, rows = 0, all_items, all_rows;
+  Segment kept{};                                // the thread's segment where it has but one
+  if (per == 1 && s0 < s1) kept = segment(s0);
+  auto get = [&](int s) { return per == 1 ? kept : segment(s); };
+  int cost[2] = {0, 0}, all_cost[2];             // wide, narrow
   for (int s = s0; s < s1; s++) {
-    const Segment x = segment(s);
-    pieces(x, at, [&](int, int, int) { count++; rows += x.rows; });
-    at += cost_of(x);
+    const Segment x = get(s);
+    cost[is_narrow(x)] += cost_of(x);
   }
-  count = plan_scan(count, waves, &all_items);
-  rows = plan_scan(rows, waves, &all_rows);
-  at = cost0;
+  plan_scan(cost, all_cost, waves);
+  int wide = all_cost[0] == 0 ? 0 : (int)(c.slots * ((float)all_cost[0] / ((float)all_cost[0] + (float)all_cost[1])) + 0.5f);
+  wide = min(max(wide, (int)(all_cost[0] > 0)), c.slots - (all_cost[1] > 0));
+  const int narrow = 4 * (c.slots - wide);
+  auto line = [&](int total, int count, int start, int least, int granule) {
+    const int share = max((total + max(count, 1) - 1) / max(count, 1), start + least);
+    return Line{share, start, granule, 1.f / (float)share};
+  };
+  const Line lines[2] = {line(all_cost[0], wide, AS_WIDE_START, AS_WIDE_LEAST, 4), line(all_cost[1], narrow, AS_NARROW_START, AS_NARROW_LEAST, 2)};
+  int sums[2] = {0, 0}, all[2], at[2] = {cost[0], cost[1]};        // items (narrow ones in the upper half), partial rows
   for (int s = s0; s < s1; s++) {
-    const Segment x = segment(s);
-    int mine = 0;
-    pieces(x, at, [&](int, int, int) { mine++; });
-    const bool own = s >= T;
-    const bool done = own && mine == 1 && x.pg0 == 0;
-    const int part = (int)rows;
-    pieces(x, at, [&](int slot, int from, int to) {
-      c.plan.items[count] = Item{x.row0, x.rows, x.request, from, to, x.len, done ? -1 : (int)rows, slot};
-      atomicMin(&slot_at[slot], (int)count);
-      count++;
-      rows += x.rows;
-    });
-    if (own) {
+    const Segment x = get(s);
+    const int kind = is_narrow(x);
+    int first, count;
+    lines[kind].cut(at[kind], x.pages, &first, &count);
+    at[kind] += cost_of(x);
+    sums[0] += kind ? count << 16 : count;
+    sums[1] += count * x.rows;
+  }
+  plan_scan(sums, all, waves);
+  at[0] = cost[0]; at[1] = cost[1];
+  for (int s = s0; s < s1; s++) {
+    const Segment x = get(s);
+    const int kind = is_narrow(x);
+    int first, count;
+    lines[kind].cut(at[kind], x.pages, &first, &count);
+    if (s < T) wide_at[s] = at[0];
+    narrow_at[s] = at[1];
+    item0[s] = (unsigned short)(kind ? (all[0] & 0xFFFF) + (sums[0] >> 16) : sums[0] & 0xFFFF);      // wide ones first
+    part0[s] = sums[1];
+    if (s >= T) {
       Parts* p = c.plan.parts + x.request;
-      p->s_part = part; p->s_count = mine; p->len = len(x.request); p->done = done;
+      p->s_part = sums[1]; p->s_count = count; p->len = x.len; p->done = count == 1 && x.pg0 == 0;
       if (x.pg0 == 0) p->p_count = 0;
     } else {
-      for (int i = 0; i < x.rows; i += c.heads) {
-        Parts* p = c.plan.parts + (x.row0 + i) / c.heads;
-        p->p_part = part + i; p->p_step = x.rows; p->p_count = mine;
+      Parts* p = c.plan.parts + x.row0 / c.heads;
+      for (int i = 0; i < x.rows; i += c.heads, p++) { p->p_part = sums[1] + i; p->p_step = x.rows; p->p_count = count; }
+    }
+    at[kind] += cost_of(x);
+    sums[0] += kind ? count << 16 : count;
+    sums[1] += count * x.rows;
+  }
+  if (tid == 0) { wide_at[T] = all_cost[0]; narrow_at[segments] = all_cost[1]; }
+  __syncthreads();
+  // The items of a share, by a thread of its own. Neighbouring narrow shares go to different workgroups.
+  for (int i = tid; i < wide + narrow; i += AS_PLAN_THREADS) {
+    const int kind = i >= wide, k = kind ? i - wide : i, *places = kind ? narrow_at : wide_at, count_of = kind ? segments : T;
+    const Line& l = lines[kind];
+    Range r{};
+    if ((long long)k * l.share < all_cost[kind]) {
+      for (int s = last_up_to(places, count_of, k * l.share); s < count_of && places[s] < (k + 1) * l.share; s++) {
+        if (places[s + 1] == places[s]) continue;                 // of the other kind, or without pages
+        const Segment x = segment(s);
+        int first, count;
+        l.cut(places[s], x.pages, &first, &count);
+        if (k < first || k >= first + count) continue;
+        const int from = k == first ? 0 : l.up_to(places[s], x.pages, k - 1), to = k == first + count - 1 ? x.pages : l.up_to(places[s], x.pages, k);
+        const int item = item0[s] + k - first;
+        const bool done = s >= T && x.pg0 == 0 && count == 1;     // a request without a shared part whose pages are all here
+        const Item it{x.row0, x.rows, x.request, x.pg0 + from, x.pg0 + to, x.len, done ? -1 : part0[s] + (k - first) * x.rows, s >= T};
+        if (r.end == 0) {
+          r.first = it;
+          r.next = item + 1;
+        } else {
+          c.plan.items[item] = it;
+        }
+        r.end = item + 1;
       }
     }
-    at += cost_of(x);
-  }
-  __syncthreads();
-  // a slot without items begins where the next one does
-  for (int k = tid; k <= c.slots; k += AS_PLAN_THREADS) {
-    int j = k;
-    while (j < c.slots && slot_at[j] == 0x7FFFFFFF) j++;
-    c.plan.slot_first[k] = j < c.slots ? slot_at[j] : (int)all_items;
+    if (kind) {
+      const int others = c.slots - wide;
+      c.plan.ranges[(wide + k % others) * 4 + k / others] = r;
+    } else {
+      for (int w = 0; w < 4; w++) c.plan.ranges[k * 4 + w] = r;
+    }
   }
 }
 
@@ -239,7 +313,7 @@ struct AttnCall {
   const int* tables; long long table_stride;
   int n, n_q, n_kv, heads, pool_pages;
   float scale_log2e;
-  bool q_vec;                                    // q's rows can be loaded 16 bytes at a time
+  bool q_vec, out_vec;                           // rows can be loaded 16 bytes, stored 8 bytes at a time
   Plan plan;
 };
 
@@ -248,18 +322,29 @@ __device__ __forceinline__ float half_swap_max_f(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// A value that the compiler derives nothing from earlier on: addresses made from it are not kept in registers over a whole loop of items.
+__device__ __forceinline__ int fresh(int x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(x));
+#endif
+  return x;
+}
+
 constexpr int AS_LDS_BASE = 1024;                // buffers filled by direct-to-LDS loads stay clear of address 0
 template <int D>
-constexpr int attn_shared_lds() { return AS_LDS_BASE + std::max(4 * 2 * 2 * 16 * D * 2, 4 * AS_ROWS * (D + 2) * 4); }
+constexpr int attn_shared_lds() { return AS_LDS_BASE + 4 * 2 * 2 * 16 * D * 2; }   // two blocks of K for each wave; two tiles of K and V^T; 128 rows of output
 
-template <typename T, int D>
-__device__ __forceinline__ void run_item(unsigned char* smem, const AttnCall<T>& c, const Item& it, int kvh) {
+// ---- narrow items, one wave: blocks of two pages (32 tokens), K rows global -> LDS without passing through registers, V^T straight into the
+// registers of its product, both two blocks ahead, with the waits of attn_decode.hip, which explains the order of the tokens.
+// ONCE: pages that nobody else reads are fetched with the non-temporal hint.
+template <typename T, int D, bool ONCE>
+__device__ __forceinline__ void run_narrow(unsigned char* smem, const AttnCall<T>& c, const Item& it, int kvh) {
   typedef typename Mfma<T>::V V;
   constexpr int KSTEPS = D / 16, DB = D / 32;
   constexpr int ROWB = D * 2, CPR = D / 8, RPI = 64 / CPR, IPP = 16 / RPI;   // K row bytes, 16-byte chunks, rows per load, loads per page
   constexpr int PAGE_KB = 16 * ROWB, STAGE = 2 * PAGE_KB;
   constexpr int LOADS = 2 * IPP + 2 * DB;            // loads of a block: K to LDS, V^T to registers
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
+  const int tid = fresh(threadIdx.x), lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int npg = it.pg1 - it.pg0, nblk = (npg + 1) >> 1;
   const int nt = min(it.len, it.pg1 * OP_PAGE) - it.pg0 * OP_PAGE;           // tokens
@@ -269,12 +354,12 @@ __device__ __forceinline__ void run_item(unsigned char* smem, const AttnCall<T>&
   // is not followed: page 0 is read for it, and the rows come out as NaN.
   bool bad = false;
   auto load_pages = [&](int window) {
-    const int page = npg > 0 ? table[min(window * 64 + lane, npg - 1)] : 0;
+    const int page = table[min(window * 64 + lane, npg - 1)];
     const bool out = (unsigned)page >= (unsigned)c.pool_pages;
     bad |= out;
     return out ? 0 : page;
   };
-  int window = 0, pages_now = load_pages(0), pages_next = load_pages(1);
+  int window = 0, pages_now = load_pages(0), pages_next = npg > 64 ? load_pages(1) : 0;
   auto page_base = [&](int i) -> const T* {           // windows are asked for in order
     const int j = __builtin_amdgcn_readfirstlane(min(i, npg - 1));
     if ((j >> 6) > window) { window++; pages_now = pages_next; pages_next = load_pages(window + 1); }
@@ -295,21 +380,27 @@ __device__ __forceinline__ void run_item(unsigned char* smem, const AttnCall<T>&
     for (int u = 0; u < 2; u++) {
       base[u] = page_base(2 * b + u);
 #pragma unroll
-      for (int j = 0; j < IPP; j++) load_to_lds16(base[u] + ksrc[j], kbuf + stage * STAGE + u * PAGE_KB + j * 1024);
+      for (int j = 0; j < IPP; j++) {
+        unsigned char* to = kbuf + stage * STAGE + u * PAGE_KB + j * 1024;
+        if constexpr (ONCE) load_to_lds16_nt(base[u] + ksrc[j], to); else load_to_lds16(base[u] + ksrc[j], to);
+      }
     }
   };
   auto load_v = [&](u32x4 (&vr)[2][DB]) {
 #pragma unroll
     for (int u = 0; u < 2; u++)
 #pragma unroll
-      for (int bb = 0; bb < DB; bb++) vr[u][bb] = *reinterpret_cast<const u32x4*>(base[u] + (size_t)16 * D + (bb * 32 + l32) * 16 + lh * 8);
+      for (int bb = 0; bb < DB; bb++) {
+        const u32x4* from = reinterpret_cast<const u32x4*>(base[u] + (size_t)16 * D + (bb * 32 + l32) * 16 + lh * 8);
+        if constexpr (ONCE) vr[u][bb] = __builtin_nontemporal_load(from); else vr[u][bb] = *from;
+      }
   };
 
   // Q^T operand: column l32 is row l32 of the item
   V qf[KSTEPS];
-  const int vrow = it.row0 + min(l32, it.rows - 1);
+  const int vrow = it.row0 + min(l32, it.rows - 1), request = vrow / c.heads, head = kvh * c.heads + vrow % c.heads;
   {
-    const T* q = c.q + (long long)(vrow / c.heads) * c.q_stride + (kvh * c.heads + vrow % c.heads) * D + lh * 8;
+    const T* q = c.q + (long long)request * c.q_stride + head * D + lh * 8;
 #pragma unroll
     for (int kk = 0; kk < KSTEPS; kk++) {
       if (c.q_vec) qf[kk] = *reinterpret_cast<const V*>(q + kk * 16);
@@ -340,8 +431,7 @@ __device__ __forceinline__ void run_item(unsigned char* smem, const AttnCall<T>&
   };
   auto softmax_pv = [&](int b, f32x16& s, u32x4 (&vr)[2][DB]) {
     const int t_base = b * 32 + 8 * lh;               // register r: page r >> 3 of the pair, token 8 * half + (r & 7)
-    const bool tail = b * 32 + 32 > nt;               // wave-uniform: some tokens of the block are left out
-    if (tail) {
+    if (b * 32 + 32 > nt) {                           // wave-uniform: some tokens of the block are left out
 #pragma unroll
       for (int r = 0; r < 16; r++)
         if (t_base + (r >> 3) * 16 + (r & 7) >= nt) s[r] = -INFINITY;
@@ -391,133 +481,368 @@ __device__ __forceinline__ void run_item(unsigned char* smem, const AttnCall<T>&
   };
   auto fence = [] { __asm__ volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); };
   u32x4 va[2][DB], vb[2][DB];
-  const int nmine = wv < nblk ? (nblk - wv + 3) >> 2 : 0;
   auto step = [&](int i, int stage, u32x4 (&vr)[2][DB]) {
-    const int b = wv + 4 * i;
-    if (i + 1 < nmine) wait_vmem<LOADS>(); else wait_vmem<0>();
+    if (i + 1 < nblk) wait_vmem<LOADS>(); else wait_vmem<0>();
     fence();
     f32x16 s;
     scores(stage, s);
-    if (i + 2 < nmine) {
+    if (i + 2 < nblk) {
       __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): every K operand of this block has been read
       fence();
-      issue_k(b + 8, stage);
+      issue_k(i + 2, stage);
     }
-    softmax_pv(b, s, vr);
-    if (i + 2 < nmine) load_v(vr);
+    softmax_pv(i, s, vr);
+    if (i + 2 < nblk) load_v(vr);
   };
-  if (nmine > 0) {
-    issue_k(wv, 0); load_v(va);
-    if (nmine > 1) { issue_k(wv + 4, 1); load_v(vb); }
-    for (int i = 0; i < nmine; i += 2) {
-      step(i, 0, va);
-      if (i + 1 < nmine) step(i + 1, 1, vb);
-    }
+  issue_k(0, 0); load_v(va);
+  if (nblk > 1) { issue_k(1, 1); load_v(vb); }
+  for (int i = 0; i < nblk; i += 2) {
+    step(i, 0, va);
+    if (i + 1 < nblk) step(i + 1, 1, vb);
   }
   l_run += __shfl_xor(l_run, 32, 64);
   if (__any(bad)) l_run = NAN;
 
-  // ---- the four waves' results meet in LDS (the K buffers are free once every wave is past its loop)
-  __syncthreads();
-  float* sm = reinterpret_cast<float*>(smem + AS_LDS_BASE);              // [4][rows] maxima, then sums, in log2 units
-  float* sl = sm + 4 * AS_ROWS;
-  float* red = sl + 4 * AS_ROWS;                                         // [4][rows][D]
-  const int rows = it.rows;
-  const float m2 = m_ref * c.scale_log2e;
-  if (lane < 32) { sm[wv * AS_ROWS + lane] = m2; sl[wv * AS_ROWS + lane] = l_run; }
-  __syncthreads();
-  auto max_of = [&](int g) { return fmaxf(fmaxf(sm[g], sm[AS_ROWS + g]), fmaxf(sm[2 * AS_ROWS + g], sm[3 * AS_ROWS + g])); };
-  auto sum_of = [&](int g, float mall) {
-    float l = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; w++) {
-      const float m = sm[w * AS_ROWS + g], x = sl[w * AS_ROWS + g];
-      l += m == -INFINITY ? x : x * __builtin_amdgcn_exp2f(m - mall);    // 0 of a wave without scores above -inf, or NaN
-    }
-    return l;
-  };
-  if (l32 < rows) {
-    const float mall = max_of(l32), f = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - mall);
-#pragma unroll
-    for (int bb = 0; bb < DB; bb++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) red[(wv * AS_ROWS + l32) * D + bb * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)] = o[bb][r] * f;
-  }
-  __syncthreads();
-  for (int i = tid; i < rows * D; i += 256) {
-    const int g = i / D, e = i % D;
-    const float sum = red[i] + red[AS_ROWS * D + i] + red[2 * AS_ROWS * D + i] + red[3 * AS_ROWS * D + i];
+  // a lane has four elements in a row of its row's output, 32 bb + 8 r4 + 4 lh
+  if (l32 < it.rows) {
+    const float m2 = m_ref * c.scale_log2e;
     if (it.part < 0) {
-      const float mall = max_of(g), l = sum_of(g, mall);
-      const int v = it.row0 + g, r = v / c.heads, h = kvh * c.heads + v % c.heads;
-      c.out[(long long)r * c.out_stride + h * D + e] = (T)(sum / l);
-      if (e == 0 && c.lse) c.lse[(long long)r * c.n_q + h] = LN2 * (mall + __builtin_amdgcn_logf(l));
+      T* out = c.out + (long long)request * c.out_stride + head * D + 4 * lh;
+      const float f = 1.f / l_run;
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; r4++) {
+          typedef T T4 __attribute__((ext_vector_type(4)));
+          T4 v;
+#pragma unroll
+          for (int e = 0; e < 4; e++) v[e] = (T)(o[bb][4 * r4 + e] * f);
+          T* to = out + bb * 32 + 8 * r4;
+          if (c.out_vec) *reinterpret_cast<T4*>(to) = v;
+          else
+#pragma unroll
+            for (int e = 0; e < 4; e++) to[e] = v[e];
+        }
+      if (lh == 0 && c.lse) c.lse[(long long)request * c.n_q + head] = LN2 * (m2 + __builtin_amdgcn_logf(l_run));
     } else {
-      c.plan.outs[((size_t)(it.part + g) * c.n_kv + kvh) * D + e] = sum;
+      const size_t row = (size_t)(it.part + l32) * c.n_kv + kvh;
+      float* out = c.plan.outs + row * D + 4 * lh;
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; r4++) *reinterpret_cast<f32x4*>(out + bb * 32 + 8 * r4) = f32x4{o[bb][4 * r4], o[bb][4 * r4 + 1], o[bb][4 * r4 + 2], o[bb][4 * r4 + 3]};
+      if (lh == 0) c.plan.stats[row] = f32x2{m2, l_run};
     }
   }
-  if (it.part >= 0 && tid < rows) {
-    const float mall = max_of(tid);
-    c.plan.stats[(size_t)(it.part + tid) * c.n_kv + kvh] = f32x2{mall, sum_of(tid, mall)};
+}
+
+// ---- wide items, a workgroup: every wave takes 32 rows over all the pages. Tiles of four pages go global -> LDS, two stages deep, a page
+// a wave; products, order of the tokens and softmax as in attn_prefill.hip, whose queries lie in a row where these come from any request.
+constexpr float AS_RESCALE_LOG2 = 8.f;           // the reference maximum moves when a score outgrows it by 2^8
+
+template <typename T, int D>
+__device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>& c, const Item& it, int kvh) {
+  typedef typename Mfma<T>::V V;
+  constexpr int KSTEPS = D / 16, DB = D / 32;
+  constexpr int ROWB = D * 2, CPR = D / 8, RPI = 64 / CPR, IPP = 16 / RPI;     // K row bytes, 16-byte chunks, rows per load, loads per page
+  constexpr int PAGE = 16 * ROWB, TILE = 4 * PAGE, STAGE = 2 * TILE;           // bytes of a K (or V^T) page, tile; of a stage
+  const int tid = fresh(threadIdx.x), lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int npg = it.pg1 - it.pg0, tiles = (npg + 3) >> 2;
+  const int* table = c.tables + (long long)it.request * c.table_stride + it.pg0;
+  const int my_rows = min(it.rows - wave * 32, 32);                            // none or fewer: the wave only fetches
+
+  V qf[KSTEPS];
+  {
+    const int v = it.row0 + min(wave * 32 + l32, it.rows - 1);
+    const T* q = c.q + (long long)(v / c.heads) * c.q_stride + (kvh * c.heads + v % c.heads) * D + 8 * lh;
+#pragma unroll
+    for (int j = 0; j < KSTEPS; j++) {
+      if (c.q_vec) qf[j] = *reinterpret_cast<const V*>(q + 16 * j);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; e++) qf[j][e] = q[16 * j + e];
+    }
   }
-  __syncthreads();                                   // before the next item's K lands there
+  // This wave's page of tile kt; past the last page that page again, whose products are left out.
+  bool bad = false;
+  const size_t page_stride = (size_t)c.n_kv * 2 * OP_PAGE * D;
+  const T* pool_h = c.pool + (size_t)kvh * 2 * OP_PAGE * D;
+  auto page_id = [&](int kt) {
+    const int page = table[min(kt * 4 + wave, npg - 1)];
+    const bool out = (unsigned)page >= (unsigned)c.pool_pages;
+    bad |= out;
+    return out ? 0 : page;
+  };
+  unsigned k_off[IPP];
+#pragma unroll
+  for (int j = 0; j < IPP; j++) {
+    const int row = j * RPI + lane / CPR, swz = D == 128 ? row : (row >> 1) & 7;
+    k_off[j] = (unsigned)row * ROWB + (unsigned)((lane % CPR) ^ swz) * 16u;
+  }
+  unsigned char* arena = smem + AS_LDS_BASE;
+  auto issue = [&](int stage, int page) {
+    const T* pb = pool_h + (size_t)__builtin_amdgcn_readfirstlane(page) * page_stride;
+    unsigned char* dst = arena + stage * STAGE + wave * PAGE;
+#pragma unroll
+    for (int j = 0; j < IPP; j++) lds_dma16(pb, k_off[j], dst + j * 1024);
+#pragma unroll
+    for (int j = 0; j < IPP; j++) lds_dma16(pb + (size_t)16 * D, (unsigned)(j * 1024 + lane * 16), dst + TILE + j * 1024);
+  };
+  const int tok = (l32 & 3) | (((l32 >> 3) & 1) << 2) | (((l32 >> 2) & 1) << 3);
+  const int k_row = (l32 >> 4) * PAGE + tok * ROWB;
+  int k_slot[KSTEPS];
+#pragma unroll
+  for (int j = 0; j < KSTEPS; j++) k_slot[j] = k_row + ((2 * j + lh) ^ (D == 128 ? tok : (tok >> 1) & 7)) * 16;
+  const int v_lane = TILE + l32 * 32 + lh * 16;          // V^T operand: d row l32 of a 32-row block, tokens 8 lh .. of a page
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int b = 0; b < DB; b++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) o[b][r] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f;
+  issue(0, page_id(0));
+  int next_page = page_id(1);
+  auto tile = [&](int kt, auto whole) {
+    const unsigned char* st = arena + (kt & 1) * STAGE;
+    const int here = decltype(whole)::value ? 4 : npg - kt * 4;                // pages of the tile
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) s[kb][r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+    {
+      V kf[2][2];
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++) kf[0][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[0]);
+#pragma unroll
+      for (int j = 0; j < KSTEPS; j++) {
+        const int a = j & 1, b = a ^ 1;
+        if (j + 1 < KSTEPS) {
+#pragma unroll
+          for (int kb = 0; kb < 2; kb++) kf[b][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[j + 1]);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) s[kb] = Mfma<T>::mul(kf[a][kb], qf[j], s[kb]);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+      for (int j = 0; j + 1 < KSTEPS; j++) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    V vf[2][DB];                                           // first V^T operands: in flight during the softmax arithmetic
+#pragma unroll
+    for (int b = 0; b < DB; b++) vf[0][b] = *reinterpret_cast<const V*>(st + v_lane + b * 1024);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!decltype(whole)::value) {
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          if (2 * kb + (r >> 3) >= here) s[kb][r] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[kb][r]);
+    mx = half_swap_max_f(mx);
+    const bool grow = (mx - m_ref) * c.scale_log2e > AS_RESCALE_LOG2;          // false when both are -inf (NaN)
+    if (__any(grow)) {                                                         // wave-uniform
+      const float m_upd = grow ? mx : m_ref;
+      const float corr = (m_upd == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_upd) * c.scale_log2e);
+      m_ref = m_upd;
+      l_run *= corr;
+#pragma unroll
+      for (int b = 0; b < DB; b++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[b][r] *= corr;
+    }
+    const float nm = (m_ref == -INFINITY) ? 0.f : -m_ref * c.scale_log2e;
+    float rs = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c.scale_log2e, nm));
+        s[kb][r] = p;
+        rs += p;
+      }
+    l_run += rs;                                                               // this half's keys; halves are added at the end
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      const int a = g & 1, b2 = a ^ 1;
+      if (g + 1 < 4) {
+#pragma unroll
+        for (int b = 0; b < DB; b++) vf[b2][b] = *reinterpret_cast<const V*>(st + v_lane + (g + 1) * PAGE + b * 1024);
+      }
+      V pb;
+#pragma unroll
+      for (int e = 0; e < 8; e++) pb[e] = (T)s[g >> 1][8 * (g & 1) + e];
+      if (decltype(whole)::value || g < here) {
+#pragma unroll
+        for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pb, o[b]);
+      }
+    }
+    if constexpr (decltype(whole)::value) {
+#pragma unroll
+      for (int g = 0; g + 1 < 4; g++) {
+        __builtin_amdgcn_sched_group_barrier(0x100, DB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, DB, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, DB, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto landed = [&](int kt) {                              // every wave waits for its own page, and nobody reads the other stage any more
+    wait_vmem<0>();
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 1 < tiles) {
+      issue((kt + 1) & 1, next_page);
+      next_page = page_id(kt + 2);
+    }
+  };
+  const int whole = npg >> 2;
+  for (int kt = 0; kt < whole; kt++) {
+    landed(kt);
+    if (my_rows > 0) tile(kt, std::true_type{});           // wave-uniform
+  }
+  if (whole < tiles) {
+    landed(whole);
+    if (my_rows > 0) tile(whole, std::false_type{});
+  }
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (__syncthreads_or(bad)) l_run = NAN;                // LDS now takes the output
+  if (my_rows > 0) {
+    // whole rows through LDS: 16-byte chunks, swizzled by row
+    constexpr int OROWB = D * 4, OCPR = OROWB / 16, ORPI = 64 / OCPR;
+    unsigned char* buf = arena + wave * 32 * OROWB;
+    const int lane = fresh(tid & 63), l32 = lane & 31, lh = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < DB; b++)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; r4++)
+        *reinterpret_cast<f32x4*>(buf + l32 * OROWB + ((b * 8 + 2 * r4 + lh) ^ (l32 % 16)) * 16) = f32x4{o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int r0 = lane / OCPR, ch = lane % OCPR, part = it.part + wave * 32;
+#pragma unroll
+    for (int i = 0; i < 32 / ORPI; i++) {
+      const int r = i * ORPI + r0;
+      const f32x4 v = *reinterpret_cast<const f32x4*>(buf + r * OROWB + (ch ^ (r % 16)) * 16);
+      if (r < my_rows) *reinterpret_cast<f32x4*>(c.plan.outs + ((size_t)(part + r) * c.n_kv + kvh) * D + ch * 4) = v;
+    }
+    if (lane < my_rows) c.plan.stats[(size_t)(part + lane) * c.n_kv + kvh] = f32x2{m_ref * c.scale_log2e, l_run};
+  }
+  __syncthreads();                                       // before the next item's K lands there
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256, 2) attn_shared_kernel(AttnCall<T> c) {
   __shared__ __align__(16) unsigned char smem[attn_shared_lds<D>()];
+  // With 8 KV heads a head's workgroups are all on one XCD: the tiles of a prefix find each other's pages in its L2.
   const int slot = blockIdx.x / c.n_kv, kvh = blockIdx.x % c.n_kv;
-  const int first = c.plan.slot_first[slot], end = c.plan.slot_first[slot + 1];
-  for (int i = first; i < end; i++) run_item<T, D>(smem, c, c.plan.items[i], kvh);
+  const Range r = c.plan.ranges[slot * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
+  if (r.first.rows == 0) return;
+  Item it = r.first;
+  for (int i = r.next;; i++) {
+    if (it.rows > AS_ROWS) run_wide<T, D>(smem, c, it, kvh);
+    else if (it.once) run_narrow<T, D, true>(smem, c, it, kvh);
+    else run_narrow<T, D, false>(smem, c, it, kvh);
+    if (i >= r.end) break;
+    it = c.plan.items[i];
+  }
 }
 
-// Joins the partial results of a (request, query head): a wave each, d / 64 elements a lane.
-template <typename T, int D>
+// Joins the partial results of a (request, query head): WAVES waves each, a lane four elements of every 256 / D-th part (of a wave's share).
+template <typename T, int D, int WAVES>
 __global__ void __launch_bounds__(256) attn_shared_join_kernel(AttnCall<T> c) {
-  constexpr int PER = D / 64;
-  const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int LANES = D / 4, APART = 64 / LANES * WAVES;       // lanes of a part, parts side by side
+  __shared__ f32x4 sums[WAVES > 1 ? WAVES : 1][LANES];
+  __shared__ float ls[WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + wave;
   if (at >= c.n * c.n_q) return;
   const int r = at / c.n_q, head = at % c.n_q, kvh = head / c.heads, h = head % c.heads;
   const Parts p = c.plan.parts[r];
-  if (p.done && p.len >= 0) return;
+  if (p.done) return;
   const int count = p.len < 0 ? 0 : p.p_count + p.s_count;
   auto row_of = [&](int j) { return (size_t)((j < p.p_count ? p.p_part + j * p.p_step : p.s_part + (j - p.p_count) * c.heads) + h) * c.n_kv + kvh; };
   float m = -INFINITY;
   for (int j = lane; j < count; j += 64) m = fmaxf(m, c.plan.stats[row_of(j)][0]);
   m = wave_max(m);
-  float l = 0.f, o[PER];
-#pragma unroll
-  for (int e = 0; e < PER; e++) o[e] = 0.f;
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const int first = (WAVES > 1 ? wave * (64 / LANES) : 0) + lane / LANES, e4 = lane % LANES * 4;
 #pragma unroll 4
-  for (int j = 0; j < count; j++) {
+  for (int j = first; j < count; j += APART) {
     const size_t row = row_of(j);
     const f32x2 st = c.plan.stats[row];
+    const f32x4 x = *reinterpret_cast<const f32x4*>(c.plan.outs + row * D + e4);
     const float w = st[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - m);
-    l += st[0] == -INFINITY ? st[1] : st[1] * w;
+    l += st[0] == -INFINITY ? st[1] : st[1] * w;                 // 0 of a part without scores above -inf, or NaN
 #pragma unroll
-    for (int e = 0; e < PER; e++) o[e] += c.plan.outs[row * D + lane * PER + e] * w;
+    for (int e = 0; e < 4; e++) o[e] += x[e] * w;
   }
-  T* out = c.out + (long long)r * c.out_stride + head * D + lane * PER;
-  const bool none = p.len == 0;                      // nothing to attend to: zeros, and the logarithm of an empty sum
 #pragma unroll
-  for (int e = 0; e < PER; e++) out[e] = (T)(p.len < 0 ? NAN : none ? 0.f : o[e] / l);
-  if (lane == 0 && c.lse) c.lse[(long long)r * c.n_q + head] = p.len < 0 ? NAN : none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
+  for (int s = LANES; s < 64; s <<= 1) {
+    l += __shfl_xor(l, s, 64);
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] += __shfl_xor(o[e], s, 64);
+  }
+  if constexpr (WAVES > 1) {
+    if (lane < LANES) sums[wave][lane] = o;
+    if (lane == 0) ls[wave] = l;
+    __syncthreads();
+    if (wave > 0) return;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) l += ls[w];
+    if (lane < LANES) {
+      o = sums[0][lane];
+#pragma unroll
+      for (int w = 1; w < WAVES; w++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] += sums[w][lane][e];
+    }
+  }
+  if (lane < LANES) {
+    T* out = c.out + (long long)r * c.out_stride + head * D + e4;
+    const bool none = p.len == 0;                      // nothing to attend to: zeros, and the logarithm of an empty sum
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 v;
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = (T)(p.len < 0 ? NAN : none ? 0.f : o[e] / l);
+    if (c.out_vec) *reinterpret_cast<T4*>(out) = v;
+    else
+#pragma unroll
+      for (int e = 0; e < 4; e++) out[e] = v[e];
+    if (lane == 0 && c.lse) c.lse[(long long)r * c.n_q + head] = p.len < 0 ? NAN : none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
+  }
 }
 
 template <typename T, int D>
 hipError_t launch_attn(hipStream_t s, const AttnCall<T>& c) {
   hipError_t e = launch(attn_shared_kernel<T, D>, dim3(slots_of(c.n_kv) * c.n_kv), dim3(256), 0, s, c);
-  if (e == hipSuccess) e = launch(attn_shared_join_kernel<T, D>, dim3((unsigned)(((int64_t)c.n * c.n_q + 3) / 4)), dim3(256), 0, s, c);
-  return e;
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)c.n * c.n_q;
+  if (rows <= AS_JOIN_ROWS) return launch(attn_shared_join_kernel<T, D, 4>, dim3((unsigned)rows), dim3(256), 0, s, c);
+  return launch(attn_shared_join_kernel<T, D, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, c);
 }
 
 bool sizes_ok(int n, int n_q, int n_kv, int d) {
-  return n >= 0 && n <= OP_MAX_REQUESTS && n_kv >= 1 && n_kv <= AS_SLOTS && n_q >= n_kv && n_q % n_kv == 0 && n_q / n_kv <= AS_ROWS && (d == 64 || d == 128);
+  return n >= 0 && n <= OP_MAX_REQUESTS && n_kv >= 1 && n_kv <= AS_SLOTS / 2 && n_q >= n_kv && n_q % n_kv == 0 && n_q / n_kv <= AS_ROWS && (d == 64 || d == 128);
 }
 // The batch's description, without what a call of one layer adds.
 int check_batch(const sts_attn_batch* b, Plan* plan) {
   if (!b || (b->dtype != STS_BF16 && b->dtype != STS_F16) || !sizes_ok(b->n_requests, b->n_q, b->n_kv, b->d)) return STS_EINVAL;
-  if (b->n_groups < 0 || b->n_groups > b->n_requests || b->pool_pages < 0 || b->max_pages < 0 || b->max_pages > (1 << 26) || b->table_stride < b->max_pages) return STS_EINVAL;
+  if (b->n_groups < 0 || b->n_groups > b->n_requests || b->pool_pages < 0 || b->max_pages < 0 || (int64_t)b->n_requests * b->max_pages > (1 << 28) || b->table_stride < b->max_pages) return STS_EINVAL;
   if (b->n_requests == 0) return STS_OK;
   if (!b->lens || (b->max_pages > 0 && !b->tables) || (b->n_groups > 0 && (!b->group_starts || !b->shared_lens))) return STS_EINVAL;
   if (!b->workspace || !aligned(b->workspace, 256)) return STS_EINVAL;
@@ -544,14 +869,14 @@ extern "C" int sts_op_attn_shared_plan(const sts_attn_batch* b, void* stream) {
   if (dev.error() != hipSuccess) return op_result(dev.error());
   const int n = b->n_requests, slots = slots_of(b->n_kv);
   const PlanCall c{n, b->n_groups, b->n_q / b->n_kv, slots, b->max_pages, b->lens, b->group_starts, b->shared_lens, plan};
-  return op_result(launch(attn_shared_plan_kernel, dim3(1), dim3(AS_PLAN_THREADS), (size_t)(3 * n + 2 + slots + 1) * sizeof(int), s, c));
+  return op_result(launch(attn_shared_plan_kernel, dim3(1), dim3(AS_PLAN_THREADS), 0, s, c));
 }
 
 template <typename T>
 static int attn_shared(const sts_attn_batch* b, const Plan& plan, const void* q, int64_t q_stride, const void* pool, void* out, int64_t out_stride, float* lse, float scale, hipStream_t s) {
-  const bool q_vec = aligned(q, 16) && q_stride % 8 == 0;
+  const bool q_vec = aligned(q, 16) && q_stride % 8 == 0, out_vec = aligned(out, 8) && out_stride % 4 == 0;
   const AttnCall<T> c{reinterpret_cast<const T*>(q), q_stride, reinterpret_cast<const T*>(pool), reinterpret_cast<T*>(out), out_stride, lse, b->tables, b->table_stride,
-                      b->n_requests, b->n_q, b->n_kv, b->n_q / b->n_kv, b->pool_pages, scale * LOG2E, q_vec, plan};
+                      b->n_requests, b->n_q, b->n_kv, b->n_q / b->n_kv, b->pool_pages, scale * LOG2E, q_vec, out_vec, plan};
   return op_result(b->d == 128 ? launch_attn<T, 128>(s, c) : launch_attn<T, 64>(s, c));
 }
 

@@ -62,7 +62,7 @@ def test_attention_refuses(sts):
                 workspace=5 * A, workspace_bytes=size)
     batch = [dict(dtype=0), dict(dtype=3), dict(n_requests=-1), dict(n_requests=4097), dict(n_groups=-1), dict(n_groups=7), dict(n_q=7), dict(n_q=0), dict(n_kv=0), dict(n_q=66),
              dict(d=32), dict(d=96), dict(pool_pages=-1), dict(max_pages=-1), dict(table_stride=4), dict(tables=None), dict(lens=None), dict(group_starts=None), dict(shared_lens=None),
-             dict(workspace=None), dict(workspace=5 * A + 16), dict(workspace_bytes=size - 1), dict(n_kv=1024, n_q=1024)]
+             dict(workspace=None), dict(workspace=5 * A + 16), dict(workspace_bytes=size - 1), dict(n_kv=257, n_q=257)]
     layer = lambda b, q=A, qs=512, pool=A, out=A, os_=512, scale=0.0: sts.op_attn_shared(b, q, qs, pool, out, os_, None, scale)  # noqa: E731
     for change in batch:
         refused(sts, sts.op_attn_shared_plan, sts.AttnBatch, good, **change)
