@@ -538,7 +538,6 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const AttnCall<T
 
 // ---- wide items, a workgroup: every wave takes 32 rows over all the pages. Tiles of four pages go global -> LDS, two stages deep, a page
 // a wave; products, order of the tokens and softmax as in attn_prefill.hip, whose queries lie in a row where these come from any request.
-constexpr float AS_RESCALE_LOG2 = 8.f;           // the reference maximum moves when a score outgrows it by 2^8
 
 template <typename T, int D>
 __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>& c, const Item& it, int kvh) {
@@ -653,11 +652,13 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>&
 #pragma unroll
       for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[kb][r]);
     mx = half_swap_max_f(mx);
-    const bool grow = (mx - m_ref) * c.scale_log2e > AS_RESCALE_LOG2;          // false when both are -inf (NaN)
-    if (__any(grow)) {                                                         // wave-uniform
-      const float m_upd = grow ? mx : m_ref;
-      const float corr = (m_upd == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_upd) * c.scale_log2e);
-      m_ref = m_upd;
+    // The reference follows every new maximum: the largest probability is then 1, which the type holds exactly. Moving it only when a score
+    // outgrew it by 2^8 took 51 instead of 55 us for 256 requests on 8192 tokens, but left the outputs at 1.37 times the distance from 64 bits
+    // that rounding them once has, against 1.08.
+    if (__any(mx > m_ref)) {                                                   // wave-uniform
+      const float m_new = fmaxf(m_ref, mx);
+      const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c.scale_log2e);
+      m_ref = m_new;
       l_run *= corr;
 #pragma unroll
       for (int b = 0; b < DB; b++)
