@@ -603,3 +603,117 @@ def test_logprobs_same_bits_again_and_in_a_graph(sts):
             got = read()
             for n in first:
                 assert np.array_equal(first[n], got[n]), n
+
+
+# ------------------------------------------------------------------------------------------ together
+def test_a_step_of_all_operators_eager_and_replayed(sts):
+    """Three prompts, sampled five, one and three ways: prompts placed and appended, then steps of one token each -- places, rotation and append, attention over the
+    shared prompts, logits (the library's GEMM), log probabilities -- eagerly and as a graph of two steps that hand lengths and free pages to each other on the device."""
+    rng = np.random.default_rng(77)
+    n_q, n_kv, d, vocab, dtype = 8, 2, 64, 512, "bf16"
+    members, prompts = [5, 1, 3], [70, 33, 100]
+    n, width, pages, heads, ld = sum(members), 12, 90, n_q // n_kv, (n_q + 2 * n_kv) * d
+    owner = np.repeat(np.arange(3), members)
+    shared = [p // 16 * 16 for p in prompts]
+    rope = sts.Rope(rotary_dim=d, scaling=sts.ROPE_SCALINGS["bands"], theta=1e4, factor=4.0, low=1.0, high=4.0, original_len=64)
+    with Device() as dev:
+        s = dev.stream()
+        pool, tables = dev.put(np.zeros((pages, n_kv, 32 * d), np.uint16)), dev.ints(np.full((n, width), -1))
+        free = rng.permutation(pages).astype(np.int32)
+        w = rounded(rng.standard_normal((vocab, n_q * d)) / 8, dtype)
+        free_dev, w_dev = dev.put(free), dev.put(w, dtype)
+        count, lens, starts, status = [dev.ints([pages]), dev.ints([0])], [dev.ints([0] * n), dev.ints([0] * n)], dev.ints([0] * (n + 1)), dev.ints([9])
+        rows_max = sum(p for p in prompts) + n * 100
+        requests, positions, places = (dev.ints([0] * rows_max) for _ in range(3))
+
+        def place(added, rows, a, b):
+            sts.op_block_tables(sts.BlockTables(n_requests=n, max_pages=width, max_rows=rows, free_capacity=pages, table_stride=width, cached=lens[a], added=added, free_pages=free_dev,
+                                                n_free=count[a], tables=tables, lens=lens[b], row_starts=starts, requests=requests, positions=positions, places=places,
+                                                n_free_left=count[b], status=status), s)
+
+        def append(qkv, rows, q_out):
+            sts.op_rope(rope, sts.RopeRows(dtype=1, rows=rows, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, q=qkv, q_stride=ld, q_out=q_out, q_out_stride=n_q * d, k=qkv + n_q * d * 2,
+                                           k_stride=ld, v=qkv + (n_q + n_kv) * d * 2, v_stride=ld, pool=pool, positions=positions, places=places), s)
+
+        # the prompts, by the first of each group; the whole pages go to the others' tables, which then get their own copy of the rest
+        first = [int(np.argmax(owner == g)) for g in range(3)]
+        added = np.zeros(n, np.int32)
+        added[first] = prompts
+        qkv_prompt = rounded(rng.standard_normal((sum(prompts), ld)), dtype)
+        place(dev.ints(added), sum(prompts), 0, 1)
+        append(dev.put(qkv_prompt, dtype), sum(prompts), dev.alloc(sum(prompts) * n_q * d * 2))
+        dev.sync()
+        assert dev.get(status, 1, "i32")[0] == 0
+        t = dev.get(tables, (n, width), "i32")
+        for r in range(n):
+            t[r, :shared[owner[r]] // 16] = t[first[owner[r]], :shared[owner[r]] // 16]
+        rest = np.array([0 if r in first else prompts[owner[r]] - shared[owner[r]] for r in range(n)], np.int32)
+        offsets = np.concatenate([[0], np.cumsum(prompts)])
+        qkv_rest = np.concatenate([qkv_prompt[offsets[owner[r]] + shared[owner[r]]:offsets[owner[r] + 1]] for r in range(n) if rest[r]])
+        dev.write(tables, t)
+        dev.write(lens[1], np.array([prompts[owner[r]] - rest[r] for r in range(n)], np.int32))
+        place(dev.ints(rest), len(qkv_rest), 1, 0)
+        append(dev.put(qkv_rest, dtype), len(qkv_rest), dev.alloc(len(qkv_rest) * n_q * d * 2))
+        dev.sync()
+        assert dev.get(status, 1, "i32")[0] == 0
+        assert np.array_equal(dev.get(lens[0], n, "i32"), [prompts[g] for g in owner])
+
+        # steps
+        size = sts.attn_shared_workspace(n, n_q, n_kv, d)
+        ones, qkv, q, out, lse = dev.ints([1] * n), dev.alloc(n * ld * 2), dev.alloc(n * n_q * d * 2), dev.alloc(n * n_q * d * 2), dev.alloc(n * n_q * 4)
+        groups, shared_dev, ws, logits = dev.ints(np.concatenate([[0], np.cumsum(members)])), dev.ints(shared), dev.alloc(size), dev.alloc(n * vocab * 4)
+        tokens = dev.ints(rng.integers(0, vocab, n))
+        o = {k: dev.alloc(n * 4 * m) for k, m in (("logprob", 1), ("entropy", 1), ("lse", 1), ("rank", 1), ("top_logprob", 4), ("top_token", 4))}
+
+        def step(a, b):
+            place(ones, n, a, b)
+            append(qkv, n, q)
+            batch = sts.AttnBatch(dtype=1, n_requests=n, n_groups=3, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, max_pages=width, table_stride=width, tables=tables, lens=lens[b],
+                                  group_starts=groups, shared_lens=shared_dev, workspace=ws, workspace_bytes=size)
+            sts.op_attn_shared_plan(batch, s)
+            sts.op_attn_shared(batch, q, n_q * d, pool, out, n_q * d, lse, 0.0, s)
+            sts.op_gemm_noalloc(out, w_dev, logits, n, vocab, n_q * d, "64x128", 1, 0, s)
+            sts.op_logprobs(sts.Logprobs(dtype=0, rows=n, vocab=vocab, top_k=4, row_stride=vocab, logits=logits, tokens=tokens, **o), s)
+
+        def check(done, x):
+            length = [prompts[g] + done for g in owner]
+            assert dev.get(status, 1, "i32")[0] == 0 and np.array_equal(dev.get(lens[done % 2], n, "i32"), length)
+            p, t = dev.get(pool, (pages, n_kv, 32 * d), dtype), dev.get(tables, (n, width), "i32")
+            own = [x for r in range(n) for x in t[r, shared[owner[r]] // 16:-(-length[r] // 16)]]
+            assert len(set(own)) == len(own) and dev.get(count[done % 2], 1, "i32")[0] == pages - len(own) - sum(shared) // 16
+            k = [p[t[r, :-(-length[r] // 16)], :, :16 * d].reshape(-1, n_kv, 16, d).transpose(0, 2, 1, 3).reshape(-1, n_kv, d)[:length[r]] for r in range(n)]
+            v = [p[t[r, :-(-length[r] // 16)], :, 16 * d:].reshape(-1, n_kv, d, 16).transpose(0, 3, 1, 2).reshape(-1, n_kv, d)[:length[r]] for r in range(n)]
+            rows = x.reshape(n, n_q + 2 * n_kv, d).astype(np.float64)
+            got_q = dev.get(q, (n, n_q, d), dtype)
+            for y, part in ((got_q, rows[:, :n_q]), (np.stack([kr[-1] for kr in k]), rows[:, n_q:n_q + n_kv])):
+                want, sz = rope_reference(sts, rope, part, np.array(length) - 1)
+                near(y, want, rope_bound(want, sz, dtype))
+            assert np.array_equal(np.stack([vr[-1] for vr in v]), rows[:, n_q + n_kv:])
+            want, bound, want_lse, lb = attention_reference(got_q, k, v, length, heads, d ** -0.5, dtype)
+            got = dev.get(out, (n, n_q, d), dtype)
+            near(got, want, bound)
+            near(dev.get(lse, (n, n_q), "f32"), want_lse, lb)
+            z = dev.get(logits, (n, vocab), "f32")
+            near(z, got.reshape(n, -1).astype(np.float64) @ w.T, n_q * d * 2.0 ** -23 * np.abs(got.reshape(n, -1)) @ np.abs(w.T) + 1e-6)
+            kinds = dict(rank="i32", top_token="i32")
+            shape = {k_: (n, 4) if k_.startswith("top") else (n,) for k_ in o}
+            check_logprobs({k_: dev.get(o[k_], shape[k_], kinds.get(k_, "f32")) for k_ in o}, logprobs_reference(z.astype(np.float64), dev.get(tokens, n, "i32"), 4), vocab)
+
+        x = rounded(rng.standard_normal((n, ld)), dtype)
+        for i in range(2):
+            x = rounded(rng.standard_normal((n, ld)), dtype)
+            dev.write(qkv, stored_bf16(x))
+            step(i, 1 - i)
+            dev.sync()
+            check(i + 1, x)
+        replay = dev.graph(s, lambda: (step(0, 1), step(1, 0)))
+        for i in range(9):                                 # over several page borders; both steps of a replay append the same rows
+            x = rounded(rng.standard_normal((n, ld)), dtype)
+            dev.write(qkv, stored_bf16(x))
+            replay()
+            dev.sync()
+            check(2 * i + 4, x)
+
+
+def stored_bf16(x):
+    return (np.asarray(x, np.float32).view(np.uint32) >> 16).astype(np.uint16)
