@@ -330,7 +330,7 @@ enum { STS_F32 = 0, STS_BF16 = 1, STS_F16 = 2 };
  * requests' order and are entered into its table. Rows are the added tokens, request after request. */
 typedef struct {
   int32_t n_requests, max_pages;        /* entries of a table row that may be used */
-  int32_t max_rows;                     /* length of requests, positions and places */
+  int32_t max_rows;                     /* length of requests, positions and places, up to 2^30 */
   int32_t free_capacity;                /* length of free_pages */
   int64_t table_stride;                 /* entries from a table row to the next, >= max_pages */
   const int32_t *cached, *added;        /* [n_requests] */

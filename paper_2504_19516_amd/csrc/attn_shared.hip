@@ -634,11 +634,9 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>&
       }
       __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
     }
-    __builtin_amdgcn_sched_barrier(0);
     V vf[2][DB];                                           // first V^T operands: in flight during the softmax arithmetic
 #pragma unroll
     for (int b = 0; b < DB; b++) vf[0][b] = *reinterpret_cast<const V*>(st + v_lane + b * 1024);
-    __builtin_amdgcn_sched_barrier(0);
     if constexpr (!decltype(whole)::value) {
 #pragma unroll
       for (int kb = 0; kb < 2; kb++)
@@ -676,7 +674,6 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>&
         rs += p;
       }
     l_run += rs;                                                               // this half's keys; halves are added at the end
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int g = 0; g < 4; g++) {
       const int a = g & 1, b2 = a ^ 1;

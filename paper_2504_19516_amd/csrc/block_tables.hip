@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(BT_THREADS) block_tables_kernel(sts_block_tabl
 using namespace sts;
 
 extern "C" int sts_op_block_tables(const sts_block_tables* a, void* stream) {
-  if (!a || a->n_requests < 0 || a->n_requests > OP_MAX_REQUESTS || a->max_pages < 0 || a->max_rows < 0 || a->free_capacity < 0 || a->table_stride < a->max_pages) return STS_EINVAL;
+  if (!a || a->n_requests < 0 || a->n_requests > OP_MAX_REQUESTS || a->max_pages < 0 || a->max_rows < 0 || a->max_rows > (1 << 30) || a->free_capacity < 0 || a->table_stride < a->max_pages) return STS_EINVAL;
   if (!a->n_free || !a->n_free_left || !a->status || !a->row_starts) return STS_EINVAL;
   if (a->n_requests > 0 && (!a->cached || !a->added || !a->lens || (a->max_pages > 0 && !a->tables))) return STS_EINVAL;
   if (a->max_rows > 0 && (!a->requests || !a->positions || !a->places)) return STS_EINVAL;

@@ -147,7 +147,9 @@ def lib():
         _lib.sts_kernel_name.restype = C.c_char_p
         _lib.sts_op_logprobs_workspace.restype = C.c_int64
         _lib.sts_attn_shared_workspace.restype = C.c_int64
-        # called once a layer: converting by declared types takes a third of the time that wrapping each argument does
+        # called once a step or layer: declared types are converted in a third of the time that wrapping each argument takes
+        _lib.sts_op_block_tables.argtypes = _lib.sts_op_attn_shared_plan.argtypes = _lib.sts_op_logprobs.argtypes = [C.c_void_p, C.c_void_p]
+        _lib.sts_op_rope.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
         _lib.sts_op_attn_shared.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c_void_p]
     return _lib
 
@@ -474,7 +476,7 @@ def op_attn_decode(q, k, v, ctx, chunk_pages):
 # hipStream_t value, None or 0 = the null stream) and not waited for. A process that also uses torch imports torch first: the library then
 # shares its HIP runtime, and with it streams and graphs.
 def op_block_tables(a: BlockTables, stream=None):
-    _ck(lib().sts_op_block_tables(C.byref(a), C.c_void_p(stream)), "sts_op_block_tables")
+    _ck(lib().sts_op_block_tables(C.byref(a), stream), "sts_op_block_tables")
 
 
 def rope_frequencies(rope: Rope):
@@ -485,7 +487,7 @@ def rope_frequencies(rope: Rope):
 
 
 def op_rope(rope: Rope, a: RopeRows, stream=None):
-    _ck(lib().sts_op_rope(C.byref(rope), C.byref(a), C.c_void_p(stream)), "sts_op_rope")
+    _ck(lib().sts_op_rope(C.byref(rope), C.byref(a), stream), "sts_op_rope")
 
 
 def attn_shared_workspace(n_requests, n_q, n_kv, d):
@@ -494,7 +496,7 @@ def attn_shared_workspace(n_requests, n_q, n_kv, d):
 
 
 def op_attn_shared_plan(b: AttnBatch, stream=None):
-    _ck(lib().sts_op_attn_shared_plan(C.byref(b), C.c_void_p(stream)), "sts_op_attn_shared_plan")
+    _ck(lib().sts_op_attn_shared_plan(C.byref(b), stream), "sts_op_attn_shared_plan")
 
 
 def op_attn_shared(b: AttnBatch, q, q_stride, pool, out, out_stride, lse=None, scale=0.0, stream=None):
@@ -507,7 +509,7 @@ def op_logprobs_workspace(dtype, rows, vocab, top_k):
 
 
 def op_logprobs(a: Logprobs, stream=None):
-    _ck(lib().sts_op_logprobs(C.byref(a), C.c_void_p(stream)), "sts_op_logprobs")
+    _ck(lib().sts_op_logprobs(C.byref(a), stream), "sts_op_logprobs")
 
 
 def release_streams():

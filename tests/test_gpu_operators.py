@@ -324,6 +324,9 @@ CASES = [
     (8, 2, 64, [(150, 700), (3, 32)], [6]),
     (4, 2, 128, [(1, 0)], [5000]),
     (8, 1, 64, [(2, 20000)], [3000, 1]),
+    (6, 3, 64, [(25, 33), (20, 100)], [1, 15, 40]),
+    (256, 256, 64, [(3, 32)], [5, 20]),
+    (2, 2, 64, [(1000, 16), (24, 0)], [1, 2, 3, 20]),
 ]
 
 
@@ -461,6 +464,58 @@ def test_shared_attention_same_bits_again_and_in_a_graph(sts):
             replay()
             dev.sync()
             assert np.array_equal(dev.get(out, first.shape, "bf16"), first) and np.array_equal(dev.get(lse, lse0.shape, "f32"), lse0)
+
+
+def test_shared_attention_of_two_streams_at_once(sts):
+    """Workspaces of their own: calls under way together do not see each other."""
+    rng = np.random.default_rng(21)
+    cases = [small_case(rng, "bf16", [600 + 5 * i for i in range(50)], [(30, 560), (20, 100)]), small_case(rng, "bf16", [90 + 11 * i for i in range(70)], [(70, 80)])]
+    with Device() as dev:
+        runs, want = [], []
+        for q, k, v, tables, pages, lens, groups in cases:
+            pool, s = pool_of(k, v, tables, lens, pages, "bf16"), dev.stream()
+            out, lse, call, at = run_attention(sts, dev, "bf16", q, pool, tables, lens, groups, 4, stream=s)
+            runs.append((call, at, out.shape))
+            want.append(out)
+        for _ in range(20):
+            for call, _, _ in runs:
+                call()
+        dev.sync()
+        for (_, (out, _), shape), w in zip(runs, want):
+            assert np.array_equal(dev.get(out, shape, "bf16"), w)
+
+
+def test_append_and_attention_behind_32_bits(sts):
+    """A pool of more than 2^31 elements and 2^32 bytes: its last pages are written and read."""
+    rng = np.random.default_rng(22)
+    n_q, n_kv, d, pages, n, ctx = 16, 16, 128, 34000, 3, 40
+    rope = sts.Rope(rotary_dim=d, theta=1e4)
+    tables = np.array([[pages - 1, 5, pages - 2], [pages - 3, pages - 4, 0], [1, pages - 5, pages - 6]], np.int32)
+    qkv = rounded(rng.standard_normal((n * ctx, 3 * n_q * d)), "bf16")
+    positions = np.tile(np.arange(ctx), n)
+    places = np.array([tables[r, t // 16] * 16 + t % 16 for r in range(n) for t in range(ctx)], np.int32)
+    with Device() as dev:
+        assert pages * n_kv * 32 * d > 2 ** 31
+        pool, base, ld = dev.alloc(pages * n_kv * 32 * d * 2), dev.put(qkv, "bf16"), 3 * n_q * d
+        q, out, lse, size = dev.alloc(n * ctx * n_q * d * 2), dev.alloc(n * n_q * d * 2), dev.alloc(n * n_q * 4), sts.attn_shared_workspace(n, n_q, n_kv, d)
+        sts.op_rope(rope, sts.RopeRows(dtype=1, rows=n * ctx, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, q=base, q_stride=ld, q_out=q, q_out_stride=n_q * d, k=base + n_q * d * 2, k_stride=ld,
+                                       v=base + 2 * n_q * d * 2, v_stride=ld, pool=pool, positions=dev.ints(positions), places=dev.put(places)))
+        batch = sts.AttnBatch(dtype=1, n_requests=n, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, max_pages=3, table_stride=3, tables=dev.ints(tables), lens=dev.ints([ctx] * n),
+                              workspace=dev.alloc(size), workspace_bytes=size)
+        sts.op_attn_shared_plan(batch)
+        sts.op_attn_shared(batch, q + (ctx - 1) * n_q * d * 2, ctx * n_q * d, pool, out, n_q * d, lse)
+        dev.sync()
+        got_q, got = dev.get(q, (n, ctx, n_q, d), "bf16")[:, -1], dev.get(out, (n, n_q, d), "bf16")
+        page = np.stack([[dev.get(pool + int(p) * n_kv * 32 * d * 2, (n_kv, 32 * d), "bf16") for p in row] for row in tables])
+    x = qkv.reshape(n, ctx, 3 * n_q, d)
+    k = page[..., :16 * d].reshape(n, 3, n_kv, 16, d).transpose(0, 1, 3, 2, 4).reshape(n, 48, n_kv, d)[:, :ctx]
+    v = page[..., 16 * d:].reshape(n, 3, n_kv, d, 16).transpose(0, 1, 4, 2, 3).reshape(n, 48, n_kv, d)[:, :ctx]
+    assert np.array_equal(v, x[:, :, 2 * n_q:])
+    for r in range(n):
+        want, size = rope_reference(sts, rope, x[r, :, n_q:2 * n_q].astype(np.float64), positions[:ctx])
+        near(k[r], want, rope_bound(want, size, "bf16"))
+    want, bound, _, _ = attention_reference(got_q, k, v, [ctx] * n, 1, d ** -0.5, "bf16")
+    near(got, want, bound)
 
 
 # ------------------------------------------------------------------------------------------ log probabilities

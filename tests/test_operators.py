@@ -29,7 +29,7 @@ A = 1 << 20            # an address
 def test_block_tables_refuses(sts):
     good = dict(n_requests=4, max_pages=8, max_rows=10, free_capacity=5, table_stride=8, cached=A, added=2 * A, free_pages=3 * A, n_free=4 * A, tables=5 * A, lens=6 * A,
                 row_starts=7 * A, requests=8 * A, positions=9 * A, places=10 * A, n_free_left=11 * A, status=12 * A)
-    for change in [dict(n_requests=-1), dict(n_requests=4097), dict(max_pages=-1), dict(max_rows=-1), dict(free_capacity=-1), dict(table_stride=7), dict(n_free_left=4 * A),
+    for change in [dict(n_requests=-1), dict(n_requests=4097), dict(max_pages=-1), dict(max_rows=-1), dict(max_rows=(1 << 30) + 1), dict(free_capacity=-1), dict(table_stride=7), dict(n_free_left=4 * A),
                    dict(lens=A), dict(lens=2 * A)] + [{k: None} for k in good if k not in ("n_requests", "max_pages", "max_rows", "free_capacity", "table_stride")]:
         refused(sts, sts.op_block_tables, sts.BlockTables, good, **change)
     with pytest.raises(sts.StsError):
@@ -61,7 +61,7 @@ def test_attention_refuses(sts):
     good = dict(dtype=1, n_requests=6, n_groups=2, n_q=8, n_kv=2, d=64, pool_pages=9, max_pages=5, table_stride=5, tables=A, lens=2 * A, group_starts=3 * A, shared_lens=4 * A,
                 workspace=5 * A, workspace_bytes=size)
     batch = [dict(dtype=0), dict(dtype=3), dict(n_requests=-1), dict(n_requests=4097), dict(n_groups=-1), dict(n_groups=7), dict(n_q=7), dict(n_q=0), dict(n_kv=0), dict(n_q=66),
-             dict(d=32), dict(d=96), dict(pool_pages=-1), dict(max_pages=-1), dict(table_stride=4), dict(tables=None), dict(lens=None), dict(group_starts=None), dict(shared_lens=None),
+             dict(d=32), dict(d=96), dict(pool_pages=-1), dict(max_pages=-1), dict(max_pages=1 << 26, table_stride=1 << 26), dict(table_stride=4), dict(tables=None), dict(lens=None), dict(group_starts=None), dict(shared_lens=None),
              dict(workspace=None), dict(workspace=5 * A + 16), dict(workspace_bytes=size - 1), dict(n_kv=257, n_q=257)]
     layer = lambda b, q=A, qs=512, pool=A, out=A, os_=512, scale=0.0: sts.op_attn_shared(b, q, qs, pool, out, os_, None, scale)  # noqa: E731
     for change in batch:
