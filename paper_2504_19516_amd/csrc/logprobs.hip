@@ -34,10 +34,10 @@ constexpr double LN2 = 0.69314718055994530942;
 // Sums of a part of a row; above: elements that stand before the token.
 struct RowSums { float m, z, s; int above; };
 __device__ __forceinline__ bool beyond(float m) { return !(fabsf(m) < 0x1p100f) && m != -INFINITY; }
-// (a - b) log2(e), as the sums over y refer to it; b >= a
+// (a - b) log2(e), as the sums over y refer to it; b >= a. Bounded: 2^ of it is 0 anyway, and 0 times it has to be 0.
 __device__ __forceinline__ float log2_diff(float a, float b) {
 #pragma clang fp contract(off)
-  return beyond(a) || beyond(b) ? (a - b) * LOG2E : a * LOG2E - b * LOG2E;
+  return fmaxf(beyond(a) || beyond(b) ? (a - b) * LOG2E : a * LOG2E - b * LOG2E, -0x1p100f);
 }
 
 // An element's place in the order, larger = earlier: value (-0 as 0, NaN as -inf), then the lower index. 0: no element.
@@ -168,20 +168,21 @@ __device__ __forceinline__ void lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// A wave's 64 best of every fourth load of a part, in descending order, with a buffer of its own of 64 + 64 E keys.
+// A wave's 64 best of every fourth load of a part's vectors, and of one more key a lane (0: none), in descending order, with a buffer of its own
+// of 64 + 64 E keys.
 template <typename T, typename L>
-__device__ unsigned long long second_pass(unsigned long long* buffer, int n_vecs, int base, int i0, int i1, int k, L load) {
+__device__ unsigned long long second_pass(unsigned long long* buffer, int n_vecs, int a0, int k, unsigned long long more, L load) {
   constexpr int E = 16 / sizeof(T);
   const int lane = threadIdx.x & 63;
   unsigned long long best = 0, least = 0;        // the list, and its k-th key: what is not above it is not among the k best
   int count = 0;
-  for (int q = (threadIdx.x & ~63) + lane; q - lane < n_vecs; q += LP_THREADS) {
-    const int at = base + q * E;
-    const vec16<T> v = load(at);
+  merge_64(best, more);
+  for (int q = threadIdx.x; q - lane < n_vecs; q += LP_THREADS) {
+    const vec16<T> v = load(q);
 #pragma unroll
     for (int e = 0; e < E; e++) {
-      const unsigned long long key = order_key((float)v[e], at + e);
-      const bool pass = key > least && at + e >= i0 && at + e < i1;
+      const unsigned long long key = order_key((float)v[e], a0 + q * E + e);
+      const bool pass = key > least && q < n_vecs;
       const unsigned long long mask = __ballot(pass);
       if (pass) buffer[count + __popcll(mask & ((1ull << lane) - 1))] = key;
       count += __popcll(mask);
@@ -217,25 +218,26 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
   const int row = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T* x = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
   const int i0 = part * c.width, i1 = min(a.vocab, i0 + c.width), k = TOP ? a.top_k : 0;
-  // vectors lie at 16-byte addresses: the first may begin before the part
-  const int base = i0 - (int)(reinterpret_cast<uintptr_t>(x + i0) % 16 / sizeof(T));
-  const int n_vecs = (i1 - base + E - 1) / E;
-  auto load = [&](int at) {                      // elements at .. at + E - 1, -inf outside the part
+  // vectors at 16-byte addresses, from element a0 to a1; the fewer than 2 E elements around them go to the first wave's lanes
+  const int a0 = min(i1, i0 + (int)(-reinterpret_cast<uintptr_t>(x + i0) % 16 / sizeof(T))), n_vecs = (i1 - a0) / E, a1 = a0 + n_vecs * E;
+  auto load = [&](int q) {
     V v;
-    if (at >= i0 && at + E <= i1) v = *reinterpret_cast<const V*>(x + at);
+    if (q < n_vecs) v = *reinterpret_cast<const V*>(x + a0 + q * E);
     else {
 #pragma unroll
-      for (int e = 0; e < E; e++) v[e] = at + e >= i0 && at + e < i1 ? x[at + e] : (T)-INFINITY;
+      for (int e = 0; e < E; e++) v[e] = (T)-INFINITY;
     }
     return v;
   };
-
   V raw[VECS];
   auto fetch = [&](int b) {
 #pragma unroll
-    for (int j = 0; j < VECS; j++) raw[j] = load(base + (b + j * 64 + lane) * E);
+    for (int j = 0; j < VECS; j++) raw[j] = load(b + j * 64 + lane);
   };
   fetch(wave * BATCH);
+  const bool edge = tid < (a0 - i0) + (i1 - a1);
+  const int edge_at = tid < a0 - i0 ? i0 + tid : a1 + tid - (a0 - i0);
+  const float edge_x = edge ? (float)x[edge_at] : -INFINITY;
   const int tok = a.tokens ? a.tokens[row] : -1;
   const float xt = tok >= 0 && tok < a.vocab ? (float)x[tok] : NAN;
   // an element stands before the token if it is above xt -- or, at a lower index, above `loose`, the next value below. A token of -inf:
@@ -244,8 +246,29 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
   if (TOP && tid == 0) candidates = 0;
 
   RowSums t{-INFINITY, 0.f, 0.f, 0};
-  int above = 0;                                 // wave-uniform
-  float lane_max = -INFINITY, slot_max = -INFINITY;
+  auto raise = [&](float mx) {                   // the lane's maximum
+    if (mx > t.m) {
+      const float shift = log2_diff(t.m, mx), f = __builtin_amdgcn_exp2f(shift);
+      t.s = t.z == 0.f ? 0.f : f * (t.s + shift * t.z);
+      t.z *= f;
+      t.m = mx;
+    }
+  };
+  float scale, ref;
+  auto refer = [&] {
+    const bool far = beyond(t.m);                // there other values are 2^77 and more away: x - m is as good as any multiple of it
+    scale = far ? 1.f : LOG2E; ref = t.m == -INFINITY ? 0.f : t.m * scale;
+  };
+  auto add = [&](float x1) {
+    const float y = fmaf(x1, scale, -ref), p = __builtin_amdgcn_exp2f(y);
+    t.z += p;
+    t.s = fmaf(p, fmaxf(y, -200.f), t.s);        // p is 0 there; -inf * 0 is not
+  };
+  raise(edge_x);
+  refer();
+  add(edge_x);
+  int above = __popcll(__ballot(edge && edge_x > (edge_at < tok ? loose : xt)));         // wave-uniform
+  float lane_max = edge_x, slot_max = -INFINITY;
   // batches of a wave, and of a group
   const int batches = max(0, (n_vecs - wave * BATCH + LP_WAVES * BATCH - 1) / (LP_WAVES * BATCH)), span = (batches + LP_SLOTS - 1) / LP_SLOTS;
   int slot = 0, in_slot = 0;
@@ -259,23 +282,15 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
         mx = fmaxf(mx, v[j][e]);
       }
     if (i + 1 < batches) fetch(b + LP_WAVES * BATCH);
-    if (mx > t.m) {
-      const float shift = log2_diff(t.m, mx), f = __builtin_amdgcn_exp2f(shift);
-      t.s = t.z == 0.f ? 0.f : f * (t.s + shift * t.z);
-      t.z *= f;
-      t.m = mx;
-    }
-    const bool far = beyond(t.m);                // there other values are 2^77 and more away: x - m is as good as any multiple of it
-    const float scale = far ? 1.f : LOG2E, ref = t.m == -INFINITY ? 0.f : t.m * scale;
+    raise(mx);
+    refer();
 #pragma unroll
     for (int j = 0; j < VECS; j++) {
       // a vector lies before the token or behind it; the one around it counts as behind (mended below)
-      const float limit = base + (b + j * 64 + lane + 1) * E <= tok ? loose : xt;
+      const float limit = a0 + (b + j * 64 + lane + 1) * E <= tok ? loose : xt;
 #pragma unroll
       for (int e = 0; e < E; e++) {
-        const float y = fmaf(v[j][e], scale, -ref), p = __builtin_amdgcn_exp2f(y);
-        t.z += p;
-        t.s = fmaf(p, fmaxf(y, -200.f), t.s);    // p is 0 there; -inf * 0 is not
+        add(v[j][e]);
         above += __popcll(__ballot(v[j][e] > limit));
       }
     }
@@ -290,9 +305,9 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
     }
   }
   // the elements before the token in its own vector
-  if (wave == 0 && tok >= i0 && tok < i1) {
-    const int at = base + (tok - base) / E * E + lane;
-    const float xe = at >= i0 && at < tok ? (float)x[at] : NAN;
+  if (wave == 0 && tok >= a0 && tok < a1) {
+    const int at = a0 + (tok - a0) / E * E + lane;
+    const float xe = at < tok ? (float)x[at] : NAN;
     above += __popcll(__ballot(xe > loose)) - __popcll(__ballot(xe > xt));
   }
   // ---- the lanes' sums, the waves' sums and lists
@@ -323,8 +338,13 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
     const bool open = kth <= value_key(-INFINITY);
     float bound = open ? -INFINITY : below(key_value(kth));
     // Without a bound everything above -inf is a candidate, and the part's first 64 elements: among them are 32 of -inf, or more than k others
+    auto append = [&](float xe, int at) {
+      const int n = atomicAdd(&candidates, 1);
+      if (n < LP_BUFFER) first.buffer[n] = order_key(xe, at);
+    };
+    if (edge && (edge_x > bound || (open && edge_at < i0 + 64))) append(edge_x, edge_at);
     unsigned hits = 0;
-    for (int g = 0; g < slot; g++) hits |= (unsigned)(first.group_max[g][tid] > bound || (open && g == 0 && tid * E < 64 + E)) << g;
+    for (int g = 0; g < slot; g++) hits |= (unsigned)(first.group_max[g][tid] > bound || (open && g == 0 && tid * E < 64)) << g;
     while (hits) {                               // lanes apart: their groups
       const int g = __builtin_ctz(hits);
       hits &= hits - 1;
@@ -332,20 +352,19 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
         const int b = wave * BATCH + i * LP_WAVES * BATCH;
         V again[VECS];
 #pragma unroll
-        for (int j = 0; j < VECS; j++) again[j] = load(base + (b + j * 64 + lane) * E);
+        for (int j = 0; j < VECS; j++) again[j] = load(b + j * 64 + lane);
         unsigned found = 0;                      // bit j E + e
 #pragma unroll
         for (int j = 0; j < VECS; j++)
 #pragma unroll
-          for (int e = 0; e < E; e++) found |= (unsigned)((float)again[j][e] > bound || (open && b + j * 64 + lane < 64 + E)) << (j * E + e);
+          for (int e = 0; e < E; e++) found |= (unsigned)((float)again[j][e] > bound) << (j * E + e);
+        if (open && i == 0 && tid * E < 64) found |= (1u << E) - 1;             // the first load's
         while (found) {                          // few: their values again, from L1
-          const int q = __builtin_ctz(found), at = base + (b + q / E * 64 + lane) * E + q % E;
+          const int q = b + __builtin_ctz(found) / E * 64 + lane, at = a0 + q * E + __builtin_ctz(found) % E;
           found &= found - 1;
-          if (at < i0 || at >= i1) continue;
+          if (q >= n_vecs) continue;
           const float xe = (float)x[at];
-          if (!(xe > bound) && at >= i0 + 64) continue;
-          const int n = atomicAdd(&candidates, 1);
-          if (n < LP_BUFFER) first.buffer[n] = order_key(xe, at);
+          if (xe > bound || at < i0 + 64) append(xe, at);
         }
       }
     }
@@ -356,7 +375,7 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
       for (int i = 0; i < n; i += 64) merge_64(best, i + lane < n ? first.buffer[i + lane] : 0);
     } else {
       __syncthreads();                           // the second pass takes the scratch over
-      best = second_pass<T>(reinterpret_cast<Scratch*>(scratch)->second[wave], n_vecs, base, i0, i1, k, load);
+      best = second_pass<T>(reinterpret_cast<Scratch*>(scratch)->second[wave], n_vecs, a0, k, edge ? order_key(edge_x, edge_at) : 0, load);
       if (lane < LP_MAX_K) lists[wave][lane] = best;
       __syncthreads();
       if (wave != 0) return;

@@ -607,6 +607,9 @@ def masks(rng, vocab, dtype):
     yield "one token left, another given", one, vocab - 1
     yield "nothing left", np.full(vocab, -inf, np.float32), 3
     yield "all the lowest value", np.full(vocab, lowest, np.float32), 5
+    yield "the lowest value, then logits", np.where(np.arange(vocab) < vocab - vocab // 3, np.float32(lowest), x), vocab - 2
+    yield "logits, then the lowest value", np.where(np.arange(vocab) > vocab // 3, np.float32(lowest), x), 2
+    yield "-inf, then logits", np.where(np.arange(vocab) < vocab - vocab // 3, -inf, x), vocab - 2
     yield "lowest and -inf", np.where(half, -inf, np.float32(lowest)), int(np.flatnonzero(~half)[1])
     yield "all equal", np.full(vocab, 1.5, np.float32), vocab - 1
     yield "zeros of both signs", np.where(half, np.float32(0.0), np.float32(-0.0)), vocab // 3
