@@ -198,6 +198,14 @@ int sts_last_timing(sts_ctx* ctx, int64_t* prefill_ns, int64_t* decode_ns, int64
 /* Test hook: hidden state (residual stream) after the last call of a phase, fp32 [rows, hidden];
  * phase 0 = prefill batch rows, 1 = decode rows. */
 int sts_read_hidden(sts_ctx* ctx, int32_t phase, float* out, int32_t rows);
+/* Log probabilities, entropies, ranks and the top_k most likely tokens from the logits of a phase's last finished call, if that call computed
+ * any (a prefill's last slice that asked for logits: a row a sequence; a decode step that asked for logits or tokens: a row a request): the
+ * first `rows` of them, with a token each. sts_op_logprobs on logits that are still on the device; its description says what the outputs are
+ * where a row has nothing, NaN or infinities, and what a token out of range gives. Outputs [rows] and [rows, top_k] may each be NULL; tokens may be
+ * NULL if logprob and rank are. STS_EINVAL if the call left fewer rows, STS_ESTATE while a launch of the phase is outstanding or its
+ * partition is empty. */
+int sts_read_logprobs(sts_ctx* ctx, int32_t phase, const int32_t* tokens, int32_t rows, int32_t top_k, float* logprob, float* entropy, int32_t* rank,
+                      float* top_logprob, int32_t* top_token);
 
 /* ---- CU partition (Section 3.4). prefill_cus / decode_cus: CUs given to each phase, each a
  * multiple of 8 (every XCD must keep a CU of a partition) in [8, total], or 0 = phase
@@ -365,6 +373,10 @@ typedef struct {
 } sts_rope;
 /* Host only, no GPU state: f_i, rotary_dim / 2 of them. */
 int sts_rope_frequencies(const sts_rope* rope, double* out);
+/* The rotation of an engine's own steps from now on, instead of rope_theta's plain one: contexts that were cached before keep the angles they
+ * were cached with. rotary_dim = head_dim, not interleaved, magnitude 0 or 1 (STS_EINVAL otherwise); STS_ESTATE while a launch is
+ * outstanding or a layer-sliced prefill batch is in flight. */
+int sts_set_rope(sts_ctx* ctx, const sts_rope* rope);
 /* Rows of Q and K, heads behind each other; strides in elements from row to row. Q rows are turned into q_out, K rows into k_out
  * (may be NULL with a pool) and the pool, V rows into the pool. q_out = q and k_out = k, with equal strides, turn rows in place. */
 typedef struct {

@@ -78,6 +78,9 @@ struct Phase {
   int* h_tokens = nullptr; int* h_pos = nullptr; int* h_place = nullptr; int* h_bt = nullptr; int* h_rows = nullptr;
   PrefillSeq* h_pseq = nullptr; DecodeSeq* h_dseq = nullptr; AttnItem* h_items = nullptr; DecodeItem* h_ditems = nullptr;
   float* h_logits = nullptr; ArgBest* h_best = nullptr;
+  // the last call's logits (device or pinned memory), none: head_rows 0; what sts_read_logprobs keeps, made by its first call
+  const float* head_at = nullptr; int head_rows = 0;
+  unsigned char* h_lp = nullptr; unsigned char* lp_ws = nullptr;
   int rows = 0;                               // rows of the last call
   bool alone = false;                         // neither queued together with the other phase nor while a launched step of it was in flight (blocking calls of two threads do not see each other)
   // per-kernel timing
@@ -826,6 +829,7 @@ int decode_launch_checked(sts_ctx* c, const int32_t* seqs, const int32_t* in_tok
 
 int DecodeRun::begin() {
   Phase& ph = c->ph[1];
+  ph.head_rows = 0;
   const sts_model_desc& d = c->d;
   const int mp = c->p.max_pages_per_seq, pt = c->geo.page_tokens;
   ph.meta_used = 0;
@@ -914,9 +918,10 @@ int DecodeRun::end() {
     STSCK(run_head(c, ph, few.plan.kslice ? ph.X : nullptr, nullptr, ph.Xn, few.xn_scale, n, ph.part, ph.part_floats, few.nt, direct ? ph.h_logits : ph.logits));
     if (want_next) KL(ph, STS_K_SAMPLE, argmax_rows(st, ph.h_best, ph.logits, n, d.vocab, stored ? ph.h_logits : nullptr));
     if (want_logits && !stored) HIPCK(hipMemcpyAsync(ph.h_logits, ph.logits, bytes, hipMemcpyDeviceToHost, st));
+    ph.head_at = direct ? ph.h_logits : ph.logits;
   }
   HIPCK(hipEventRecord(ph.ev1, st));
-  ph.ran = true; ph.rows = n;
+  ph.ran = true; ph.rows = n; ph.head_rows = want_logits || want_next ? n : 0;
   return STS_OK;
 }
 
@@ -967,6 +972,7 @@ bool prefill_few_rows(sts_ctx* c, Phase& ph, int rows, const PrefillGemm (&tiles
 int prefill_launch_body(sts_ctx* c, int n_seqs, const int32_t* seqs, const int32_t* lens, const int32_t* tokens,
                         int lb, int le, bool want_logits, DecodeRun* beside) {
   Phase& ph = c->ph[0];
+  ph.head_rows = 0;
   const sts_model_desc& d = c->d;
   int rows = 0;
   for (int i = 0; i < n_seqs; i++) rows += lens[i];
@@ -1060,9 +1066,10 @@ int prefill_launch_body(sts_ctx* c, int n_seqs, const int32_t* seqs, const int32
     const bool direct = bytes <= stored_logits_bytes(ph, false);   // the head's last kernel stores to host memory
     STSCK(run_head(c, ph, ph.X, ph.d_rows, ph.Xlast_n, RowScale{nullptr, 0, 0.f}, n_seqs, ph.tail_ws, ph.tail_ws_bytes / sizeof(float), false, direct ? ph.h_logits : ph.logits));
     if (!direct) HIPCK(hipMemcpyAsync(ph.h_logits, ph.logits, bytes, hipMemcpyDeviceToHost, st));
+    ph.head_at = direct ? ph.h_logits : ph.logits;
   }
   HIPCK(hipEventRecord(ph.ev1, st));
-  ph.ran = true; ph.rows = rows;
+  ph.ran = true; ph.rows = rows; ph.head_rows = le == d.n_layers && want_logits ? n_seqs : 0;
   return STS_OK;
 }
 
@@ -1308,7 +1315,7 @@ extern "C" int sts_destroy(sts_ctx* c) {
     if (ph.ev0) (void)hipEventDestroy(ph.ev0);
     if (ph.ev1) (void)hipEventDestroy(ph.ev1);
     for (hipEvent_t e : ph.kev) (void)hipEventDestroy(e);
-    void* hosts[] = {ph.h_meta, ph.h_logits, ph.h_best};
+    void* hosts[] = {ph.h_meta, ph.h_logits, ph.h_best, ph.h_lp};
     for (void* p : hosts) if (p) (void)hipHostFree(p);
   }
   trace("destroy: device memory");
@@ -1637,6 +1644,46 @@ extern "C" int sts_last_timing(sts_ctx* c, int64_t* prefill_ns, int64_t* decode_
 extern "C" int sts_read_hidden(sts_ctx* c, int32_t phase, float* out, int32_t rows) {
   if (!c || phase < 0 || phase > 1 || !out || rows < 1 || rows > c->ph[phase].rows) return STS_EINVAL;
   HIPCK(hipMemcpy(out, c->ph[phase].X, (size_t)rows * c->d.hidden * sizeof(float), hipMemcpyDeviceToHost));
+  return STS_OK;
+}
+
+extern "C" int sts_read_logprobs(sts_ctx* c, int32_t phase, const int32_t* tokens, int32_t rows, int32_t top_k, float* logprob, float* entropy, int32_t* rank,
+                                 float* top_logprob, int32_t* top_token) {
+  if (!c || phase < 0 || phase > 1 || rows < 1 || top_k < 0 || top_k > 32 || top_k > c->d.vocab) return STS_EINVAL;
+  if ((!tokens && (logprob || rank)) || ((top_logprob || top_token) && top_k == 0)) return STS_EINVAL;
+  Phase& ph = c->ph[phase];
+  if ((phase == 0 ? c->pend_prefill : c->pend_decode) || !ph.stream) return STS_ESTATE;
+  if (rows > ph.head_rows) return STS_EINVAL;
+  // tokens and outputs in pinned memory, which the kernels read and write themselves: token, three figures a row, top_k pairs
+  const int32_t most = phase == 0 ? c->p.max_prefill_seqs : c->p.max_decode_batch;
+  int64_t ws_bytes = 0;
+  for (int32_t r = 1; r <= most; r++) ws_bytes = std::max(ws_bytes, sts_op_logprobs_workspace(STS_F32, r, c->d.vocab, std::min(32, c->d.vocab)));
+  if (!ph.h_lp) {
+    std::lock_guard<std::mutex> g(c->alloc_mu);              // the other phase's control thread may be here too
+    if (!ph.lp_ws) STSCK(dev_alloc(c, &ph.lp_ws, (size_t)ws_bytes));
+    STSCK(host_alloc(&ph.h_lp, (size_t)most * (4 + 64) * sizeof(int32_t)));
+  }
+  int32_t* tok = reinterpret_cast<int32_t*>(ph.h_lp);
+  float *lp = reinterpret_cast<float*>(tok + most), *ent = lp + most, *top_lp = ent + 2 * most;
+  int32_t *rk = reinterpret_cast<int32_t*>(ent + most), *top_tok = reinterpret_cast<int32_t*>(top_lp + (size_t)most * 32);
+  if (tokens) std::memcpy(tok, tokens, rows * sizeof(int32_t));
+  const sts_logprobs a{STS_F32, rows, c->d.vocab, top_k, c->d.vocab, ph.head_at, tokens ? tok : nullptr, logprob ? lp : nullptr, ent, nullptr, rank ? rk : nullptr,
+                       top_logprob ? top_lp : nullptr, top_token ? top_tok : nullptr, ph.lp_ws, ws_bytes};
+  STSCK(sts_op_logprobs(&a, ph.stream));
+  HIPCK(wait_stream(ph.stream));
+  auto give = [&](void* to, const void* from, size_t n) { if (to) std::memcpy(to, from, n * sizeof(int32_t)); };
+  give(logprob, lp, rows); give(entropy, ent, rows); give(rank, rk, rows);
+  give(top_logprob, top_lp, (size_t)rows * top_k); give(top_token, top_tok, (size_t)rows * top_k);
+  return STS_OK;
+}
+
+extern "C" int sts_set_rope(sts_ctx* c, const sts_rope* rope) {
+  double f[128];
+  if (!c || !rope || rope->rotary_dim != c->d.head_dim || rope->interleaved != 0 || (rope->magnitude != 0.f && rope->magnitude != 1.f)) return STS_EINVAL;
+  STSCK(sts_rope_frequencies(rope, f));
+  if (c->pend_prefill || c->pend_decode) return STS_ESTATE;
+  { std::lock_guard<std::mutex> g(c->state_mu); if (c->pf_active) return STS_ESTATE; }
+  HIPCK(hipMemcpy(c->inv_freq, f, c->d.head_dim / 2 * sizeof(double), hipMemcpyHostToDevice));
   return STS_OK;
 }
 

@@ -133,7 +133,7 @@ EXPORTS = [
     "sts_profile_parse", "sts_profile_load", "sts_profile_dump", "sts_profile_free", "sts_latency_query",
     "sts_latency_roofline", "sts_sched_decide", "sts_sched_replay", "sts_max_pages_per_seq_limit", "sts_decode_chunk_plan", "sts_decode_gemm_plan", "sts_decode_layer_plan", "sts_decode_layer_all_rows", "sts_decode_gemm_all_rows", "sts_probe_read", "sts_set_stream_model", "sts_profile_stream_model", "sts_op_gemm_noalloc", "sts_op_gemm_cols", "sts_weight_packed_index", "sts_probe_gemm", "sts_set_tile_model",
     "sts_profile_tile_model", "sts_op_block_tables", "sts_rope_frequencies", "sts_op_rope", "sts_attn_shared_workspace", "sts_op_attn_shared_plan",
-    "sts_op_attn_shared", "sts_op_logprobs_workspace", "sts_op_logprobs",
+    "sts_op_attn_shared", "sts_op_logprobs_workspace", "sts_op_logprobs", "sts_read_logprobs", "sts_set_rope",
 ]
 
 
@@ -371,6 +371,19 @@ class Engine:
         out = np.empty((rows, self.desc.hidden), np.float32)
         _ck(lib().sts_read_hidden(self._ctx, phase, _p(out, C.c_float), rows), "sts_read_hidden")
         return out
+
+    def read_logprobs(self, phase, tokens, top_k=0):
+        """Of the logits of a phase's last call (0 prefill, 1 decode) and a token a row: dict of logprob, entropy, rank [rows], top_logprob, top_token [rows, top_k]."""
+        toks = _i32(tokens)
+        n = toks.size
+        out = dict(logprob=np.empty(n, np.float32), entropy=np.empty(n, np.float32), rank=np.empty(n, np.int32), top_logprob=np.empty((n, top_k), np.float32),
+                   top_token=np.empty((n, top_k), np.int32))
+        _ck(lib().sts_read_logprobs(self._ctx, phase, _p(toks), n, top_k, *[_p(out[k]) for k in ("logprob", "entropy", "rank")],
+                                    *[_p(out[k]) if top_k > 0 else None for k in ("top_logprob", "top_token")]), "sts_read_logprobs")
+        return out
+
+    def set_rope(self, rope: Rope):
+        _ck(lib().sts_set_rope(self._ctx, C.byref(rope)), "sts_set_rope")
 
     # partition and measurement
     def set_partition(self, prefill_cus, decode_cus):

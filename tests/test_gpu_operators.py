@@ -775,3 +775,102 @@ def test_a_step_of_all_operators_eager_and_replayed(sts):
 
 def stored_bf16(x):
     return (np.asarray(x, np.float32).view(np.uint32) >> 16).astype(np.uint16)
+
+
+# ------------------------------------------------------------------------------------------ in the engine
+@pytest.fixture(scope="module")
+def engine(sts):
+    from paper_2504_19516_amd import synth
+    desc = synth.tiny_model("fp32")
+    e = sts.Engine(desc, weight_seed=5, kv_pool_pages=300, max_prefill_tokens=256, max_prefill_seqs=4, max_decode_batch=40, max_seqs=48, max_pages_per_seq=20)
+    yield e, desc
+    e.close()
+
+
+def test_engine_reads_log_probabilities_of_its_last_call(sts, engine):
+    """Of logits that the call returned, of logits that only made tokens, of a prefill's; a call that made none leaves none."""
+    from paper_2504_19516_amd import synth
+    e, desc = engine
+    seqs = [e.seq_create() for _ in range(33)]
+    prompts = [synth.tokens(40 + i, 5 + 3 * i, desc.vocab) for i in range(3)]
+    rng = np.random.default_rng(3)
+
+    def check(phase, logits, tokens, k):
+        got = e.read_logprobs(phase, tokens, k)
+        want = logprobs_reference(logits.astype(np.float64), np.asarray(tokens), k)
+        check_logprobs(dict(got, lse=want["lse"].astype(np.float32)), want, desc.vocab)
+
+    logits = e.prefill_batch(seqs[:3], prompts)
+    check(0, logits, [7, desc.vocab - 1, -1], 5)
+    check(0, logits[:2], [1, 2], 32)                       # the first rows
+    for s in seqs[3:]:
+        e.prefill_append(s, prompts[0], want_logits=False)
+    for code, call in ((sts.EINVAL, lambda: e.read_logprobs(0, [1])), (sts.EINVAL, lambda: e.read_logprobs(1, [1]))):      # that call made none; no decode step yet
+        with pytest.raises(sts.StsError) as x:
+            call()
+        assert x.value.code == code
+    tokens = rng.integers(0, desc.vocab, 33)
+    for n, with_logits, with_next in ((33, True, True), (33, True, False), (1, True, True)):
+        logits, nxt = e.decode_step(seqs[:n], tokens[:n], want_logits=with_logits, want_next=with_next)
+        check(1, logits, rng.integers(0, desc.vocab, n), 8)
+    _, nxt = e.decode_step(seqs, tokens, want_logits=False)
+    got = e.read_logprobs(1, nxt, 1)
+    assert (got["rank"] == 0).all() and np.array_equal(got["top_token"][:, 0], nxt) and np.array_equal(got["top_logprob"][:, 0], got["logprob"])
+    for bad in (dict(phase=2, tokens=[1]), dict(phase=1, tokens=[1] * 34), dict(phase=1, tokens=[]), dict(phase=1, tokens=[1], top_k=33), dict(phase=1, tokens=[1], top_k=-1)):
+        with pytest.raises((sts.StsError, ValueError)) as x:
+            e.read_logprobs(**bad)
+        assert getattr(x.value, "code", sts.EINVAL) == sts.EINVAL
+    e.decode_launch(seqs[:4], tokens[:4])
+    with pytest.raises(sts.StsError) as x:
+        e.read_logprobs(1, [1])
+    assert x.value.code == sts.ESTATE
+    e.decode_finish(4)
+    e.decode_step(seqs, tokens, want_logits=False, want_next=False)
+    with pytest.raises(sts.StsError) as x:
+        e.read_logprobs(1, [1])
+    assert x.value.code == sts.EINVAL
+    for s in seqs:
+        e.seq_free(s)
+
+
+def test_engine_takes_scaled_rotations(sts, engine):
+    """K of a prompt as the engine caches it: the plain rotation's bits come back with the plain description; scaled ones are the plain K turned on by the difference of the
+    angles (both rounded to bf16 once: 2 half steps of the size of the pair)."""
+    from paper_2504_19516_amd import synth
+    e, desc = engine
+    prompt, d = synth.tokens(9, 200, desc.vocab), desc.head_dim
+    plain = sts.Rope(rotary_dim=d, theta=desc.rope_theta)
+
+    def keys():
+        s = e.seq_create()
+        logits = e.prefill_append(s, prompt)
+        k, _ = e.kv_read(0, s, 0, 200)
+        e.seq_free(s)
+        return k.astype(np.float64), logits
+
+    before, first = keys()
+    for change in (dict(scaling=1, factor=4.0), dict(scaling=2, factor=8.0), dict(scaling=3, factor=8.0, low=1.0, high=4.0, original_len=256), dict(scaling=4, factor=8.0, low=1.0, high=32.0,
+                                                                                                                                                    original_len=256)):
+        rope = sts.Rope(rotary_dim=d, theta=desc.rope_theta, **change)
+        e.set_rope(rope)
+        got, logits = keys()
+        a = np.arange(200)[:, None, None] * (sts.rope_frequencies(rope) - sts.rope_frequencies(plain))
+        p, q = before[..., :d // 2], before[..., d // 2:]
+        want = np.concatenate([p * np.cos(a) - q * np.sin(a), q * np.cos(a) + p * np.sin(a)], axis=-1)
+        size = np.tile(np.abs(p) + np.abs(q), 2)
+        near(got, want, 2.0 ** -8 * (size + np.abs(want)) + 1e-6)
+        assert np.abs(got - before).max() > 0.1 and not np.array_equal(logits, first)
+    e.set_rope(plain)
+    after, last = keys()
+    assert np.array_equal(after, before) and np.array_equal(last, first)
+    for bad in (dict(rotary_dim=d // 2), dict(interleaved=1), dict(magnitude=1.3), dict(theta=0.0), dict(scaling=9)):
+        with pytest.raises(sts.StsError) as x:
+            e.set_rope(sts.Rope(**{**dict(rotary_dim=d, theta=1e4), **bad}))
+        assert x.value.code == sts.EINVAL
+    s = e.seq_create()
+    e.prefill_append(s, prompt, 0, 1, want_logits=False)
+    with pytest.raises(sts.StsError) as x:
+        e.set_rope(plain)
+    assert x.value.code == sts.ESTATE
+    e.prefill_abort()
+    e.seq_free(s)
