@@ -16,6 +16,11 @@
 // work, lays each kind's segments end to end (pages, and the start and end of a segment counted as pages) and cuts each line into equal
 // shares, one for each workgroup or wave: a long context is shared by many, short ones are strung together.
 //
+// Measured, bf16, 32 query and 8 KV heads of 128; us of the plan (once a step), and of products and join (each layer):
+//   8 requests on 1031 shared tokens, 6 MB of pages a layer     9    8   4    latency
+//   64 requests on 2048 shared tokens, 100 MB                   10   23   5    4.3 TB/s in the products: memory
+//   256 requests on a document of 8192 tokens, 187 MB           14   72   9    2.6 TB/s and 0.49 PFLOP/s at once: matrix cores and exponentials
+// (read by every request for itself, the document alone would be 8.6 GB a layer).
 #include <algorithm>
 
 #include "device_ops.h"
@@ -27,10 +32,16 @@ constexpr int AS_ROWS = 32;                     // rows of a narrow segment: col
 constexpr int AS_TILE = 128;                    // rows of a wide one
 constexpr int AS_SLOTS = 512;                   // workgroups of a launch: two on each CU
 constexpr int AS_PLAN_THREADS = 512;
-constexpr int AS_JOIN_ROWS = 1024;              // up to so many (request, head) pairs, four waves join each
-// Start and end of a wide and of a narrow segment, and the smallest shares beyond them, in pages. A page takes a workgroup about as long in
-// either kind.
-constexpr int AS_WIDE_START = 16, AS_NARROW_START = 2, AS_WIDE_LEAST = 8, AS_NARROW_LEAST = 4;
+// Up to so many (request, head) pairs four waves join each, beyond it one: step of 16 requests on 8192 tokens (512 pairs) 21.1 us with four and
+// 22.6 with one, of 128 on 2048 (4096 pairs) 30.3 and 24.3.
+constexpr int AS_JOIN_ROWS = 1024;
+// Start and end of a wide and of a narrow segment, and the smallest shares beyond them, in pages; what a page of a wide segment takes a
+// workgroup, in pages of a narrow one. Steps of 40 requests on 1000 tokens / 96 in four groups on 4096 / 256 on one document (two layers):
+// 15.3 / 50.9 / 168 us as here; wide start and least share of 16 and 8 pages 18.8 / 48.8 / 166; wide weight 1: 15.0 / 51.6 / 173, 1.6: 15.0 / 50.9 /
+// 163; narrow least share of 2: 15.9 / 50.0 / 170, 8: 17.2 / 48.1 / 172 (a single request of 8192 tokens 15.6, 14.7 and 14.1 with 2, 4 and 8;
+// 8 requests on 1000 tokens, four layers, 53.7, 56.3 and 61.6).
+constexpr int AS_WIDE_START = 8, AS_NARROW_START = 2, AS_WIDE_LEAST = 4, AS_NARROW_LEAST = 4;
+constexpr float AS_WIDE_WEIGHT = 1.25f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // A piece of a segment: rows row0 .. row0 + rows - 1 (request * heads of a group + head) over the pages [pg0, pg1) of a request's
@@ -219,7 +230,8 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
     cost[is_narrow(x)] += cost_of(x);
   }
   plan_scan(cost, all_cost, waves);
-  int wide = all_cost[0] == 0 ? 0 : (int)(c.slots * ((float)all_cost[0] / ((float)all_cost[0] + (float)all_cost[1])) + 0.5f);
+  const float wide_work = AS_WIDE_WEIGHT * all_cost[0];
+  int wide = all_cost[0] == 0 ? 0 : (int)(c.slots * (wide_work / (wide_work + all_cost[1])) + 0.5f);
   wide = min(max(wide, (int)(all_cost[0] > 0)), c.slots - (all_cost[1] > 0));
   const int narrow = 4 * (c.slots - wide);
   auto line = [&](int total, int count, int start, int least, int granule) {
