@@ -375,13 +375,13 @@ typedef struct {
 int sts_rope_frequencies(const sts_rope* rope, double* out);
 /* The rotation of an engine's own steps from now on, instead of rope_theta's plain one: contexts that were cached before keep the angles they
  * were cached with. rotary_dim = head_dim, not interleaved, magnitude 0 or 1 (STS_EINVAL otherwise); STS_ESTATE while a launch is
- * outstanding or a layer-sliced prefill batch is in flight. */
+ * outstanding or a layer-sliced prefill batch is in flight. Not while another thread's call runs a step. */
 int sts_set_rope(sts_ctx* ctx, const sts_rope* rope);
 /* Rows of Q and K, heads behind each other; strides in elements from row to row. Q rows are turned into q_out, K rows into k_out
  * (may be NULL with a pool) and the pool, V rows into the pool. q_out = q and k_out = k, with equal strides, turn rows in place. */
 typedef struct {
   int32_t dtype;                        /* STS_F32 (no pool), STS_BF16, STS_F16 */
-  int32_t rows, n_q, n_kv, d;           /* n_q or n_kv may be 0 (their pointers are then not read) */
+  int32_t rows, n_q, n_kv, d;           /* rows up to 2^27; n_q or n_kv may be 0 (their pointers are then not read) */
   int32_t pool_pages;
   const void* q; int64_t q_stride; void* q_out; int64_t q_out_stride;
   const void* k; int64_t k_stride; void* k_out; int64_t k_out_stride;
@@ -399,12 +399,12 @@ int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* stream);
  * A context of length 0 gives zeros and an lse of -inf; one that is negative or longer than max_pages, or whose table names a page
  * outside the pool, gives NaN. What lies in a page behind its context is not looked at.
  * The plan is made from the lengths once a step and serves all layers: sts_op_attn_shared_plan, then sts_op_attn_shared for each layer on the
- * same stream (or ordered behind it) with the same description. Calls that may run at the same time need workspaces of their own. */
+ * same stream (or ordered behind it) with the same description; a workspace that holds no plan, or one of a batch of other sizes, gives NaN. Calls that may run at the same time need workspaces of their own. */
 typedef struct {
   int32_t dtype;                        /* STS_BF16 or STS_F16: of q, pool and out */
   int32_t n_requests, n_groups;         /* n_groups 0: nothing is shared, group_starts and shared_lens are not read */
   int32_t n_q, n_kv, d;                 /* n_q / n_kv up to 32, n_kv up to 256, d 64 or 128 */
-  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read; n_requests * max_pages up to 2^28 */
+  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read, up to 2^26; n_requests * max_pages up to 2^28 */
   int64_t table_stride;                 /* >= max_pages */
   const int32_t *tables, *lens;         /* [n_requests][table_stride]; [n_requests]: tokens to attend to, the new one included */
   const int32_t *group_starts, *shared_lens;   /* [n_groups + 1]; [n_groups] */
@@ -421,7 +421,7 @@ int sts_op_attn_shared(const sts_attn_batch* b, const void* q, int64_t q_stride,
  * Logits may be -inf (no probability); a row of nothing else has log probabilities and lse -inf and entropy 0. A row with +inf or NaN has
  * NaN for all of them; in the order of its tokens NaN counts as -inf. */
 typedef struct {
-  int32_t dtype, rows, vocab, top_k;    /* rows up to 65535, top_k 0 to 32 and at most vocab */
+  int32_t dtype, rows, vocab, top_k;    /* rows up to 65535, vocab up to 2^30, top_k 0 to 32 and at most vocab */
   int64_t row_stride;                   /* elements from row to row */
   const void* logits;                   /* aligned to its elements */
   const int32_t* tokens;                /* [rows]; one outside [0, vocab): log probability NaN, rank -1. NULL: no tokens */
@@ -430,6 +430,7 @@ typedef struct {
   float* top_logprob; int32_t* top_token;      /* [rows][top_k], in that order */
   void* workspace; int64_t workspace_bytes;    /* 16-byte aligned, sts_op_logprobs_workspace bytes (0 where there are many rows) */
 } sts_logprobs;
+/* Host only, no GPU state: bytes of workspace; -1 for sizes out of range. */
 int64_t sts_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t top_k);
 int sts_op_logprobs(const sts_logprobs* a, void* stream);
 

@@ -52,6 +52,7 @@ struct Range { Item first; int next, end, pad[2]; };              // items of a 
 // done: its one piece finishes it. len < 0: its length is out of range.
 struct Parts { int p_part, p_step, p_count, s_part, s_count, len, done, pad; };
 struct Plan {
+  unsigned long long* sizes;                     // sizes_tag() of the batch that it was made for
   Range* ranges;                                 // [slots][4]
   Item* items;
   Parts* parts;                                  // [n_requests]
@@ -71,6 +72,7 @@ size_t lay_out(unsigned char* base, int n, int n_q, int n_kv, int d, Plan* p) {
   auto take = [&](size_t bytes) { unsigned char* q = base + at; at += up256(bytes); return q; };
   const size_t rows = (size_t)max_part_rows(n, n_q, n_kv) * n_kv;
   Plan q;
+  q.sizes = reinterpret_cast<unsigned long long*>(take(sizeof(unsigned long long)));
   q.ranges = reinterpret_cast<Range*>(take(slots_of(n_kv) * 4 * sizeof(Range)));
   q.items = reinterpret_cast<Item*>(take(max_items(n, n_kv) * sizeof(Item)));
   q.parts = reinterpret_cast<Parts*>(take(n * sizeof(Parts)));
@@ -80,8 +82,15 @@ size_t lay_out(unsigned char* base, int n, int n_q, int n_kv, int d, Plan* p) {
   return at;
 }
 
+// The sizes on which the indexes of a plan's users depend, never 0. A workspace without a plan of the batch's sizes gives NaN: nothing in it is followed.
+unsigned long long sizes_tag(const sts_attn_batch& b) {
+  unsigned long long t = 1;
+  for (int32_t x : {b.n_requests, b.n_q, b.n_kv, b.d, b.max_pages}) t = t * 0x9E3779B97F4A7C15ull + (uint32_t)x;
+  return t << 1 | 1;
+}
+
 // ---- the plan: one workgroup
-struct PlanCall { int n, groups, heads, slots, max_pages; const int *lens, *group_starts, *shared_lens; Plan plan; };
+struct PlanCall { unsigned long long tag; int n, groups, heads, slots, max_pages; const int *lens, *group_starts, *shared_lens; Plan plan; };
 
 // Exclusive sums over the workgroup's threads, and the totals, of N values.
 template <int N>
@@ -160,7 +169,7 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
   __shared__ unsigned short start[N + 1], tile0[N + 1], item0[2 * N + 1];
   __shared__ int lens[N], pages[N], wide_at[N + 1], narrow_at[2 * N + 1], part0[2 * N], waves[2][AS_PLAN_THREADS / 64], malformed;
   const int n = c.n, groups = c.groups, tid = threadIdx.x;
-  if (tid == 0) malformed = 0;
+  if (tid == 0) { malformed = 0; *c.plan.sizes = c.tag; }
   for (int i = tid; i < n; i += AS_PLAN_THREADS) {               // -1: longer than its table, or negative
     const int l = c.lens[i];
     lens[i] = l < 0 || l > c.max_pages * (long long)OP_PAGE ? -1 : l;
@@ -326,6 +335,7 @@ struct AttnCall {
   int n, n_q, n_kv, heads, pool_pages;
   float scale_log2e;
   bool q_vec, out_vec;                           // rows can be loaded 16 bytes, stored 8 bytes at a time
+  unsigned long long tag;                        // what plan.sizes has to hold
   Plan plan;
 };
 
@@ -760,7 +770,7 @@ __global__ void __launch_bounds__(256, 2) attn_shared_kernel(AttnCall<T> c) {
   // With 8 KV heads a head's workgroups are all on one XCD: the tiles of a prefix find each other's pages in its L2.
   const int slot = blockIdx.x / c.n_kv, kvh = blockIdx.x % c.n_kv;
   const Range r = c.plan.ranges[slot * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
-  if (r.first.rows == 0) return;
+  if (*c.plan.sizes != c.tag || r.first.rows == 0) return;
   Item it = r.first;
   for (int i = r.next;; i++) {
     if (it.rows > AS_ROWS) run_wide<T, D>(smem, c, it, kvh);
@@ -780,7 +790,8 @@ __global__ void __launch_bounds__(256) attn_shared_join_kernel(AttnCall<T> c) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + wave;
   if (at >= c.n * c.n_q) return;
   const int r = at / c.n_q, head = at % c.n_q, kvh = head / c.heads, h = head % c.heads;
-  const Parts p = c.plan.parts[r];
+  Parts p = c.plan.parts[r];
+  if (*c.plan.sizes != c.tag) p = Parts{0, 0, 0, 0, 0, -1, 0, 0};
   if (p.done) return;
   const int count = p.len < 0 ? 0 : p.p_count + p.s_count;
   auto row_of = [&](int j) { return (size_t)((j < p.p_count ? p.p_part + j * p.p_step : p.s_part + (j - p.p_count) * c.heads) + h) * c.n_kv + kvh; };
@@ -852,7 +863,7 @@ bool sizes_ok(int n, int n_q, int n_kv, int d) {
 // The batch's description, without what a call of one layer adds.
 int check_batch(const sts_attn_batch* b, Plan* plan) {
   if (!b || (b->dtype != STS_BF16 && b->dtype != STS_F16) || !sizes_ok(b->n_requests, b->n_q, b->n_kv, b->d)) return STS_EINVAL;
-  if (b->n_groups < 0 || b->n_groups > b->n_requests || b->pool_pages < 0 || b->max_pages < 0 || (int64_t)b->n_requests * b->max_pages > (1 << 28) || b->table_stride < b->max_pages) return STS_EINVAL;
+  if (b->n_groups < 0 || b->n_groups > b->n_requests || b->pool_pages < 0 || b->max_pages < 0 || b->max_pages > (1 << 26) || (int64_t)b->n_requests * b->max_pages > (1 << 28) || b->table_stride < b->max_pages) return STS_EINVAL;
   if (b->n_requests == 0) return STS_OK;
   if (!b->lens || (b->max_pages > 0 && !b->tables) || (b->n_groups > 0 && (!b->group_starts || !b->shared_lens))) return STS_EINVAL;
   if (!b->workspace || !aligned(b->workspace, 256)) return STS_EINVAL;
@@ -878,7 +889,7 @@ extern "C" int sts_op_attn_shared_plan(const sts_attn_batch* b, void* stream) {
   OnStreamDevice dev(s);
   if (dev.error() != hipSuccess) return op_result(dev.error());
   const int n = b->n_requests, slots = slots_of(b->n_kv);
-  const PlanCall c{n, b->n_groups, b->n_q / b->n_kv, slots, b->max_pages, b->lens, b->group_starts, b->shared_lens, plan};
+  const PlanCall c{sizes_tag(*b), n, b->n_groups, b->n_q / b->n_kv, slots, b->max_pages, b->lens, b->group_starts, b->shared_lens, plan};
   return op_result(launch(attn_shared_plan_kernel, dim3(1), dim3(AS_PLAN_THREADS), 0, s, c));
 }
 
@@ -886,7 +897,7 @@ template <typename T>
 static int attn_shared(const sts_attn_batch* b, const Plan& plan, const void* q, int64_t q_stride, const void* pool, void* out, int64_t out_stride, float* lse, float scale, hipStream_t s) {
   const bool q_vec = aligned(q, 16) && q_stride % 8 == 0, out_vec = aligned(out, 8) && out_stride % 4 == 0;
   const AttnCall<T> c{reinterpret_cast<const T*>(q), q_stride, reinterpret_cast<const T*>(pool), reinterpret_cast<T*>(out), out_stride, lse, b->tables, b->table_stride,
-                      b->n_requests, b->n_q, b->n_kv, b->n_q / b->n_kv, b->pool_pages, scale * LOG2E, q_vec, out_vec, plan};
+                      b->n_requests, b->n_q, b->n_kv, b->n_q / b->n_kv, b->pool_pages, scale * LOG2E, q_vec, out_vec, sizes_tag(*b), plan};
   return op_result(b->d == 128 ? launch_attn<T, 128>(s, c) : launch_attn<T, 64>(s, c));
 }
 

@@ -1658,6 +1658,8 @@ extern "C" int sts_read_logprobs(sts_ctx* c, int32_t phase, const int32_t* token
   const int32_t most = phase == 0 ? c->p.max_prefill_seqs : c->p.max_decode_batch;
   int64_t ws_bytes = 0;
   for (int32_t r = 1; r <= most; r++) ws_bytes = std::max(ws_bytes, sts_op_logprobs_workspace(STS_F32, r, c->d.vocab, std::min(32, c->d.vocab)));
+  OnStreamDevice dev(ph.stream);
+  if (dev.error() != hipSuccess) return op_result(dev.error());
   if (!ph.h_lp) {
     std::lock_guard<std::mutex> g(c->alloc_mu);              // the other phase's control thread may be here too
     if (!ph.lp_ws) STSCK(dev_alloc(c, &ph.lp_ws, (size_t)ws_bytes));

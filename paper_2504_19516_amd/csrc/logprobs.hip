@@ -461,7 +461,7 @@ hipError_t launch_logprobs(hipStream_t s, const LogprobsCall& c) {
 using namespace sts;
 
 extern "C" int64_t sts_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t top_k) {
-  if (dtype < STS_F32 || dtype > STS_F16 || rows < 0 || vocab < 1 || top_k < 0 || top_k > LP_MAX_K) return -1;
+  if (dtype < STS_F32 || dtype > STS_F16 || rows < 0 || rows > 65535 || vocab < 1 || vocab > (1 << 30) || top_k < 0 || top_k > LP_MAX_K) return -1;
   return rows == 0 ? 0 : (int64_t)workspace_of(rows, logprob_parts(rows, vocab), top_k);
 }
 

@@ -335,7 +335,7 @@ extern "C" int sts_rope_frequencies(const sts_rope* rope, double* out) {
 extern "C" int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* stream) {
   RopeTurns turns;
   if (!rope || !a || !rope_turns(*rope, &turns)) return STS_EINVAL;
-  if (a->dtype < STS_F32 || a->dtype > STS_F16 || a->rows < 0 || a->n_q < 0 || a->n_kv < 0 || a->d < rope->rotary_dim || a->d > 1024 || a->n_q > 4096 || a->n_kv > 4096) return STS_EINVAL;
+  if (a->dtype < STS_F32 || a->dtype > STS_F16 || a->rows < 0 || a->rows > (1 << 27) || a->n_q < 0 || a->n_kv < 0 || a->d < rope->rotary_dim || a->d > 1024 || a->n_q > 4096 || a->n_kv > 4096) return STS_EINVAL;
   if (a->n_q > 0 && (!a->q || !a->q_out)) return STS_EINVAL;
   if (a->n_kv > 0 && (!a->k || (!a->k_out && !a->pool))) return STS_EINVAL;
   if (a->pool && (a->n_kv < 1 || !a->v || !a->places || a->dtype == STS_F32 || (a->d != 64 && a->d != 128) || a->pool_pages < 0)) return STS_EINVAL;
@@ -343,6 +343,8 @@ extern "C" int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* s
   const int64_t q_row = (int64_t)a->n_q * a->d, k_row = (int64_t)a->n_kv * a->d;
   if (a->rows > 1 && ((a->n_q > 0 && (a->q_stride < q_row || a->q_out_stride < q_row)) || (a->n_kv > 0 && (a->k_stride < k_row || (a->k_out && a->k_out_stride < k_row) ||
       (a->pool && a->v_stride < k_row))))) return STS_EINVAL;
+  auto elements = [&](const void* p) { return aligned(p, dtype_bytes(a->dtype)); };
+  if ((a->n_q > 0 && !(elements(a->q) && elements(a->q_out))) || (a->n_kv > 0 && !(elements(a->k) && elements(a->k_out))) || (a->pool && !(elements(a->v) && elements(a->pool)))) return STS_EINVAL;
   if ((a->q && a->q == a->q_out && a->q_stride != a->q_out_stride) || (a->k && a->k == a->k_out && a->k_stride != a->k_out_stride)) return STS_EINVAL;
   if (a->rows == 0 || (a->n_q == 0 && a->n_kv == 0)) return STS_OK;
   if (!a->positions) return STS_EINVAL;

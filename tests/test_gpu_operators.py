@@ -466,6 +466,44 @@ def test_shared_attention_same_bits_again_and_in_a_graph(sts):
             assert np.array_equal(dev.get(out, first.shape, "bf16"), first) and np.array_equal(dev.get(lse, lse0.shape, "f32"), lse0)
 
 
+def test_shared_attention_without_a_plan_of_its_sizes_is_nan(sts):
+    """A workspace that holds none, or one of other requests, heads or tables: nothing in it is followed."""
+    rng = np.random.default_rng(22)
+    n, heads, n_kv, d, pages = 70, 4, 2, 64, 40
+    q = rng.standard_normal((n, heads * n_kv * d))
+    with Device() as dev:
+        size = sts.attn_shared_workspace(n, heads, 1, 2 * d)                 # the largest of those below
+        dev_q, pool = dev.put(q, "bf16"), dev.put(rng.standard_normal((pages, n_kv, 2 * 16 * d)), "bf16")
+        tables, lens = dev.ints(rng.integers(0, pages, (n, 6))), dev.ints(rng.integers(60, 90, n))
+        starts, shared = dev.ints([0, n]), dev.ints([48])
+        ws = dev.put(np.zeros(size, np.uint8))
+
+        def batch(**change):
+            good = dict(dtype=sts.DTYPES["bf16"], n_requests=n, n_groups=1, n_q=heads * n_kv, n_kv=n_kv, d=d, pool_pages=pages, max_pages=6, table_stride=6, tables=tables, lens=lens,
+                        group_starts=starts, shared_lens=shared, workspace=ws, workspace_bytes=size)
+            return sts.AttnBatch(**{**good, **change})
+
+        width = heads * n_kv * d                             # elements of a row of q and out, whatever of them a batch has
+
+        def layer(b):
+            out, lse = dev.put(np.full((n, width), 7.0), "bf16"), dev.put(np.full((n, width // d), 7.0, np.float32))
+            sts.op_attn_shared(b, dev_q, width, pool, out, width, lse)
+            dev.sync()
+            got = dev.get(out, (n, width), "bf16")
+            assert (got[b.n_requests:] == 7.0).all() and (got[:, b.n_q * b.d:] == 7.0).all()
+            return got[:b.n_requests, :b.n_q * b.d], dev.get(lse, n * width // d, "f32")[:b.n_requests * b.n_q]
+
+        out, lse = layer(batch())
+        assert np.isnan(out).all() and np.isnan(lse).all()
+        sts.op_attn_shared_plan(batch())
+        assert np.isfinite(layer(batch())[0]).all()
+        other = dict(n_groups=0)
+        for change in (dict(n_requests=n - 1, **other), dict(n_q=n_kv), dict(n_q=heads, n_kv=1), dict(n_q=heads, n_kv=1, d=2 * d), dict(max_pages=5)):
+            out, lse = layer(batch(**change))
+            assert np.isnan(out).all() and np.isnan(lse).all(), change
+        assert np.isfinite(layer(batch())[0]).all()
+
+
 def test_shared_attention_of_two_streams_at_once(sts):
     """Workspaces of their own: calls under way together do not see each other."""
     rng = np.random.default_rng(21)
@@ -829,6 +867,30 @@ def test_engine_reads_log_probabilities_of_its_last_call(sts, engine):
     with pytest.raises(sts.StsError) as x:
         e.read_logprobs(1, [1])
     assert x.value.code == sts.EINVAL
+    for s in seqs:
+        e.seq_free(s)
+
+
+def test_engine_reads_log_probabilities_of_both_phases_of_a_step(sts, engine):
+    """Each phase's own, before and after the partition changes."""
+    from paper_2504_19516_amd import synth
+    e, desc = engine
+    seqs = [e.seq_create() for _ in range(7)]
+    prompts = [synth.tokens(60 + i, 9 + 2 * i, desc.vocab) for i in range(7)]
+    e.prefill_batch(seqs[2:6], prompts[2:6])
+    e.prefill_append(seqs[6], prompts[6])
+    try:
+        e.set_partition(128, 128)
+        plog, dlog, _ = e.step_concurrent(seqs[:2], prompts[:2], 0, desc.n_layers, seqs[2:], [3, 4, 5, 6, 7])
+        for split in (None, (192, 64)):
+            if split:
+                e.set_partition(*split)
+            for phase, logits in ((0, plog), (1, dlog)):
+                tokens = np.arange(len(logits)) * 11 + 1
+                got, want = e.read_logprobs(phase, tokens, 3), logprobs_reference(logits.astype(np.float64), tokens, 3)
+                check_logprobs(dict(got, lse=want["lse"].astype(np.float32)), want, desc.vocab)
+    finally:
+        e.set_partition(256, 256)
     for s in seqs:
         e.seq_free(s)
 

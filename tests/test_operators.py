@@ -43,7 +43,8 @@ def test_rope_refuses(sts):
     call = lambda a: sts.op_rope(plain, a)  # noqa: E731
     for change in [dict(dtype=-1), dict(dtype=3), dict(dtype=0), dict(rows=-1), dict(n_q=-1), dict(n_kv=-1), dict(d=62), dict(d=96), dict(q=None), dict(q_out=None), dict(k=None), dict(v=None),
                    dict(pool=None), dict(positions=None), dict(places=None), dict(q_stride=255), dict(q_out_stride=0), dict(k_stride=127), dict(v_stride=127), dict(pool_pages=-1),
-                   dict(k_out=8 * A, k_out_stride=100), dict(q_out=A, q_out_stride=300), dict(k_out=3 * A, k_out_stride=136), dict(n_kv=0)]:
+                   dict(k_out=8 * A, k_out_stride=100), dict(q_out=A, q_out_stride=300), dict(k_out=3 * A, k_out_stride=136), dict(n_kv=0),
+                   dict(rows=(1 << 27) + 1), dict(q=A + 1), dict(q_out=2 * A + 1), dict(k=3 * A + 1), dict(k_out=8 * A + 1, k_out_stride=128), dict(v=4 * A + 1), dict(pool=5 * A + 1)]:
         refused(sts, call, sts.RopeRows, good, **change)
     ok = dict(rotary_dim=64, theta=1e4, factor=2.0, low=1.0, high=4.0, original_len=4096, scaling=3)
     bad = [dict(rotary_dim=0), dict(rotary_dim=63), dict(rotary_dim=258), dict(theta=0.0), dict(theta=math.nan), dict(theta=math.inf), dict(scaling=5), dict(scaling=-1), dict(factor=0.0),
@@ -62,7 +63,7 @@ def test_attention_refuses(sts):
                 workspace=5 * A, workspace_bytes=size)
     batch = [dict(dtype=0), dict(dtype=3), dict(n_requests=-1), dict(n_requests=4097), dict(n_groups=-1), dict(n_groups=7), dict(n_q=7), dict(n_q=0), dict(n_kv=0), dict(n_q=66),
              dict(d=32), dict(d=96), dict(pool_pages=-1), dict(max_pages=-1), dict(max_pages=1 << 26, table_stride=1 << 26), dict(table_stride=4), dict(tables=None), dict(lens=None), dict(group_starts=None), dict(shared_lens=None),
-             dict(workspace=None), dict(workspace=5 * A + 16), dict(workspace_bytes=size - 1), dict(n_kv=257, n_q=257)]
+             dict(workspace=None), dict(workspace=5 * A + 16), dict(workspace_bytes=size - 1), dict(n_kv=257, n_q=257), dict(n_requests=1, n_groups=1, max_pages=(1 << 26) + 1, table_stride=1 << 27)]
     layer = lambda b, q=A, qs=512, pool=A, out=A, os_=512, scale=0.0: sts.op_attn_shared(b, q, qs, pool, out, os_, None, scale)  # noqa: E731
     for change in batch:
         refused(sts, sts.op_attn_shared_plan, sts.AttnBatch, good, **change)
@@ -92,7 +93,7 @@ def test_logprobs_refuses(sts):
                    dict(logits=None), dict(logits=A + 2), dict(tokens=None), dict(top_k=0), dict(workspace=None), dict(workspace=9 * A + 8), dict(workspace_bytes=size - 1)]:
         refused(sts, sts.op_logprobs, sts.Logprobs, good, **change)
     sts.op_logprobs(sts.Logprobs(**{**good, "rows": 0}))
-    for bad in [(3, 2, 10, 1), (0, -1, 10, 1), (0, 2, 0, 1), (0, 2, 10, 33), (0, 2, 10, -1)]:
+    for bad in [(3, 2, 10, 1), (0, -1, 10, 1), (0, 2, 0, 1), (0, 2, 10, 33), (0, 2, 10, -1), (0, 65536, 10, 1), (0, 2, (1 << 31) - 1, 1)]:
         assert sts.op_logprobs_workspace(*bad) == -1
     assert sts.op_logprobs_workspace(1, 4000, 128256, 20) == 0
 
