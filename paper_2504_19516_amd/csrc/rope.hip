@@ -9,8 +9,8 @@
 // host makes the fractions in 64 bits and hands them over as a kernel argument; a workgroup computes its rows' cosines and sines once
 // and keeps them in LDS for all heads.
 //
-// Bound by memory for prefills (8192 rows of 32 + 8 heads of 128: 201 MB in 54 us, 3.7 TB/s, where a plain copy takes 40), by latency for decodes
-// (64 rows 4.4 us). V columns stored 1 KB in a row by neighbouring lanes, both halves of a page at once, were level.
+// Bound by memory for prefills (8192 rows of 32 + 8 heads of 128: 201 MB in 44 us, 4.6 TB/s, where a plain copy takes 38), by latency for decodes
+// (64 rows 4 us). V columns stored 1 KB in a row by neighbouring lanes, both halves of a page at once, were level.
 #include <algorithm>
 #include <cmath>
 
@@ -21,10 +21,10 @@ namespace {
 
 constexpr int RP_THREADS = 256, RP_MAX_PAIRS = 128;   // head elements that turn: up to 256
 // Rows from which a workgroup takes a page's 16 (its V then leaves in whole 32-byte columns); below it takes one, 32 heads at a time. 300
-// rows of 32 + 8 heads 6.3 us with one row a workgroup, 6.6 with 16; 1000 12.9 and 8.5.
+// rows of 32 + 8 heads 6.1 us with one row a workgroup, 5.6 with 16, but 6.6 and 7.6 of as many requests; 1000 rows 11.2 and 7.6, 12.6 and 12.3.
 constexpr int RP_PAGE_ROWS = 512, RP_HEADS = 32;
 // Workgroups wanted of launches with 16 rows each, in up to eight parts of their rotations and of their V: 512 / 1024 / 2048 wanted, 8192 rows took
-// 55 / 54 / 55 us, with neighbours as pairs 67 / 54 / 55.
+// 45 / 44 / 44 us, with neighbours as pairs 52 / 44 / 45.
 constexpr int RP_WORKGROUPS = 1024, RP_PARTS = 8;
 
 struct RopeTurns { uint64_t step[RP_MAX_PAIRS]; };    // pair i: 2^64 * f_i / 2 pi, modulo 2^64
@@ -139,15 +139,15 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
     auto source = [&](const Task& k) {
       return k.h < a.n_q ? reinterpret_cast<const T*>(a.q) + (row0 + k.r) * a.q_stride + k.h * d : reinterpret_cast<const T*>(a.k) + (row0 + k.r) * a.k_stride + (k.h - a.n_q) * d;
     };
-    auto targets = [&](const Task& k, T** to, T** page) {              // up to two
-      *page = nullptr;
-      if (k.h < a.n_q) { *to = reinterpret_cast<T*>(a.q_out) + (row0 + k.r) * a.q_out_stride + k.h * d; return; }
-      const int h = k.h - a.n_q, p = places[k.r];
-      *to = a.k_out ? reinterpret_cast<T*>(a.k_out) + (row0 + k.r) * a.k_out_stride + h * d : nullptr;
-      if (p >= 0) *page = page_head(p, h) + p % OP_PAGE * d;
+    struct Targets { T *row, *page; bool to_row, to_page; };           // pointers by value: through memory they would be generic ones
+    auto targets = [&](const Task& k) {
+      const bool q = k.h < a.n_q;
+      const int h = q ? 0 : k.h - a.n_q, p = q ? -1 : places[k.r];
+      T* row = q ? reinterpret_cast<T*>(a.q_out) + (row0 + k.r) * a.q_out_stride + k.h * d : reinterpret_cast<T*>(a.k_out) + (row0 + k.r) * a.k_out_stride + h * d;
+      return Targets{row, page_head(max(p, 0), h) + max(p, 0) % OP_PAGE * d, q || a.k_out, p >= 0};
     };
     if constexpr (VEC) {
-      constexpr int DEPTH = ROWS == 1 ? 1 : 4;         // tasks of a thread under way
+      constexpr int DEPTH = ROWS == 1 ? 1 : 2;         // tasks of a thread under way: 8192 rows 44.4 / 44.0 / 48.4 us with 1 / 2 / 4
       V x[DEPTH], y[DEPTH];
       Task k[DEPTH];
       auto is_pair = [&](const Task& q) { return !c.interleaved && q.task < pair_tasks; };
@@ -169,8 +169,7 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
 #pragma unroll
         for (int u = 0; u < DEPTH; u++) {
           if (t + u * RP_THREADS >= t1) break;
-          T *to, *page;
-          targets(k[u], &to, &page);
+          const Targets to = targets(k[u]);
           const f32x2* tr = trig + k[u].r * P;
           const int at = place_in(k[u]);
           if (is_pair(k[u])) {
@@ -181,8 +180,8 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
               rotate_pair((float)x[u][e], (float)y[u][e], cs[0], cs[1], &v, &w);
               x[u][e] = (T)v; y[u][e] = (T)w;
             }
-            if (to) *reinterpret_cast<V*>(to + at + P) = y[u];
-            if (page) *reinterpret_cast<V*>(page + at + P) = y[u];
+            if (to.to_row) *reinterpret_cast<V*>(to.row + at + P) = y[u];
+            if (to.to_page) *reinterpret_cast<V*>(to.page + at + P) = y[u];
           } else if (at < R) {
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
@@ -192,8 +191,8 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
               x[u][e] = (T)v; x[u][e + 1] = (T)w;
             }
           }
-          if (to) *reinterpret_cast<V*>(to + at) = x[u];
-          if (page) *reinterpret_cast<V*>(page + at) = x[u];
+          if (to.to_row) *reinterpret_cast<V*>(to.row + at) = x[u];
+          if (to.to_page) *reinterpret_cast<V*>(to.page + at) = x[u];
         }
       }
     } else {
@@ -201,11 +200,10 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
       for (int t = t0 + tid; t < t1; t += RP_THREADS) {
         const Task k = task_of(t);
         const T* src = source(k);
-        T *to, *page;
-        targets(k, &to, &page);
+        const Targets to = targets(k);
         auto put = [&](int e, T v) {
-          if (to) to[e] = v;
-          if (page) page[e] = v;
+          if (to.to_row) to.row[e] = v;
+          if (to.to_page) to.page[e] = v;
         };
         if (k.task < P) {
           const int e = c.interleaved ? 2 * k.task : k.task, f = c.interleaved ? e + 1 : e + P;
