@@ -90,7 +90,22 @@ unsigned long long sizes_tag(const sts_attn_batch& b) {
 }
 
 // ---- the plan: one workgroup
-struct PlanCall { unsigned long long tag; int n, groups, heads, slots, max_pages; const int *lens, *group_starts, *shared_lens; Plan plan; };
+// wide_requests: of a wide tile, and 2^20 over it, rounded up: quotients of numbers up to 4223 by it are exact, as 4223 * 128 < 2^20
+struct PlanCall { unsigned long long tag; int n, groups, heads, slots, max_pages, wide_requests; unsigned wide_inverse; const int *lens, *group_starts, *shared_lens; Plan plan; };
+
+// The sum of a wave's values up to each lane's: within rows of 16 lanes, then the rows before.
+__device__ __forceinline__ int wave_sums_up(int x) {
+  auto moved = [&](auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
+  using std::integral_constant;
+  const integral_constant<int, 0xF> all;
+  x += moved(integral_constant<int, 0x111>{}, all);              // from 1, 2, 4, 8 lanes below
+  x += moved(integral_constant<int, 0x112>{}, all);
+  x += moved(integral_constant<int, 0x114>{}, all);
+  x += moved(integral_constant<int, 0x118>{}, all);
+  x += moved(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});      // rows 1 and 3: the last lane of the row before
+  x += moved(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});      // rows 2 and 3: lane 31
+  return x;
+}
 
 // Exclusive sums over the workgroup's threads, and the totals, of N values.
 template <int N>
@@ -99,12 +114,7 @@ __device__ __forceinline__ void plan_scan(int (&v)[N], int (&total)[N], int (*wa
   int x[N];
 #pragma unroll
   for (int i = 0; i < N; i++) {
-    x[i] = v[i];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x[i], o, 64);
-      if (lane >= o) x[i] += y;
-    }
+    x[i] = wave_sums_up(v[i]);
     if (lane == 63) waves[i][wave] = x[i];
   }
   __syncthreads();
@@ -140,14 +150,15 @@ struct Line {
     const int room = (k + 1) * share - at - start;
     return room >= pages ? pages : max(room, 0) & ~(granule - 1);
   }
-  // first share with pages of a segment, and how many shares have some
-  __device__ __forceinline__ void cut(int at, int pages, int* first, int* count) const {
-    *first = 0; *count = 0;
-    if (pages == 0) return;
-    int k0 = share_of(at), k1 = share_of(at + start + pages - 1);
-    if (k0 < k1 && up_to(at, pages, k0) == 0) k0++;
-    if (k0 < k1 && up_to(at, pages, k1 - 1) == pages) k1--;
-    *first = k0; *count = k1 - k0 + 1;
+  // the first share that has pages of a segment of some, and how many have
+  __device__ __forceinline__ int first(int at, int pages) const {
+    const int k = share_of(at);
+    return k + (up_to(at, pages, k) == 0);
+  }
+  __device__ __forceinline__ int pieces(int at, int pages) const {
+    if (pages == 0) return 0;
+    const int last = share_of(at + start + pages - 1), k0 = first(at, pages);
+    return last - k0 + (last == k0 || up_to(at, pages, last - 1) < pages);
   }
 };
 
@@ -167,24 +178,23 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
   // by group: first request, shared pages, first tile; by tile: place on the line of wide segments; by segment: place on the line of narrow
   // ones, first item, first partial row
   __shared__ unsigned short start[N + 1], tile0[N + 1], item0[2 * N + 1];
-  __shared__ int lens[N], pages[N], wide_at[N + 1], narrow_at[2 * N + 1], part0[2 * N], waves[2][AS_PLAN_THREADS / 64], malformed;
+  __shared__ int lens[N], pages[N], wide_at[N + 1], narrow_at[2 * N + 1], part0[2 * N], waves[2][AS_PLAN_THREADS / 64];
   const int n = c.n, groups = c.groups, tid = threadIdx.x;
-  if (tid == 0) { malformed = 0; *c.plan.sizes = c.tag; }
-  for (int i = tid; i < n; i += AS_PLAN_THREADS) {               // -1: longer than its table, or negative
-    const int l = c.lens[i];
-    lens[i] = l < 0 || l > c.max_pages * (long long)OP_PAGE ? -1 : l;
-  }
-  __syncthreads();
+  if (tid == 0) *c.plan.sizes = c.tag;
   // groups whose starts do not lead from 0 to n in order are left aside: every request then reads all its pages for itself
+  bool malformed = false;
   for (int g = tid; groups > 0 && g <= groups; g += AS_PLAN_THREADS) {
     const int s = c.group_starts[g];
     const bool ok = s >= 0 && s <= n && (g > 0 || s == 0) && (g < groups ? s <= c.group_starts[g + 1] : s == n);
     start[g] = (unsigned short)(ok ? s : 0);
-    if (!ok) malformed = 1;
+    malformed |= !ok;
     if (g < groups) pages[g] = max(c.shared_lens[g], 0) / OP_PAGE;
   }
-  __syncthreads();
-  const bool shares = groups > 0 && !malformed;
+  for (int i = tid; i < n; i += AS_PLAN_THREADS) {               // -1: longer than its table, or negative
+    const int l = c.lens[i];
+    lens[i] = l < 0 || l > c.max_pages * (long long)OP_PAGE ? -1 : l;
+  }
+  const bool shares = !__syncthreads_or(malformed) && groups > 0;
   // a group shares what its shortest member holds in whole pages
   if (shares)
     for (int i = tid; i < n; i += AS_PLAN_THREADS) {
@@ -194,10 +204,10 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
     }
   __syncthreads();
   // requests of a tile: a group that fills more than the columns of one product takes wide ones
-  auto per_tile = [&](int members) { return (members * c.heads > AS_ROWS ? AS_TILE : AS_ROWS) / c.heads; };
+  auto per_tile = [&](int members) { return members * c.heads > AS_ROWS ? c.wide_requests : AS_TILE; };
   auto tiles_of = [&](int g) {
-    const int members = start[g + 1] - start[g], per = per_tile(members);
-    return pages[g] > 0 ? (members + per - 1) / per : 0;
+    const int members = start[g + 1] - start[g];
+    return pages[g] == 0 ? 0 : members * c.heads > AS_ROWS ? (int)((members + c.wide_requests - 1) * (unsigned long long)c.wide_inverse >> 20) : 1;
   };
   const int gper = (groups + AS_PLAN_THREADS - 1) / AS_PLAN_THREADS, g0 = min(groups, tid * gper), g1 = min(groups, g0 + gper);
   int tiles[1] = {0}, all_tiles[1];
@@ -214,29 +224,28 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
 
   // segments: the tiles, then the requests' own pages
   const int T = all_tiles[0], segments = T + n;
-  struct Segment { int row0, rows, request, pg0, pages, len; };
-  auto segment = [&](int s) {
-    Segment x;
-    if (s < T) {
-      const int g = last_up_to(tile0, groups, s);                 // the last of several with that first tile: it has tiles
-      const int per = per_tile(start[g + 1] - start[g]), r0 = start[g] + (s - tile0[g]) * per;
-      x = {r0 * c.heads, min(per, start[g + 1] - r0) * c.heads, start[g], 0, pages[g], pages[g] * OP_PAGE};
-    } else {
-      const int r = s - T, l = lens[r], shared = shares ? pages[last_up_to(start, groups, r)] : 0;
-      x = {r * c.heads, c.heads, r, shared, (max(l, 0) + OP_PAGE - 1) / OP_PAGE - shared, l};
-    }
-    return x;
+  struct Tile { int group, request, rows; };          // its first request
+  auto tile = [&](int s) {
+    const int g = last_up_to(tile0, groups, s);                   // the last of several with that first tile: it has tiles
+    const int per = per_tile(start[g + 1] - start[g]), r0 = start[g] + (s - tile0[g]) * per;
+    return Tile{g, r0, min(per, start[g + 1] - r0) * c.heads};
   };
-  auto is_narrow = [](const Segment& x) { return x.rows <= AS_ROWS; };
-  auto cost_of = [&](const Segment& x) { return x.pages > 0 ? x.pages + (is_narrow(x) ? AS_NARROW_START : AS_WIDE_START) : 0; };
+  auto rows_of = [&](int s) { return s < T ? tile(s).rows : c.heads; };
+  auto held_pages = [&](int r) { return (max(lens[r], 0) + OP_PAGE - 1) / OP_PAGE; };
+  auto cost_of = [&](int pages, int kind) { return pages > 0 ? pages + (kind ? AS_NARROW_START : AS_WIDE_START) : 0; };
   const int per = (segments + AS_PLAN_THREADS - 1) / AS_PLAN_THREADS, s0 = min(segments, tid * per), s1 = min(segments, s0 + per);
-  Segment kept{};                                // the thread's segment where it has but one
-  if (per == 1 && s0 < s1) kept = segment(s0);
-  auto get = [&](int s) { return per == 1 ? kept : segment(s); };
   int cost[2] = {0, 0}, all_cost[2];             // wide, narrow
+  int rows = c.heads;                            // of the thread's last segment
   for (int s = s0; s < s1; s++) {
-    const Segment x = get(s);
-    cost[is_narrow(x)] += cost_of(x);
+    int seg_pages;
+    if (s < T) {
+      const Tile t = tile(s);
+      rows = t.rows; seg_pages = pages[t.group];
+    } else {
+      rows = c.heads; seg_pages = held_pages(s - T) - (shares ? pages[last_up_to(start, groups, s - T)] : 0);
+    }
+    part0[s] = seg_pages;                        // for now
+    cost[rows <= AS_ROWS] += cost_of(seg_pages, rows <= AS_ROWS);
   }
   plan_scan(cost, all_cost, waves);
   const float wide_work = AS_WIDE_WEIGHT * all_cost[0];
@@ -249,37 +258,38 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
   };
   const Line lines[2] = {line(all_cost[0], wide, AS_WIDE_START, AS_WIDE_LEAST, 4), line(all_cost[1], narrow, AS_NARROW_START, AS_NARROW_LEAST, 2)};
   int sums[2] = {0, 0}, all[2], at[2] = {cost[0], cost[1]};        // items (narrow ones in the upper half), partial rows
+  int pieces = 0;                                // of the thread's last segment
   for (int s = s0; s < s1; s++) {
-    const Segment x = get(s);
-    const int kind = is_narrow(x);
-    int first, count;
-    lines[kind].cut(at[kind], x.pages, &first, &count);
-    at[kind] += cost_of(x);
-    sums[0] += kind ? count << 16 : count;
-    sums[1] += count * x.rows;
+    if (per > 1) rows = rows_of(s);
+    const int kind = rows <= AS_ROWS;
+    pieces = lines[kind].pieces(at[kind], part0[s]);
+    at[kind] += cost_of(part0[s], kind);
+    sums[0] += kind ? pieces << 16 : pieces;
+    sums[1] += pieces * rows;
   }
   plan_scan(sums, all, waves);
   at[0] = cost[0]; at[1] = cost[1];
   for (int s = s0; s < s1; s++) {
-    const Segment x = get(s);
-    const int kind = is_narrow(x);
-    int first, count;
-    lines[kind].cut(at[kind], x.pages, &first, &count);
+    if (per > 1) rows = rows_of(s);
+    const int kind = rows <= AS_ROWS, seg_pages = part0[s];
+    if (per > 1) pieces = lines[kind].pieces(at[kind], seg_pages);
     if (s < T) wide_at[s] = at[0];
     narrow_at[s] = at[1];
     item0[s] = (unsigned short)(kind ? (all[0] & 0xFFFF) + (sums[0] >> 16) : sums[0] & 0xFFFF);      // wide ones first
     part0[s] = sums[1];
     if (s >= T) {
-      Parts* p = c.plan.parts + x.request;
-      p->s_part = sums[1]; p->s_count = count; p->len = x.len; p->done = count == 1 && x.pg0 == 0;
-      if (x.pg0 == 0) p->p_count = 0;
+      const int r = s - T;
+      const bool alone = seg_pages == held_pages(r);              // shares nothing
+      Parts* p = c.plan.parts + r;
+      p->s_part = sums[1]; p->s_count = pieces; p->len = lens[r]; p->done = pieces == 1 && alone;
+      if (alone) p->p_count = 0;
     } else {
-      Parts* p = c.plan.parts + x.row0 / c.heads;
-      for (int i = 0; i < x.rows; i += c.heads, p++) { p->p_part = sums[1] + i; p->p_step = x.rows; p->p_count = count; }
+      Parts* p = c.plan.parts + tile(s).request;
+      for (int i = 0; i < rows; i += c.heads, p++) { p->p_part = sums[1] + i; p->p_step = rows; p->p_count = pieces; }
     }
-    at[kind] += cost_of(x);
-    sums[0] += kind ? count << 16 : count;
-    sums[1] += count * x.rows;
+    at[kind] += cost_of(seg_pages, kind);
+    sums[0] += kind ? pieces << 16 : pieces;
+    sums[1] += pieces * rows;
   }
   if (tid == 0) { wide_at[T] = all_cost[0]; narrow_at[segments] = all_cost[1]; }
   __syncthreads();
@@ -287,18 +297,24 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
   for (int i = tid; i < wide + narrow; i += AS_PLAN_THREADS) {
     const int kind = i >= wide, k = kind ? i - wide : i, *places = kind ? narrow_at : wide_at, count_of = kind ? segments : T;
     const Line& l = lines[kind];
+    const int begin = k * l.share, end = begin + l.share;
     Range r{};
-    if ((long long)k * l.share < all_cost[kind]) {
-      for (int s = last_up_to(places, count_of, k * l.share); s < count_of && places[s] < (k + 1) * l.share; s++) {
-        if (places[s + 1] == places[s]) continue;                 // of the other kind, or without pages
-        const Segment x = segment(s);
-        int first, count;
-        l.cut(places[s], x.pages, &first, &count);
-        if (k < first || k >= first + count) continue;
-        const int from = k == first ? 0 : l.up_to(places[s], x.pages, k - 1), to = k == first + count - 1 ? x.pages : l.up_to(places[s], x.pages, k);
-        const int item = item0[s] + k - first;
-        const bool done = s >= T && x.pg0 == 0 && count == 1;     // a request without a shared part whose pages are all here
-        const Item it{x.row0, x.rows, x.request, x.pg0 + from, x.pg0 + to, x.len, done ? -1 : part0[s] + (k - first) * x.rows, s >= T};
+    if (begin < all_cost[kind]) {
+      for (int s = last_up_to(places, count_of, begin), from_at = places[s], to_at; s < count_of && from_at < end; s++, from_at = to_at) {
+        to_at = places[s + 1];
+        const int seg_pages = to_at - from_at - l.start;          // no more than 0: of the other kind, or without pages
+        const int from = begin > from_at ? l.up_to(from_at, seg_pages, k - 1) : 0, to = l.up_to(from_at, seg_pages, k);
+        if (from >= to) continue;
+        const int piece = from == 0 ? 0 : k - l.first(from_at, seg_pages), item = item0[s] + piece;
+        Item it;
+        if (s < T) {
+          const Tile t = tile(s);
+          it = Item{t.request * c.heads, t.rows, start[t.group], from, to, seg_pages * OP_PAGE, part0[s] + piece * t.rows, 0};
+        } else {
+          const int q = s - T, held = held_pages(q), pg0 = held - seg_pages;
+          const bool done = pg0 == 0 && to - from == held;        // a request without a shared part whose pages are all here
+          it = Item{q * c.heads, c.heads, q, pg0 + from, pg0 + to, lens[q], done ? -1 : part0[s] + piece * c.heads, 1};
+        }
         if (r.end == 0) {
           r.first = it;
           r.next = item + 1;
@@ -889,7 +905,8 @@ extern "C" int sts_op_attn_shared_plan(const sts_attn_batch* b, void* stream) {
   OnStreamDevice dev(s);
   if (dev.error() != hipSuccess) return op_result(dev.error());
   const int n = b->n_requests, slots = slots_of(b->n_kv);
-  const PlanCall c{sizes_tag(*b), n, b->n_groups, b->n_q / b->n_kv, slots, b->max_pages, b->lens, b->group_starts, b->shared_lens, plan};
+  const int heads = b->n_q / b->n_kv, wide_requests = AS_TILE / heads;
+  const PlanCall c{sizes_tag(*b), n, b->n_groups, heads, slots, b->max_pages, wide_requests, ((1u << 20) + wide_requests - 1) / wide_requests, b->lens, b->group_starts, b->shared_lens, plan};
   return op_result(launch(attn_shared_plan_kernel, dim3(1), dim3(AS_PLAN_THREADS), 0, s, c));
 }
 
