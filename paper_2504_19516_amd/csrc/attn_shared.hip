@@ -17,9 +17,9 @@
 // shares, one for each workgroup or wave: a long context is shared by many, short ones are strung together.
 //
 // Measured, bf16, 32 query and 8 KV heads of 128; us of the plan (once a step), and of products and join (each layer):
-//   8 requests on 1031 shared tokens, 6 MB of pages a layer     9    8   4    latency
-//   64 requests on 2048 shared tokens, 100 MB                   10   23   5    4.3 TB/s in the products: memory
-//   256 requests on a document of 8192 tokens, 187 MB           14   72   9    2.6 TB/s and 0.49 PFLOP/s at once: matrix cores and exponentials
+//   8 requests on 1031 shared tokens, 6 MB of pages a layer     7    8   4    latency
+//   64 requests on 2048 shared tokens, 100 MB                    8   23   5    4.3 TB/s in the products: memory
+//   256 requests on a document of 8192 tokens, 187 MB           11   72   9    2.6 TB/s and 0.49 PFLOP/s at once: matrix cores and exponentials
 // (read by every request for itself, the document alone would be 8.6 GB a layer).
 #include <algorithm>
 
