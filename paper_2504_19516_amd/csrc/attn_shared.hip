@@ -39,7 +39,7 @@ constexpr int AS_JOIN_ROWS = 1024;
 // workgroup, in pages of a narrow one. Steps of 40 requests on 1000 tokens / 96 in four groups on 4096 / 256 on one document (two layers):
 // 15.3 / 50.9 / 168 us as here; wide start and least share of 16 and 8 pages 18.8 / 48.8 / 166; wide weight 1: 15.0 / 51.6 / 173, 1.6: 15.0 / 50.9 /
 // 163; narrow least share of 2: 15.9 / 50.0 / 170, 8: 17.2 / 48.1 / 172 (a single request of 8192 tokens 15.6, 14.7 and 14.1 with 2, 4 and 8;
-// 8 requests on 1000 tokens, four layers, 53.7, 56.3 and 61.6).
+// 8 requests on 1000 tokens, four layers, 53.7, 56.3 and 61.6); all beside a plan of 2 us more than now's.
 constexpr int AS_WIDE_START = 8, AS_NARROW_START = 2, AS_WIDE_LEAST = 4, AS_NARROW_LEAST = 4;
 constexpr float AS_WIDE_WEIGHT = 1.25f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
