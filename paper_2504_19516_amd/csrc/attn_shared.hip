@@ -18,7 +18,7 @@
 //
 // Measured, bf16, 32 query and 8 KV heads of 128; us of the plan (once a step), and of products and join (each layer):
 //   8 requests on 1031 shared tokens, 6 MB of pages a layer     7    8   4    latency
-//   64 requests on 2048 shared tokens, 100 MB                    8   23   5    4.3 TB/s in the products: memory
+//   64 requests on 2048 shared tokens, 100 MB                    8   22   4    4.5 TB/s in the products: memory
 //   256 requests on a document of 8192 tokens, 187 MB           11   72   9    2.6 TB/s and 0.49 PFLOP/s at once: matrix cores and exponentials
 // (read by every request for itself, the document alone would be 8.6 GB a layer).
 #include <algorithm>
@@ -40,7 +40,10 @@ constexpr int AS_JOIN_ROWS = 1024;
 // 15.3 / 50.9 / 168 us as here; wide start and least share of 16 and 8 pages 18.8 / 48.8 / 166; wide weight 1: 15.0 / 51.6 / 173, 1.6: 15.0 / 50.9 /
 // 163; narrow least share of 2: 15.9 / 50.0 / 170, 8: 17.2 / 48.1 / 172 (a single request of 8192 tokens 15.6, 14.7 and 14.1 with 2, 4 and 8;
 // 8 requests on 1000 tokens, four layers, 53.7, 56.3 and 61.6); all beside a plan of 2 us more than now's.
-constexpr int AS_WIDE_START = 8, AS_NARROW_START = 2, AS_WIDE_LEAST = 4, AS_NARROW_LEAST = 4;
+// Narrow segments that cost AS_LONG pages each in the mean are not cut below AS_LONG_LEAST once there are AS_LONG_SHARE of them for every wave: fewer
+// partial results and joins for a longer way of each wave. 64 requests on 2048 tokens (four layers) 124 -> 116 us, the larger shape's groups (two) 66.5 ->
+// 60.7, 8 requests of 2000 tokens 19.6 -> 18.9; with 12 pages 122 and 63. Where waves have less to do, it is slower: 2 requests of 3000 tokens 11.5 -> 13.9.
+constexpr int AS_WIDE_START = 8, AS_NARROW_START = 2, AS_WIDE_LEAST = 4, AS_NARROW_LEAST = 4, AS_LONG = 16, AS_LONG_SHARE = 3, AS_LONG_LEAST = 8;
 constexpr float AS_WIDE_WEIGHT = 1.25f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -256,7 +259,8 @@ __global__ void __launch_bounds__(AS_PLAN_THREADS) attn_shared_plan_kernel(PlanC
     const int share = max((total + max(count, 1) - 1) / max(count, 1), start + least);
     return Line{share, start, granule, 1.f / (float)share};
   };
-  const Line lines[2] = {line(all_cost[0], wide, AS_WIDE_START, AS_WIDE_LEAST, 4), line(all_cost[1], narrow, AS_NARROW_START, AS_NARROW_LEAST, 2)};
+  const int narrow_least = all_cost[1] < AS_LONG * segments || all_cost[1] < AS_LONG_SHARE * narrow ? AS_NARROW_LEAST : AS_LONG_LEAST;
+  const Line lines[2] = {line(all_cost[0], wide, AS_WIDE_START, AS_WIDE_LEAST, 4), line(all_cost[1], narrow, AS_NARROW_START, narrow_least, 2)};
   int sums[2] = {0, 0}, all[2], at[2] = {cost[0], cost[1]};        // items (narrow ones in the upper half), partial rows
   int pieces = 0;                                // of the thread's last segment
   for (int s = s0; s < s1; s++) {
