@@ -9,16 +9,17 @@
 // would leave fp32's range there: it takes y = x - m, which is 0 or below -2^77. Every lane keeps its own running maximum, sum and weighted
 // sum, and they meet once at the end. A row is cut into parts (one workgroup each) when there are few rows; a second kernel joins the parts.
 //
-// Top k: while the row streams by, each lane only notes the largest element of every group of its own (32 elements or more) in LDS. The lanes'
-// largest are different elements, so the k-th largest of them bounds the k-th best from below; few groups reach the bound (some k), and
-// their elements are read again, compared with it, and sorted by compare-exchanges between lanes. Where more elements reach the bound than
-// the buffer holds (rows of equal values), the waves go through the part again, each with a sorted list of its 64 best, and compare value and
-// index with its k-th.
+// Top k: while the row streams by, each lane only notes the largest element of every group of its own (32 elements or more) in LDS. The largest
+// of the four waves' lanes i, for each i, are 64 different elements, so the k-th largest of them bounds the k-th best from below (of all 256
+// lanes it bounded it a little better, and took more time than that saved: one row 13.1 us for 12.4, 1000 rows of 4000 10.7 for 9.7). Few groups
+// reach the bound (some k), and their elements are read again, compared with it, and sorted by compare-exchanges between lanes. Where more
+// elements reach the bound than the buffer holds (rows of equal values), the waves go through the part again, each with a sorted list of its 64
+// best, and compare value and index with its k-th.
 //
-// Bound by memory: 2048 rows of 128256 bf16 logits take 103 us with one alternative (5.1 TB/s), 117 with 20. One row of fp32 takes 9 us and 5
+// Bound by memory: 2048 rows of 128256 bf16 logits take 103 us with one alternative (5.1 TB/s), 112 with 20. One row of fp32 takes 8 us and 4.5
 // for the join of its 16 parts: one batch a wave, then latencies (the bound, the groups read again, the sort) and the fetch of code that runs
-// once: with the elements before and behind the aligned vectors handled in every load instead of by one lane each, it took 11 us, and 2048 rows
-// 114. The form that tested every element as it came, with a buffer of candidates in the loop, took 140 us with one alternative, 230 with 20.
+// once: with the elements before and behind the aligned vectors handled in every load instead of by one lane each, it took 2 us more, and 2048
+// rows 11. The form that tested every element as it came, with a buffer of candidates in the loop, took 140 us with one alternative, 230 with 20.
 #include <algorithm>
 
 #include "device_ops.h"
@@ -327,17 +328,16 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
   if constexpr (TOP) {
     first.lane_maxima[tid] = lane_max;
     __syncthreads();
-    // the k-th largest of the lanes' maxima, its upper 16 bits; none where fewer than k lanes have seen anything above -inf
-    unsigned keys[LP_WAVES], kth = 0;
+    // the k-th largest of the 64, its upper 16 bits; none where fewer than k have seen anything above -inf
+    float largest = first.lane_maxima[lane];
 #pragma unroll
-    for (int w = 0; w < LP_WAVES; w++) keys[w] = value_key(first.lane_maxima[w * 64 + lane]);
+    for (int w = 1; w < LP_WAVES; w++) largest = fmaxf(largest, first.lane_maxima[w * 64 + lane]);
+    const unsigned key = value_key(largest);
+    unsigned kth = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; bit--) {
       const unsigned cand = kth | 1u << bit;
-      int n = 0;
-#pragma unroll
-      for (int w = 0; w < LP_WAVES; w++) n += __popcll(__ballot(keys[w] >= cand));
-      if (n >= k) kth = cand;
+      if (__popcll(__ballot(key >= cand)) >= k) kth = cand;
     }
     const bool open = kth <= value_key(-INFINITY);
     float bound = open ? -INFINITY : below(key_value(kth));
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(LogprobsCall 
 }
 
 // Parts of a row: enough workgroups for four per CU, none shorter than a batch of each of its waves. Wanting 512 / 1024 / 2048 workgroups, 64
-// rows of 128256 fp32 logits with 5 alternatives took 19.7 / 16.8 / 17.0 us, 200 rows 41.7 / 34.4 / 43.6 (with the join 5 us more each).
+// rows of 128256 fp32 logits with 5 alternatives took 16.9 / 17.7 / 17.7 us, 200 rows 30.4 / 29.1 / 30.7, the join among them.
 int logprob_parts(int rows, int vocab) {
   constexpr int batch = LP_WAVES * 64 * LP_ELEMS;
   return std::max(1, std::min({(vocab + batch - 1) / batch, (LP_WORKGROUPS + rows - 1) / rows, LP_MAX_PARTS}));
