@@ -202,8 +202,8 @@ int sts_read_hidden(sts_ctx* ctx, int32_t phase, float* out, int32_t rows);
  * any (a prefill's last slice that asked for logits: a row a sequence; a decode step that asked for logits or tokens: a row a request): the
  * first `rows` of them, with a token each. sts_op_logprobs on logits that are still on the device; its description says what the outputs are
  * where a row has nothing, NaN or infinities, and what a token out of range gives. Outputs [rows] and [rows, top_k] may each be NULL; tokens may be
- * NULL if logprob and rank are. STS_EINVAL if the call left fewer rows, STS_ESTATE while a launch of the phase is outstanding or its
- * partition is empty. */
+ * NULL if logprob and rank are. STS_EINVAL if the call left fewer rows (a step that failed leaves none in the
+ * phases that it was to run), STS_ESTATE while a launch of the phase is outstanding or its partition is empty. */
 int sts_read_logprobs(sts_ctx* ctx, int32_t phase, const int32_t* tokens, int32_t rows, int32_t top_k, float* logprob, float* entropy, int32_t* rank,
                       float* top_logprob, int32_t* top_token);
 

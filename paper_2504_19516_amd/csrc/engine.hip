@@ -78,8 +78,9 @@ struct Phase {
   int* h_tokens = nullptr; int* h_pos = nullptr; int* h_place = nullptr; int* h_bt = nullptr; int* h_rows = nullptr;
   PrefillSeq* h_pseq = nullptr; DecodeSeq* h_dseq = nullptr; AttnItem* h_items = nullptr; DecodeItem* h_ditems = nullptr;
   float* h_logits = nullptr; ArgBest* h_best = nullptr;
-  // the last call's logits (device or pinned memory), none: head_rows 0; what sts_read_logprobs keeps, made by its first call
-  const float* head_at = nullptr; int head_rows = 0;
+  // the last finished call's logits (device or pinned memory), none: head_rows 0, and the rows that the call in flight will leave; what
+  // sts_read_logprobs keeps, made by its first call
+  const float* head_at = nullptr; int head_rows = 0, head_queued = 0;
   unsigned char* h_lp = nullptr; unsigned char* lp_ws = nullptr;
   int rows = 0;                               // rows of the last call
   bool alone = false;                         // neither queued together with the other phase nor while a launched step of it was in flight (blocking calls of two threads do not see each other)
@@ -526,10 +527,11 @@ bool valid_seq(sts_ctx* c, int s) { return s >= 0 && s < (int)c->seqs.size() && 
 
 // Make `seq` own enough pages for n_tokens; caller holds no lock.
 // After a failure between the launches of a step: waits for those already queued, whose metadata the next call rewrites, and
-// forgets their timing events and those of the step (a beginning without an end).
+// forgets their timing events and those of the step (a beginning without an end), and its logits.
 void drop_queued(Phase& ph) {
   if (ph.stream) (void)wait_stream(ph.stream);
   ph.kkind.clear(); ph.kused = 0; ph.ran = false;
+  ph.head_rows = ph.head_queued = 0;
 }
 
 int reserve_pages(sts_ctx* c, const std::vector<std::pair<int, int>>& wants) {   // (seq, tokens)
@@ -734,6 +736,7 @@ int prefill_finish(sts_ctx* c, int n_seqs, const int32_t* seqs, const int32_t* l
   Phase& ph = c->ph[0];
   HIPCK(wait_stream(ph.stream));
   STSCK(k_collect(c, ph));
+  ph.head_rows = ph.head_queued;
   c->pf_next_layer = le;
   if (le == c->d.n_layers) {
     for (int i = 0; i < n_seqs; i++) c->seqs[seqs[i]].len += lens[i];
@@ -829,7 +832,7 @@ int decode_launch_checked(sts_ctx* c, const int32_t* seqs, const int32_t* in_tok
 
 int DecodeRun::begin() {
   Phase& ph = c->ph[1];
-  ph.head_rows = 0;
+  ph.head_rows = ph.head_queued = 0;
   const sts_model_desc& d = c->d;
   const int mp = c->p.max_pages_per_seq, pt = c->geo.page_tokens;
   ph.meta_used = 0;
@@ -921,7 +924,7 @@ int DecodeRun::end() {
     ph.head_at = direct ? ph.h_logits : ph.logits;
   }
   HIPCK(hipEventRecord(ph.ev1, st));
-  ph.ran = true; ph.rows = n; ph.head_rows = want_logits || want_next ? n : 0;
+  ph.ran = true; ph.rows = n; ph.head_queued = want_logits || want_next ? n : 0;
   return STS_OK;
 }
 
@@ -972,7 +975,7 @@ bool prefill_few_rows(sts_ctx* c, Phase& ph, int rows, const PrefillGemm (&tiles
 int prefill_launch_body(sts_ctx* c, int n_seqs, const int32_t* seqs, const int32_t* lens, const int32_t* tokens,
                         int lb, int le, bool want_logits, DecodeRun* beside) {
   Phase& ph = c->ph[0];
-  ph.head_rows = 0;
+  ph.head_rows = ph.head_queued = 0;
   const sts_model_desc& d = c->d;
   int rows = 0;
   for (int i = 0; i < n_seqs; i++) rows += lens[i];
@@ -1069,7 +1072,7 @@ int prefill_launch_body(sts_ctx* c, int n_seqs, const int32_t* seqs, const int32
     ph.head_at = direct ? ph.h_logits : ph.logits;
   }
   HIPCK(hipEventRecord(ph.ev1, st));
-  ph.ran = true; ph.rows = rows; ph.head_rows = le == d.n_layers && want_logits ? n_seqs : 0;
+  ph.ran = true; ph.rows = rows; ph.head_queued = le == d.n_layers && want_logits ? n_seqs : 0;
   return STS_OK;
 }
 
@@ -1077,6 +1080,7 @@ int decode_finish(sts_ctx* c, const int32_t* seqs, int n, float* logits, int32_t
   Phase& ph = c->ph[1];
   HIPCK(wait_stream(ph.stream));
   STSCK(k_collect(c, ph));
+  ph.head_rows = ph.head_queued;
   for (int i = 0; i < n; i++) c->seqs[seqs[i]].len += 1;
   if (logits) std::memcpy(logits, ph.h_logits, (size_t)n * c->d.vocab * sizeof(float));
   for (int i = 0, parts = argmax_parts(n, c->d.vocab); next && i < n; i++) {

@@ -895,6 +895,56 @@ def test_engine_reads_log_probabilities_of_both_phases_of_a_step(sts, engine):
         e.seq_free(s)
 
 
+@pytest.mark.parametrize("phase,after", [(1, 0), (1, 9), (0, 0), (0, 9)])
+def test_engine_has_no_log_probabilities_of_a_failed_step(sts, engine, phase, after):
+    """A launch of either phase fails: neither phase has logits then, though the other one's may be queued to its end; the next step's are read as ever. A refused call
+    changes nothing."""
+    from paper_2504_19516_amd import synth
+    e, desc = engine
+    seqs = [e.seq_create() for _ in range(5)]
+    prompts = [synth.tokens(80 + i, 7 + i, desc.vocab) for i in range(5)]
+
+    def check(p, logits):
+        tokens = np.arange(len(logits)) * 7 + 3
+        got, want = e.read_logprobs(p, tokens, 3), logprobs_reference(logits.astype(np.float64), tokens, 3)
+        check_logprobs(dict(got, lse=want["lse"].astype(np.float32)), want, desc.vocab)
+
+    def none(p):
+        with pytest.raises(sts.StsError) as x:
+            e.read_logprobs(p, [1])
+        assert x.value.code == sts.EINVAL
+    check(0, e.prefill_batch(seqs[2:], prompts[2:]))
+    first = e.decode_step(seqs[2:], [3, 4, 5])[0]
+    check(1, first)
+    step = lambda: e.step_concurrent(seqs[:2], prompts[:2], 0, desc.n_layers, seqs[2:], [6, 7, 8])  # noqa: E731
+    e.fail_launch(phase, after)
+    with pytest.raises(sts.StsError) as x:
+        step()
+    assert x.value.code == sts.EHIP
+    none(0), none(1)
+    plog, dlog, _ = step()
+    check(0, plog), check(1, dlog)
+    # a phase by itself: the other keeps its own
+    e.fail_launch(phase, 2)
+    with pytest.raises(sts.StsError):
+        e.prefill_append(seqs[0], prompts[0]) if phase == 0 else e.decode_step(seqs[2:], [1, 2, 3])
+    none(phase)
+    check(1 - phase, dlog if phase == 0 else plog)
+    # launched and finished; logits only once it is finished; a call that is refused leaves them
+    if phase == 0:
+        e.prefill_launch(seqs[:1], prompts[:1], 0, desc.n_layers, True)
+        logits = e.prefill_finish(1, True)
+    else:
+        e.decode_launch(seqs[2:], [1, 2, 3], want_logits=True)
+        logits, _ = e.decode_finish(3, True)
+    check(phase, logits)
+    with pytest.raises(sts.StsError):
+        e.prefill_append(seqs[0], [desc.vocab]) if phase == 0 else e.decode_step(seqs[2:], [1, 2, desc.vocab])
+    check(phase, logits)
+    for s in seqs:
+        e.seq_free(s)
+
+
 def test_engine_takes_scaled_rotations(sts, engine):
     """K of a prompt as the engine caches it: the plain rotation's bits come back with the plain description; scaled ones are the plain K turned on by the difference of the
     angles (both rounded to bf16 once: 2 half steps of the size of the pair)."""
