@@ -78,10 +78,10 @@ struct Phase {
   int* h_tokens = nullptr; int* h_pos = nullptr; int* h_place = nullptr; int* h_bt = nullptr; int* h_rows = nullptr;
   PrefillSeq* h_pseq = nullptr; DecodeSeq* h_dseq = nullptr; AttnItem* h_items = nullptr; DecodeItem* h_ditems = nullptr;
   float* h_logits = nullptr; ArgBest* h_best = nullptr;
-  // the last finished call's logits (device or pinned memory), none: head_rows 0, and the rows that the call in flight will leave; what
-  // sts_read_logprobs keeps, made by its first call
+  // the last finished call's logits (device or pinned memory), none: head_rows 0, and the rows that the call in flight will leave;
+  // sts_read_logprobs' tokens and results (pinned) and its workspace
   const float* head_at = nullptr; int head_rows = 0, head_queued = 0;
-  unsigned char* h_lp = nullptr; unsigned char* lp_ws = nullptr;
+  unsigned char* h_lp = nullptr; unsigned char* lp_ws = nullptr; int64_t lp_ws_bytes = 0;
   int rows = 0;                               // rows of the last call
   bool alone = false;                         // neither queued together with the other phase nor while a launched step of it was in flight (blocking calls of two threads do not see each other)
   // per-kernel timing
@@ -1124,6 +1124,10 @@ int alloc_phase(sts_ctx* c, int side) {
     STSCK(host_alloc(&ph.h_meta, ph.meta_bytes + 16));
   }
   STSCK(host_alloc(&ph.h_logits, nseq * d.vocab));
+  // fewer rows are cut into more parts: the largest workspace need not be that of the most rows
+  for (int32_t r = 1; r <= (int32_t)nseq; r++) ph.lp_ws_bytes = std::max(ph.lp_ws_bytes, sts_op_logprobs_workspace(STS_F32, r, d.vocab, std::min(32, d.vocab)));
+  STSCK(dev_alloc(c, &ph.lp_ws, (size_t)ph.lp_ws_bytes));
+  STSCK(host_alloc(&ph.h_lp, nseq * (4 + 64) * sizeof(int32_t)));
   if (side == 0) {
     STSCK(dev_alloc(c, &ph.QKV, rows * c->qkvn));
     const size_t tail_floats = (size_t)c->n_cu * 256 * 256;   // one wave of partial tiles at the largest tile on every CU
@@ -1660,21 +1664,14 @@ extern "C" int sts_read_logprobs(sts_ctx* c, int32_t phase, const int32_t* token
   if (rows > ph.head_rows) return STS_EINVAL;
   // tokens and outputs in pinned memory, which the kernels read and write themselves: token, three figures a row, top_k pairs
   const int32_t most = phase == 0 ? c->p.max_prefill_seqs : c->p.max_decode_batch;
-  int64_t ws_bytes = 0;
-  for (int32_t r = 1; r <= most; r++) ws_bytes = std::max(ws_bytes, sts_op_logprobs_workspace(STS_F32, r, c->d.vocab, std::min(32, c->d.vocab)));
   OnStreamDevice dev(ph.stream);
   if (dev.error() != hipSuccess) return op_result(dev.error());
-  if (!ph.h_lp) {
-    std::lock_guard<std::mutex> g(c->alloc_mu);              // the other phase's control thread may be here too
-    if (!ph.lp_ws) STSCK(dev_alloc(c, &ph.lp_ws, (size_t)ws_bytes));
-    STSCK(host_alloc(&ph.h_lp, (size_t)most * (4 + 64) * sizeof(int32_t)));
-  }
   int32_t* tok = reinterpret_cast<int32_t*>(ph.h_lp);
   float *lp = reinterpret_cast<float*>(tok + most), *ent = lp + most, *top_lp = ent + 2 * most;
   int32_t *rk = reinterpret_cast<int32_t*>(ent + most), *top_tok = reinterpret_cast<int32_t*>(top_lp + (size_t)most * 32);
   if (tokens) std::memcpy(tok, tokens, rows * sizeof(int32_t));
   const sts_logprobs a{STS_F32, rows, c->d.vocab, top_k, c->d.vocab, ph.head_at, tokens ? tok : nullptr, logprob ? lp : nullptr, ent, nullptr, rank ? rk : nullptr,
-                       top_logprob ? top_lp : nullptr, top_token ? top_tok : nullptr, ph.lp_ws, ws_bytes};
+                       top_logprob ? top_lp : nullptr, top_token ? top_tok : nullptr, ph.lp_ws, ph.lp_ws_bytes};
   STSCK(sts_op_logprobs(&a, ph.stream));
   HIPCK(wait_stream(ph.stream));
   auto give = [&](void* to, const void* from, size_t n) { if (to) std::memcpy(to, from, n * sizeof(int32_t)); };

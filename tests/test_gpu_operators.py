@@ -945,6 +945,35 @@ def test_engine_has_no_log_probabilities_of_a_failed_step(sts, engine, phase, af
         e.seq_free(s)
 
 
+def test_engine_reads_log_probabilities_without_allocating(sts, engine):
+    """Everything is allocated by sts_init: a ctx's first call of either phase maps no memory of the GPU driver's (pinned host memory is such a mapping), though
+    it is one of as many rows and alternatives as there can be."""
+    from paper_2504_19516_amd import synth
+    first, desc = engine
+    s = first.seq_create()
+    first.prefill_append(s, [1, 2, 3])
+    first.read_logprobs(0, [1], 32)                        # the kernels' code has been loaded
+    first.seq_free(s)
+
+    def mapped():
+        return sorted(x.split()[0] for x in open("/proc/self/maps") if "/dev/dri" in x or "/dev/kfd" in x)
+    e = sts.Engine(desc, weight_seed=5, kv_pool_pages=300, max_prefill_tokens=256, max_prefill_seqs=40, max_decode_batch=300, max_seqs=300, max_pages_per_seq=4)
+    seqs = [e.seq_create() for _ in range(300)]
+    assert mapped()
+    for i in range(0, 300, 40):
+        part = seqs[i:i + 40]
+        logits = e.prefill_batch(part, [synth.tokens(i + j, 3, desc.vocab) for j in range(len(part))])
+        if i == 0:
+            before = mapped()
+            got = e.read_logprobs(0, logits.argmax(1), 32)
+            assert mapped() == before and (got["rank"] == 0).all()
+    _, nxt = e.decode_step(seqs, np.arange(300), want_logits=False)
+    before = mapped()
+    got = e.read_logprobs(1, nxt, 32)
+    assert mapped() == before and (got["rank"] == 0).all()
+    e.close()
+
+
 def test_engine_takes_scaled_rotations(sts, engine):
     """K of a prompt as the engine caches it: the plain rotation's bits come back with the plain description; scaled ones are the plain K turned on by the difference of the
     angles (both rounded to bf16 once: 2 half steps of the size of the pair)."""
