@@ -44,7 +44,7 @@ constexpr int AS_JOIN_ROWS = 1024;
 // partial results and joins for a longer way of each wave. 64 requests on 2048 tokens (four layers) 124 -> 116 us, the larger shape's groups (two) 66.5 ->
 // 60.7, 8 requests of 2000 tokens 19.6 -> 18.9; with 12 pages 122 and 63. Where waves have less to do, it is slower: 2 requests of 3000 tokens 11.5 -> 13.9.
 constexpr int AS_WIDE_START = 8, AS_NARROW_START = 2, AS_WIDE_LEAST = 4, AS_NARROW_LEAST = 4, AS_LONG = 16, AS_LONG_SHARE = 3, AS_LONG_LEAST = 8;
-constexpr float AS_WIDE_WEIGHT = 1.25f;
+constexpr float AS_WIDE_WEIGHT = 1.25f, AS_RISE = 8.f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // A piece of a segment: rows row0 .. row0 + rows - 1 (request * heads of a group + head) over the pages [pg0, pg1) of a request's
@@ -359,6 +359,35 @@ struct AttnCall {
   Plan plan;
 };
 
+// Eight probabilities for the second product, each in two numbers of the type: p without what the type drops, and p (1 + e) less that, which is above 0
+// wherever p is, so that a V of infinity gives infinity and not inf - inf or 0 * inf (fp16: from p = 2^-16 on). With u for half a step of the type (bf16
+// 2^-8, fp16 2^-11) their sum is within 2 u (2 u + e) of p (1 + e), fp16's smallest within 2^-24; what reads the sums takes the factor out, and the
+// output is rounded once, at the end: as far from 64 bits as that leaves any output. One number each, for half the second products, left outputs 1.04 to 1.11
+// times as far and took, us a pass then / now: 8 requests on 1031 tokens (four layers) 54.9 / 56.0, 64 on 2048 (four) 116 / 119, 256 on 8192 (two) 164 / 186, the larger
+// shape's groups (two) 61 / 63.
+constexpr float AS_EXTRA = 1.f / 512;            // e
+__device__ __forceinline__ void in_two(const f32x16& p, int at, bf16x8& first, bf16x8& rest) {
+  u32x4 f;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const unsigned a = __float_as_uint(p[at + e]), b = __float_as_uint(p[at + e + 1]);
+    f[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302);              // the upper halves
+    rest[e] = (bf16)fmaf(p[at + e], 1.f + AS_EXTRA, -__uint_as_float(a & 0xFFFF0000u));
+    rest[e + 1] = (bf16)fmaf(p[at + e + 1], 1.f + AS_EXTRA, -__uint_as_float(b & 0xFFFF0000u));
+  }
+  first = __builtin_bit_cast(bf16x8, f);
+}
+__device__ __forceinline__ void in_two(const f32x16& p, int at, f16x8& first, f16x8& rest) {
+  typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const f16x2 f = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(p[at + e], p[at + e + 1]));
+    const f16x2 r = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(fmaf(p[at + e], 1.f + AS_EXTRA, -(float)f[0]), fmaf(p[at + e + 1], 1.f + AS_EXTRA, -(float)f[1])));
+    first[e] = f[0]; first[e + 1] = f[1];
+    rest[e] = r[0]; rest[e + 1] = r[1];
+  }
+}
+
 __device__ __forceinline__ float half_swap_max_f(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -514,11 +543,12 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const AttnCall<T
     l_run += rs;
 #pragma unroll
     for (int u = 0; u < 2; u++) {
-      V pb;
-#pragma unroll
-      for (int e = 0; e < 8; e++) pb[e] = (T)s[8 * u + e];
+      V pb, pr;
+      in_two(s, 8 * u, pb, pr);
 #pragma unroll
       for (int bb = 0; bb < DB; bb++) o[bb] = Mfma<T>::mul(__builtin_bit_cast(V, vr[u][bb]), pb, o[bb]);
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++) o[bb] = Mfma<T>::mul(__builtin_bit_cast(V, vr[u][bb]), pr, o[bb]);
     }
   };
   auto fence = [] { __asm__ volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); };
@@ -550,7 +580,7 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const AttnCall<T
     const float m2 = m_ref * c.scale_log2e;
     if (it.part < 0) {
       T* out = c.out + (long long)request * c.out_stride + head * D + 4 * lh;
-      const float f = 1.f / l_run;
+      const float f = 1.f / ((1.f + AS_EXTRA) * l_run);
 #pragma unroll
       for (int bb = 0; bb < DB; bb++)
 #pragma unroll
@@ -692,10 +722,9 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>&
 #pragma unroll
       for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[kb][r]);
     mx = half_swap_max_f(mx);
-    // The reference follows every new maximum: the largest probability is then 1, which the type holds exactly. Moving it only when a score
-    // outgrew it by 2^8 took 51 instead of 55 us for 256 requests on 8192 tokens, but left the outputs at 1.37 times the distance from 64 bits
-    // that rounding them once has, against 1.08.
-    if (__any(mx > m_ref)) {                                                   // wave-uniform
+    // The reference moves when a score has outgrown it by 2^8, by which probabilities and their sums may then exceed 1: two numbers of the type, and 32 bits, hold
+    // them as well there. Following every new maximum, 256 requests on 8192 tokens (two layers) took 193 instead of 186 us, with outputs as near to 64 bits.
+    if (__any((mx - m_ref) * c.scale_log2e > AS_RISE)) {                       // wave-uniform
       const float m_new = fmaxf(m_ref, mx);
       const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c.scale_log2e);
       m_ref = m_new;
@@ -723,21 +752,22 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>&
 #pragma unroll
         for (int b = 0; b < DB; b++) vf[b2][b] = *reinterpret_cast<const V*>(st + v_lane + (g + 1) * PAGE + b * 1024);
       }
-      V pb;
-#pragma unroll
-      for (int e = 0; e < 8; e++) pb[e] = (T)s[g >> 1][8 * (g & 1) + e];
+      V pb, pr;
+      in_two(s[g >> 1], 8 * (g & 1), pb, pr);
       if (decltype(whole)::value || g < here) {
 #pragma unroll
         for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pb, o[b]);
+#pragma unroll
+        for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pr, o[b]);
       }
     }
     if constexpr (decltype(whole)::value) {
 #pragma unroll
       for (int g = 0; g + 1 < 4; g++) {
         __builtin_amdgcn_sched_group_barrier(0x100, DB, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, DB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * DB, 0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, DB, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 2 * DB, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -859,7 +889,7 @@ __global__ void __launch_bounds__(256) attn_shared_join_kernel(AttnCall<T> c) {
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 v;
 #pragma unroll
-    for (int e = 0; e < 4; e++) v[e] = (T)(p.len < 0 ? NAN : none ? 0.f : o[e] / l);
+    for (int e = 0; e < 4; e++) v[e] = (T)(p.len < 0 ? NAN : none ? 0.f : o[e] / ((1.f + AS_EXTRA) * l));
     if (c.out_vec) *reinterpret_cast<T4*>(out) = v;
     else
 #pragma unroll

@@ -360,6 +360,32 @@ def small_case(rng, dtype, lens=(40, 0, 35, 16, 33, 64), groups=((3, 32), (3, 16
     return q, k, v, tables, pages, list(lens), groups
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n_q,n_kv,d,members,shared,own", [(8, 2, 64, 6, 320, 37), (8, 2, 64, 40, 320, 21), (4, 1, 128, 1, 0, 300), (8, 1, 128, 30, 640, 5)])
+def test_shared_attention_rounds_its_outputs_once(sts, dtype, n_q, n_kv, d, members, shared, own):
+    """Scores that 32 bits hold exactly (q and k of small whole numbers), so that the bound is narrow: the output's own rounding, and of the sum of |p v|
+    2 u (2 u + 2^-9) for the probabilities' two numbers of the type, the first cut off (2 u of p), the second of what is left and of 2^-9 p; 2^-22 and 2^-23 |x - m| for an
+    exponential and its argument, in numerator and denominator, and a rounding for each of the sums' tokens; fp16 holds probabilities to 2^-24 of the largest.
+    Probabilities of one number of the type would be off by u each."""
+    rng = np.random.default_rng(members + d)
+    heads, lens, groups, u = n_q // n_kv, [shared + own] * members, [(members, shared)], HALF[dtype]
+    k, v, tables, pages = attention_case(rng, groups, lens, n_kv, d)
+    v = [rounded(x, dtype) for x in v]
+    first, rest = rng.integers(-2, 3, (shared, n_kv, d)), rng.integers(-2, 3, (members, own, n_kv, d))
+    k = [np.concatenate([first, r]).astype(np.float32) for r in rest]
+    q = rng.integers(-2, 3, (members, n_q, d)).astype(np.float32)
+    pool = pool_of(k, v, tables, lens, pages, dtype, behind=np.nan)
+    with Device() as dev:
+        got, _, _, _ = run_attention(sts, dev, dtype, q, pool, tables, lens, groups, heads, scale=0.0625)
+    for r in range(members):
+        for h in range(n_q):
+            x = k[r][:, h // heads].astype(np.float64) @ q[r, h] / 16
+            w, vh = np.exp(x - x.max()), v[r][:, h // heads].astype(np.float64)
+            out, size = w @ vh / w.sum(), w @ np.abs(vh) / w.sum()
+            extra = (2 * u * (2 * u + 2.0 ** -9) + 2 * (2.0 ** -22 + 2.0 ** -23 * np.abs(x - x.max()).max()) + 2 * 2.0 ** -24 * len(x)) * size
+            near(got[r, h], out, u * np.abs(out) + extra + (2.0 ** -24 * np.abs(vh).sum(0) / w.sum() + 2.0 ** -25 if dtype == "f16" else 0.0))
+
+
 def test_shared_attention_empty_and_short_contexts(sts):
     """A context of length 0 gives zeros; a group shares what its shortest member holds."""
     rng = np.random.default_rng(5)
