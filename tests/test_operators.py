@@ -98,6 +98,13 @@ def test_logprobs_refuses(sts):
     assert sts.op_logprobs_workspace(1, 4000, 128256, 20) == 0
 
 
+def test_logprobs_refuses_vocabularies_above_the_most(sts):
+    """Of a description that nothing else is wrong with."""
+    good = dict(dtype=0, rows=2, vocab=1 << 30, top_k=5, row_stride=1 << 31, logits=A, tokens=2 * A, logprob=3 * A, workspace=9 * A, workspace_bytes=1 << 40)
+    assert sts.op_logprobs_workspace(0, 2, 1 << 30, 5) > 0 and sts.op_logprobs_workspace(0, 2, (1 << 30) + 1, 5) == -1
+    refused(sts, sts.op_logprobs, sts.Logprobs, good, vocab=(1 << 30) + 1)
+
+
 @pytest.mark.parametrize("rotary,theta", [(128, 5e5), (64, 1e4), (40, 1e6), (2, 100.0)])
 def test_rope_frequencies(sts, rotary, theta):
     i = np.arange(rotary // 2)
