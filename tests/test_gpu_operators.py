@@ -237,6 +237,14 @@ def test_rope_appends_to_pages(sts, dtype, rows, n_q, n_kv, d, rotary, interleav
     assert np.array_equal(got[:, :, :16 * d], kp.reshape(pages, n_kv, -1)) and np.array_equal(got[:, :, 16 * d:], vp.reshape(pages, n_kv, -1))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,n_q,n_kv,d,rotary,interleaved,offset", [(4500, 32, 8, 128, 128, 0, 0), (4507, 32, 8, 128, 128, 1, 0), (2049, 32, 8, 128, 104, 0, 0), (17003, 8, 8, 64, 64, 0, 0),
+                                                                      (3001, 8, 8, 64, 36, 1, 0), (9001, 6, 3, 64, 40, 0, 0), (5000, 4, 3, 64, 64, 0, 2), (8200, 8, 8, 128, 64, 0, 0)])
+def test_rope_appends_long_prefills(sts, dtype, rows, n_q, n_kv, d, rotary, interleaved, offset):
+    """Workgroups of 16 rows that go over their rotations and their heads of V more than once; vectors of eight and of four elements, and single ones; a last workgroup of a few rows."""
+    test_rope_appends_to_pages(sts, dtype, rows, n_q, n_kv, d, rotary, interleaved, offset)
+
+
 # ------------------------------------------------------------------------------------------ attention
 def attention_reference(q, k, v, lens, heads, scale, dtype):
     """Output, its bound, lse and its bound. Probabilities are rounded to the type before the product (u each, fp16's smallest ones by 2^-25), the output once; a score of
