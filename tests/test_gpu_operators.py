@@ -714,6 +714,19 @@ def test_logprobs_of_masked_and_odd_rows(sts, dtype, vocab, k, rows):
             raise AssertionError(name) from e
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab,k,pad,offset", [(1, 1100003, 32, 0, 0), (2, 1700001, 1, 1, 4), (1, 2300000, 20, 0, 0), (3, 1200007, 0, 0, 0), (1, 4400001, 5, 0, 12)])
+def test_logprobs_of_long_parts(sts, dtype, rows, vocab, k, pad, offset):
+    """Parts of a row above 65536 elements: a lane's groups hold several batches, the last one fewer."""
+    test_logprobs(sts, dtype, rows, vocab, k, pad, offset)
+
+
+@pytest.mark.parametrize("dtype,vocab,k,rows", [("bf16", 70001, 32, 52), ("f32", 70001, 1, 52), ("bf16", 128256, 1, 52), ("f16", 128256, 32, 52), ("f32", 1100001, 20, 1), ("bf16", 1500001, 32, 1)])
+def test_logprobs_of_masked_and_odd_long_rows(sts, dtype, vocab, k, rows):
+    """The same of masked rows, in parts and (1040 rows) whole."""
+    test_logprobs_of_masked_and_odd_rows(sts, dtype, vocab, k, rows)
+
+
 def test_logprobs_same_bits_again_and_in_a_graph(sts):
     rng = np.random.default_rng(1)
     x = rounded(3.0 * rng.standard_normal((5, 70001)), "bf16")
