@@ -481,6 +481,10 @@ def test_shared_attention_infinities_stay_with_their_tokens(sts):
     near(got[5][rest], o[0][rest], b[0][rest])
 
 
+# 43 requests of four heads on 11 shared pages: tiles of 128 and of 44 rows, the second of which leaves two waves without rows; the last pages are a part of a tile
+WIDE = dict(lens=tuple(176 + 1 + 5 * i % 37 for i in range(43)), groups=((43, 176),))
+
+
 def test_shared_attention_same_bits_again_and_in_a_graph(sts):
     """Nothing depends on the order in which workgroups end: the same inputs give the same bits, eagerly, on another stream and replayed."""
     rng = np.random.default_rng(11)
