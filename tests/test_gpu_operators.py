@@ -485,6 +485,68 @@ def test_shared_attention_infinities_stay_with_their_tokens(sts):
 WIDE = dict(lens=tuple(176 + 1 + 5 * i % 37 for i in range(43)), groups=((43, 176),))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_shared_attention_wide_pages_out_of_range_are_nan(sts, dtype):
+    """A bad page of the shared part, whichever wave fetches it, is the whole group's; one of a request's own its alone."""
+    q, k, v, tables, pages, lens, groups = small_case(np.random.default_rng(21), dtype, **WIDE)
+    pool = pool_of(k, v, tables, lens, pages, dtype)
+    out, bound, _, _ = attention_reference(q, k, v, lens, 4, 0.125, dtype)
+    for at, value in ((0, pages), (1, -1), (2, 2 ** 31 - 1), (3, -2 ** 31), (6, pages + 3), (8, -5), (10, pages)):
+        t = tables.copy()
+        t[0, at] = value
+        with Device() as dev:
+            got, lse, _, _ = run_attention(sts, dev, dtype, q, pool, t, lens, groups, 4)
+        assert np.isnan(got).all() and np.isnan(lse).all(), at
+    t = tables.copy()
+    t[17, 11], t[5, :11] = pages, pages                    # the shared pages are read through the first request's table
+    with Device() as dev:
+        got, lse, _, _ = run_attention(sts, dev, dtype, q, pool, t, lens, groups, 4)
+    fine = [r for r in range(43) if r != 17]
+    assert np.isnan(got[17]).all() and np.isnan(lse[17]).all()
+    near(got[fine], out[fine], bound[fine])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("q_pad,out_pad,offset", [(0, 0, 2), (3, 5, 0), (8, 1, 0), (1, 0, 2)])
+def test_shared_attention_wide_rows_at_any_element(sts, dtype, q_pad, out_pad, offset):
+    q, k, v, tables, pages, lens, groups = small_case(np.random.default_rng(22), dtype, scale=3.0, **WIDE)
+    pool = pool_of(k, v, tables, lens, pages, dtype, behind=np.nan)
+    out, bound, lse, lb = attention_reference(q, k, v, lens, 4, 0.3, dtype)
+    with Device() as dev:
+        got, got_lse, _, _ = run_attention(sts, dev, dtype, q, pool, tables, lens, groups, 4, scale=0.3, q_pad=q_pad, out_pad=out_pad, q_offset=offset)
+    near(got, out, bound)
+    near(got_lse, lse, lb)
+
+
+def test_shared_attention_wide_infinities(sts):
+    """In the shared part: scores of -inf weigh nothing, ahead of every other one and in between; a V of inf reaches every output; a score of inf or NaN is NaN for the rows that it is one of."""
+    q, k, v, tables, pages, lens, groups = small_case(np.random.default_rng(23), "bf16", **WIDE)
+    q[:] = np.abs(q) + 0.25
+    q[7, 2, 5] = np.nan
+    low = [*range(64), 70, 175]                            # the first four pages, and some
+    for r in range(43):
+        k[r][low] = -3e38
+        v[r][100, 1, 9], v[r][101, 1, 9], v[r][3, 0, 11], v[r][120, 1, 30] = np.inf, np.inf, 3e38, -np.inf
+    pool = pool_of(k, v, tables, lens, pages, "bf16")
+    with Device() as dev:
+        got, lse, _, _ = run_attention(sts, dev, "bf16", q, pool, tables, lens, groups, 4)
+        k_hot = [x.copy() for x in k]
+        for x in k_hot:
+            x[90, 1] = 3e38
+        hot, _, _, _ = run_attention(sts, dev, "bf16", q, pool_of(k_hot, v, tables, lens, pages, "bf16"), tables, lens, groups, 4)
+    assert np.isnan(got[7, 2]).all() and np.isnan(lse[7, 2])
+    nan = np.zeros((43, 8), bool)
+    nan[7, 2] = True
+    assert np.isposinf(got[:, 4:, 9][~nan[:, 4:]]).all() and np.isneginf(got[:, 4:, 30][~nan[:, 4:]]).all()
+    for r in range(43):
+        keep = [t for t in range(lens[r]) if t not in low]
+        o, b, _, _ = attention_reference(q[r:r + 1], [k[r][keep]], [np.where(np.isinf(v[r][keep]), 0, v[r][keep])], [len(keep)], 4, 0.125, "bf16")
+        check = np.broadcast_to(~nan[r][:, None], (8, 64)).copy()
+        check[4:, [9, 30]] = False
+        near(got[r][check], o[0][check], b[0][check])
+    assert np.isnan(hot[:, 4:]).all() and np.array_equal(np.isnan(hot[:, :4]).all(2), nan[:, :4])
+
+
 def test_shared_attention_same_bits_again_and_in_a_graph(sts):
     """Nothing depends on the order in which workgroups end: the same inputs give the same bits, eagerly, on another stream and replayed."""
     rng = np.random.default_rng(11)
