@@ -547,6 +547,24 @@ def test_shared_attention_wide_infinities(sts):
     assert np.isnan(hot[:, 4:]).all() and np.array_equal(np.isnan(hot[:, :4]).all(2), nan[:, :4])
 
 
+@pytest.mark.parametrize("dtype,n_q,n_kv,groups", [("bf16", 4, 2, [(2, 16)] * 2048), ("f16", 8, 1, [(4096, 48)]), ("bf16", 8, 1, [(9, 32)] * 455 + [(1, 0)]), ("f16", 2, 2, [(1, 0)] * 4096)])
+def test_shared_attention_of_the_most_requests(sts, dtype, n_q, n_kv, groups):
+    rng = np.random.default_rng(len(groups))
+    lens = [int(x) for m, s in groups for x in s + rng.choice([0, 1, 1, 2, 15, 16, 17, 33], m)]
+    assert len(lens) == 4096
+    k, v, tables, pages = attention_case(rng, groups, lens, n_kv, 64)
+    k, v = [rounded(x, dtype) for x in k], [rounded(x, dtype) for x in v]
+    q = rounded(rng.standard_normal((4096, n_q, 64)), dtype)
+    pool = pool_of(k, v, tables, lens, pages, dtype, behind=np.nan)
+    out, bound, lse, lb = attention_reference(q, k, v, lens, n_q // n_kv, 0.125, dtype)
+    with Device() as dev:
+        got, got_lse, _, _ = run_attention(sts, dev, dtype, q, pool, tables, lens, groups, n_q // n_kv)
+    some = np.asarray(lens) > 0
+    near(got, out, bound)
+    near(got_lse[some], lse[some], lb[some])
+    assert np.isneginf(got_lse[~some]).all()
+
+
 def test_shared_attention_same_bits_again_and_in_a_graph(sts):
     """Nothing depends on the order in which workgroups end: the same inputs give the same bits, eagerly, on another stream and replayed."""
     rng = np.random.default_rng(11)
