@@ -32,17 +32,19 @@ constexpr int AS_ROWS = 32;                     // rows of a narrow segment: col
 constexpr int AS_TILE = 128;                    // rows of a wide one
 constexpr int AS_SLOTS = 512;                   // workgroups of a launch: two on each CU
 constexpr int AS_PLAN_THREADS = 512;
-// Up to so many (request, head) pairs four waves join each, beyond it one: step of 16 requests on 8192 tokens (512 pairs) 21.1 us with four and
-// 22.6 with one, of 128 on 2048 (4096 pairs) 30.3 and 24.3.
+// Up to so many (request, head) pairs four waves join each, beyond it one: products and join of 16 requests on 8192 tokens (512 pairs) 22.3 us with four and
+// 23.7 with one, of 128 on 2048 (4096 pairs) 29.5 and 25.4. In between it is the parts that count, which the host does not know: 24 requests of
+// several long prompts (1536 pairs, a step of two layers) 61 and 63, 64 requests on 2048 tokens (2048 pairs, four layers) 126 and 119.
 constexpr int AS_JOIN_ROWS = 1024;
 // Start and end of a wide and of a narrow segment, and the smallest shares beyond them, in pages; what a page of a wide segment takes a
-// workgroup, in pages of a narrow one. Steps of 40 requests on 1000 tokens / 96 in four groups on 4096 / 256 on one document (two layers):
-// 15.3 / 50.9 / 168 us as here; wide start and least share of 16 and 8 pages 18.8 / 48.8 / 166; wide weight 1: 15.0 / 51.6 / 173, 1.6: 15.0 / 50.9 /
-// 163; narrow least share of 2: 15.9 / 50.0 / 170, 8: 17.2 / 48.1 / 172 (a single request of 8192 tokens 15.6, 14.7 and 14.1 with 2, 4 and 8;
-// 8 requests on 1000 tokens, four layers, 53.7, 56.3 and 61.6); all beside a plan of 2 us more than now's.
-// Narrow segments that cost AS_LONG pages each in the mean are not cut below AS_LONG_LEAST once there are AS_LONG_SHARE of them for every wave: fewer
-// partial results and joins for a longer way of each wave. 64 requests on 2048 tokens (four layers) 124 -> 116 us, the larger shape's groups (two) 66.5 ->
-// 60.7, 8 requests of 2000 tokens 19.6 -> 18.9; with 12 pages 122 and 63. Where waves have less to do, it is slower: 2 requests of 3000 tokens 11.5 -> 13.9.
+// workgroup, in pages of a narrow one. Products and join of 40 requests on 1000 tokens / of 96 in four groups on 4096 (64 heads) / a step of 256 on one document (two layers):
+// 16.2 / 58 / 187 us as here; wide start and least share of 16 and 8 pages 19.9 / 58 / 184; wide weight 1: 16.4 / 60 / 189, 1.6: 16.3 / 57 /
+// 179 (but 128 requests on 2048 tokens 27.6 for 25.4); narrow least share of 2: 17.0 / 59 / 186, 8: 19.3 / 58 / 187 (a single request of 8192 tokens 17.0, 16.5 and 16.0 with 2, 4 and 8;
+// a step of 8 requests on 1000 tokens, four layers, 54.4, 56.1 and 62.5).
+// Where the line of narrow segments costs AS_LONG pages or more for each segment of the batch (wide ones and those without pages count too) and AS_LONG_SHARE pages or more for
+// each wave, its shares are not below AS_LONG_LEAST: fewer partial results and joins for a longer way of each wave. 64 requests on 2048 tokens (four layers) 126 ->
+// 119 us, the larger shape's groups (two) 67 -> 63, 8 requests of 2000 tokens 20.0 -> 19.5; with 12 pages 123, 65 and 22.1. Where waves have less to do, it is slower: 2 requests of 3000
+// tokens 12.0 -> 14.6.
 constexpr int AS_WIDE_START = 8, AS_NARROW_START = 2, AS_WIDE_LEAST = 4, AS_NARROW_LEAST = 4, AS_LONG = 16, AS_LONG_SHARE = 3, AS_LONG_LEAST = 8;
 constexpr float AS_WIDE_WEIGHT = 1.25f, AS_RISE = 8.f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -365,15 +367,15 @@ struct AttnCall {
 // output is rounded once, at the end: as far from 64 bits as that leaves any output. One number each, for half the second products, left outputs 1.04 to 1.11
 // times as far and took, us a pass then / now: 8 requests on 1031 tokens (four layers) 54.9 / 56.0, 64 on 2048 (four) 116 / 119, 256 on 8192 (two) 164 / 186, the larger
 // shape's groups (two) 61 / 63.
-constexpr float AS_EXTRA = 1.f / 512;            // e
+template <typename T> constexpr float AS_EXTRA = std::is_same<T, f16>::value ? 0x1p-9f : 0x1p-18f;            // e: fp16's range ends soon
 __device__ __forceinline__ void in_two(const f32x16& p, int at, bf16x8& first, bf16x8& rest) {
   u32x4 f;
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const unsigned a = __float_as_uint(p[at + e]), b = __float_as_uint(p[at + e + 1]);
     f[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302);              // the upper halves
-    rest[e] = (bf16)fmaf(p[at + e], 1.f + AS_EXTRA, -__uint_as_float(a & 0xFFFF0000u));
-    rest[e + 1] = (bf16)fmaf(p[at + e + 1], 1.f + AS_EXTRA, -__uint_as_float(b & 0xFFFF0000u));
+    rest[e] = (bf16)fmaf(p[at + e], 1.f + AS_EXTRA<bf16>, -__uint_as_float(a & 0xFFFF0000u));
+    rest[e + 1] = (bf16)fmaf(p[at + e + 1], 1.f + AS_EXTRA<bf16>, -__uint_as_float(b & 0xFFFF0000u));
   }
   first = __builtin_bit_cast(bf16x8, f);
 }
@@ -382,7 +384,7 @@ __device__ __forceinline__ void in_two(const f32x16& p, int at, f16x8& first, f1
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const f16x2 f = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(p[at + e], p[at + e + 1]));
-    const f16x2 r = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(fmaf(p[at + e], 1.f + AS_EXTRA, -(float)f[0]), fmaf(p[at + e + 1], 1.f + AS_EXTRA, -(float)f[1])));
+    const f16x2 r = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(fmaf(p[at + e], 1.f + AS_EXTRA<f16>, -(float)f[0]), fmaf(p[at + e + 1], 1.f + AS_EXTRA<f16>, -(float)f[1])));
     first[e] = f[0]; first[e + 1] = f[1];
     rest[e] = r[0]; rest[e + 1] = r[1];
   }
@@ -580,7 +582,7 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const AttnCall<T
     const float m2 = m_ref * c.scale_log2e;
     if (it.part < 0) {
       T* out = c.out + (long long)request * c.out_stride + head * D + 4 * lh;
-      const float f = 1.f / ((1.f + AS_EXTRA) * l_run);
+      const float f = 1.f / ((1.f + AS_EXTRA<T>) * l_run);
 #pragma unroll
       for (int bb = 0; bb < DB; bb++)
 #pragma unroll
@@ -889,7 +891,7 @@ __global__ void __launch_bounds__(256) attn_shared_join_kernel(AttnCall<T> c) {
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 v;
 #pragma unroll
-    for (int e = 0; e < 4; e++) v[e] = (T)(p.len < 0 ? NAN : none ? 0.f : o[e] / ((1.f + AS_EXTRA) * l));
+    for (int e = 0; e < 4; e++) v[e] = (T)(p.len < 0 ? NAN : none ? 0.f : o[e] / ((1.f + AS_EXTRA<T>) * l));
     if (c.out_vec) *reinterpret_cast<T4*>(out) = v;
     else
 #pragma unroll
