@@ -203,7 +203,9 @@ int sts_read_hidden(sts_ctx* ctx, int32_t phase, float* out, int32_t rows);
  * first `rows` of them, with a token each. sts_op_logprobs on logits that are still on the device; its description says what the outputs are
  * where a row has nothing, NaN or infinities, and what a token out of range gives. Outputs [rows] and [rows, top_k] may each be NULL; tokens may be
  * NULL if logprob and rank are. STS_EINVAL if the call left fewer rows (a step that failed leaves none in the
- * phases that it was to run), STS_ESTATE while a launch of the phase is outstanding or its partition is empty. */
+ * phases that it was to run), STS_ESTATE while a launch of the phase is outstanding or its partition is empty.
+ * Some 40 us where the logits are on the device: of steps that made tokens, and of those of more than 32 MiB (8 if launched, or queued beside the other phase). Smaller
+ * ones that were only returned, a prefill's among them, are in host memory alone and come back over its link: 11 us a row of 128256 more (40 rows 450 us). */
 int sts_read_logprobs(sts_ctx* ctx, int32_t phase, const int32_t* tokens, int32_t rows, int32_t top_k, float* logprob, float* entropy, int32_t* rank,
                       float* top_logprob, int32_t* top_token);
 
@@ -362,7 +364,8 @@ int sts_op_block_tables(const sts_block_tables* a, void* stream);
  *   BASE    w_i of the base theta * factor^(rotary_dim / (rotary_dim - 2))
  *   BANDS   from w_i / factor (turns_i <= low) to w_i (turns_i >= high), in between in proportion to turns_i
  *   RAMP    from w_i (i <= a) to w_i / factor (i >= b), in between in proportion to i; a and b are the pair numbers, rounded outwards, that make
- *           `high` and `low` turns over original_len: rotary_dim ln(original_len / (turns 2 pi)) / (2 ln theta)
+ *           `high` and `low` turns over original_len: rotary_dim ln(original_len / (turns 2 pi)) / (2 ln theta), a at least 0 and b at most
+ *           rotary_dim - 1. Where that leaves b <= a, the pairs up to a keep w_i and those behind it have w_i / factor
  * magnitude: factor of cosine and sine (0: 1). */
 enum { STS_ROPE_PLAIN = 0, STS_ROPE_LINEAR, STS_ROPE_BASE, STS_ROPE_BANDS, STS_ROPE_RAMP };
 typedef struct {
@@ -394,7 +397,8 @@ int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* stream);
 
 /* Decode attention (one query row a request) for groups of requests whose contexts begin with the same pages. Requests
  * group_starts[g] .. group_starts[g + 1] - 1 are group g; the whole pages among the first shared_lens[g] tokens of their contexts, as far as
- * all of them hold them, are read through the first one's table, once for all. The caller sees to it that their tables agree there.
+ * all of them hold them, are read through the first one's table, once for all. The caller sees to it that their tables agree there. (A request of length 0, or of
+ * one out of range, holds none: padding belongs into a group of its own, or every request of its group reads all its pages for itself.)
  * shared_lens 0, a group of one, or group_starts that do not lead from 0 to n_requests in order: nothing is shared, the result is the same.
  * A context of length 0 gives zeros and an lse of -inf; one that is negative or longer than max_pages, or whose table names a page
  * outside the pool, gives NaN. What lies in a page behind its context is not looked at.
@@ -428,7 +432,7 @@ typedef struct {
   float *logprob, *entropy, *lse;       /* [rows], in nats */
   int32_t* rank;                        /* [rows]: tokens before the given one, larger logits first, then lower numbers (0: the greedy choice; a NaN logit: -1) */
   float* top_logprob; int32_t* top_token;      /* [rows][top_k], in that order */
-  void* workspace; int64_t workspace_bytes;    /* 16-byte aligned, sts_op_logprobs_workspace bytes (0 where there are many rows) */
+  void* workspace; int64_t workspace_bytes;    /* 16-byte aligned, sts_op_logprobs_workspace bytes (0 where there are many rows); calls that may run at the same time need their own */
 } sts_logprobs;
 /* Host only, no GPU state: bytes of workspace; -1 for sizes out of range. */
 int64_t sts_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t top_k);

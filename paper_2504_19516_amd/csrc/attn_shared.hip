@@ -18,8 +18,9 @@
 //
 // Measured, bf16, 32 query and 8 KV heads of 128; us of the plan (once a step), and of products and join (each layer):
 //   8 requests on 1031 shared tokens, 6 MB of pages a layer     7    8   4    latency
-//   64 requests on 2048 shared tokens, 100 MB                    8   22   4    4.5 TB/s in the products: memory
-//   256 requests on a document of 8192 tokens, 187 MB           11   72   9    2.6 TB/s and 0.49 PFLOP/s at once: matrix cores and exponentials
+//   64 requests on 2048 shared tokens, 100 MB                    8   24   5    4.2 TB/s in the products: memory
+//   256 requests on a document of 8192 tokens, 187 MB           12   89  10    2.1 TB/s and 0.39 PFLOP/s at once (0.59 with the second numbers): matrix cores and exponentials
+// (medians under a trace; on another card the document's products were 94)
 // (read by every request for itself, the document alone would be 8.6 GB a layer).
 #include <algorithm>
 
@@ -365,8 +366,8 @@ struct AttnCall {
 // wherever p is, so that a V of infinity gives infinity and not inf - inf or 0 * inf (fp16: from p = 2^-16 on). With u for half a step of the type (bf16
 // 2^-8, fp16 2^-11) their sum is within 2 u (2 u + e) of p (1 + e), fp16's smallest within 2^-24; what reads the sums takes the factor out, and the
 // output is rounded once, at the end: as far from 64 bits as that leaves any output. One number each, for half the second products, left outputs 1.04 to 1.11
-// times as far and took, us a pass then / now: 8 requests on 1031 tokens (four layers) 54.9 / 56.0, 64 on 2048 (four) 116 / 119, 256 on 8192 (two) 164 / 186, the larger
-// shape's groups (two) 61 / 63.
+// times as far and took, us a pass then / now: 8 requests on 1031 tokens (four layers) 54.9 / 56.0, 64 on 2048 (four) 116 / 119, 256 on 8192 (two) 164 / 186 (on
+// another card 172 / 196), the larger shape's groups (two) 61 / 63.
 template <typename T> constexpr float AS_EXTRA = std::is_same<T, f16>::value ? 0x1p-9f : 0x1p-18f;            // e: fp16's range ends soon
 __device__ __forceinline__ void in_two(const f32x16& p, int at, bf16x8& first, bf16x8& rest) {
   u32x4 f;

@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprobs_kernel(LogprobsCall c)
 #pragma unroll
     for (int bit = 31; bit >= 16; bit--) {
       const unsigned cand = kth | 1u << bit;
-      if (__popcll(__ballot(key >= cand)) >= k) kth = cand;
+      if ((int)__popcll(__ballot(key >= cand)) >= k) kth = cand;
     }
     const bool open = kth <= value_key(-INFINITY);
     float bound = open ? -INFINITY : below(key_value(kth));

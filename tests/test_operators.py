@@ -98,6 +98,19 @@ def test_logprobs_refuses(sts):
     assert sts.op_logprobs_workspace(1, 4000, 128256, 20) == 0
 
 
+@pytest.mark.parametrize("length,low,high,theta,rotary", [(4, 1.0, 32.0, 1e4, 64), (6, 1.0, 1.0, 1e4, 64), (1, 1.0, 32.0, 1e4, 64), (1 << 30, 1.0, 2.0, 1.5, 8), (4096, 1.0, 1.0, 1e4, 64),
+                                                           (1 << 30, 2.0 ** -10, 1.0, 1.125, 8)])
+def test_rope_ramp_that_ends_outside_the_pairs(sts, length, low, high, theta, rotary):
+    """Its ends are kept within 0 and rotary_dim - 1, and the pairs up to the first end come first."""
+    i, theta = np.arange(rotary // 2), np.float64(np.float32(theta))
+    w = theta ** (-2.0 * i / rotary)
+    pair = lambda turns: rotary * math.log(length / (turns * 2 * math.pi)) / (2 * math.log(theta))  # noqa: E731
+    a, b = max(math.floor(pair(high)), 0), min(math.ceil(pair(low)), rotary - 1)
+    want = np.where(i <= a, w, np.where(i >= b, w / 16, w + (w / 16 - w) * (i - a) / max(b - a, 1)))
+    got = sts.rope_frequencies(sts.Rope(rotary_dim=rotary, theta=theta, scaling=sts.ROPE_SCALINGS["ramp"], factor=16.0, low=low, high=high, original_len=length))
+    np.testing.assert_allclose(got, want, rtol=1e-13)
+
+
 def test_logprobs_refuses_vocabularies_above_the_most(sts):
     """Of a description that nothing else is wrong with."""
     good = dict(dtype=0, rows=2, vocab=1 << 30, top_k=5, row_stride=1 << 31, logits=A, tokens=2 * A, logprob=3 * A, workspace=9 * A, workspace_bytes=1 << 40)
