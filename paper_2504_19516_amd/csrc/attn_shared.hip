@@ -363,12 +363,15 @@ struct AttnCall {
 };
 
 // Eight probabilities for the second product, each in two numbers of the type: p without what the type drops, and p (1 + e) less that, which is above 0
-// wherever p is, so that a V of infinity gives infinity and not inf - inf or 0 * inf (fp16: from p = 2^-16 on). With u for half a step of the type (bf16
-// 2^-8, fp16 2^-11) their sum is within 2 u (2 u + e) of p (1 + e), fp16's smallest within 2^-24; what reads the sums takes the factor out, and the
+// wherever p is, so that a V of infinity gives infinity and not inf - inf or 0 * inf. With u for half a step of the type (bf16 2^-8, fp16 2^-11) their sum is
+// within 2 u (2 u + e) of p (1 + e); what reads the sums takes the factor out, and the
 // output is rounded once, at the end: as far from 64 bits as that leaves any output. One number each, for half the second products, left outputs 1.04 to 1.11
 // times as far and took, us a pass then / now: 8 requests on 1031 tokens (four layers) 54.9 / 56.0, 64 on 2048 (four) 116 / 119, 256 on 8192 (two) 164 / 186 (on
 // another card 172 / 196), the larger shape's groups (two) 61 / 63.
-template <typename T> constexpr float AS_EXTRA = std::is_same<T, f16>::value ? 0x1p-9f : 0x1p-18f;            // e: fp16's range ends soon
+// fp16 ends at 2^-24: its probabilities are lifted by 2^7, as far as AS_RISE leaves room for, and are held to 2^-31 of the reference's (the second number is above 0
+// from 2^-22 on).
+template <typename T> constexpr float AS_EXTRA = std::is_same<T, f16>::value ? 0x1p-9f : 0x1p-18f;            // e
+template <typename T> constexpr float AS_LIFT = std::is_same<T, f16>::value ? 7.f : 0.f;                       // exponent
 __device__ __forceinline__ void in_two(const f32x16& p, int at, bf16x8& first, bf16x8& rest) {
   u32x4 f;
 #pragma unroll
@@ -535,7 +538,7 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const AttnCall<T
 #pragma unroll
         for (int r = 0; r < 16; r++) o[bb][r] *= corr;
     }
-    const float nm = m_ref == -INFINITY ? 0.f : -m_ref * c.scale_log2e;
+    const float nm = m_ref == -INFINITY ? 0.f : fmaf(-m_ref, c.scale_log2e, AS_LIFT<T>);
     float rs = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; r++) {
@@ -580,7 +583,7 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const AttnCall<T
 
   // a lane has four elements in a row of its row's output, 32 bb + 8 r4 + 4 lh
   if (l32 < it.rows) {
-    const float m2 = m_ref * c.scale_log2e;
+    const float m2 = fmaf(m_ref, c.scale_log2e, -AS_LIFT<T>);
     if (it.part < 0) {
       T* out = c.out + (long long)request * c.out_stride + head * D + 4 * lh;
       const float f = 1.f / ((1.f + AS_EXTRA<T>) * l_run);
@@ -737,7 +740,7 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>&
 #pragma unroll
         for (int r = 0; r < 16; r++) o[b][r] *= corr;
     }
-    const float nm = (m_ref == -INFINITY) ? 0.f : -m_ref * c.scale_log2e;
+    const float nm = (m_ref == -INFINITY) ? 0.f : fmaf(-m_ref, c.scale_log2e, AS_LIFT<T>);
     float rs = 0.f;
 #pragma unroll
     for (int kb = 0; kb < 2; kb++)
@@ -812,7 +815,7 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const AttnCall<T>&
       const f32x4 v = *reinterpret_cast<const f32x4*>(buf + r * OROWB + (ch ^ (r % 16)) * 16);
       if (r < my_rows) *reinterpret_cast<f32x4*>(c.plan.outs + ((size_t)(part + r) * c.n_kv + kvh) * D + ch * 4) = v;
     }
-    if (lane < my_rows) c.plan.stats[(size_t)(part + lane) * c.n_kv + kvh] = f32x2{m_ref * c.scale_log2e, l_run};
+    if (lane < my_rows) c.plan.stats[(size_t)(part + lane) * c.n_kv + kvh] = f32x2{fmaf(m_ref, c.scale_log2e, -AS_LIFT<T>), l_run};
   }
   __syncthreads();                                       // before the next item's K lands there
 }

@@ -547,6 +547,35 @@ def test_shared_attention_wide_infinities(sts):
     assert np.isnan(hot[:, 4:]).all() and np.array_equal(np.isnan(hot[:, :4]).all(2), nan[:, :4])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("groups", [((43, 176),), ((3, 32), (4, 64))])
+@pytest.mark.parametrize("power", [10, 18, 21])
+def test_shared_attention_small_weights(sts, dtype, groups, power):
+    """Tokens of 2^-power of the others' weight. They count, many of them for one other, and an infinite V of one reaches the output, wide and narrow."""
+    lens = tuple(s + 40 for m, s in groups for _ in range(m))
+    q, k, v, tables, pages, lens, groups = small_case(np.random.default_rng(24), dtype, lens, groups)
+    small = rounded(-power * np.log(2.0) * 8 / 4, dtype)   # 4 k / 8: the score
+    q[:] = 0
+    q[:, :, 0] = 4
+    for r in range(len(lens)):
+        k[r][:, :, 0] = 0
+        k[r][:, 0, 0] = small                              # of the first KV head all but the last token
+        k[r][-1, 0, 0] = 0
+        k[r][5, 1, 0] = small
+        v[r][:-1, 0], v[r][-1, 0] = rounded(1024.0 + np.abs(v[r][:-1, 0]), dtype), 0
+        v[r][5, 1, 9] = np.inf
+    pool = pool_of(k, v, tables, lens, pages, dtype)
+    with Device() as dev:
+        got, lse, _, _ = run_attention(sts, dev, dtype, q, pool, tables, lens, groups, 4)
+    assert np.isposinf(got[:, 4:, 9]).all() and np.isfinite(got[:, 4:, :9]).all() and np.isfinite(lse).all()
+    # u for the output, of the weights 2 u (2 u + 2^-9), 2^-31 for fp16's last place, 2^-17 for exponentials of up to 22 and the sums
+    u = HALF[dtype]
+    for r in range(len(lens)):
+        w = np.exp(k[r][:, 0, 0].astype(np.float64) * 0.5)
+        out, size = w @ v[r][:, 0].astype(np.float64) / w.sum(), np.abs(v[r][:, 0]).astype(np.float64).sum(0)
+        near(got[r, :4], np.tile(out, (4, 1)), np.tile((u + 2 * u * (2 * u + 2.0 ** -9) + 2.0 ** -17) * out + (2.0 ** -31 * size + 2.0 ** -25 if dtype == "f16" else 0.0), (4, 1)))
+
+
 @pytest.mark.parametrize("dtype,n_q,n_kv,groups", [("bf16", 4, 2, [(2, 16)] * 2048), ("f16", 8, 1, [(4096, 48)]), ("bf16", 8, 1, [(9, 32)] * 455 + [(1, 0)]), ("f16", 2, 2, [(1, 0)] * 4096)])
 def test_shared_attention_of_the_most_requests(sts, dtype, n_q, n_kv, groups):
     rng = np.random.default_rng(len(groups))
