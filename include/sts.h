@@ -438,6 +438,91 @@ typedef struct {
 int64_t sts_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t top_k);
 int sts_op_logprobs(const sts_logprobs* a, void* stream);
 
+/* ---- operators on device data, for a step that verifies drafted tokens. A request brings nodes: its last token and what a draft guesses to follow, each
+ * with the number of its parent among the request's nodes. Conventions as above (sts_op_block_tables: places of the nodes' rows, node i at token
+ * cached + i). In their order of use: sts_op_block_tables, sts_op_attn_tree_plan (positions of the nodes, and what they see), for each layer sts_op_norm_rope (or
+ * sts_op_rope) and sts_op_attn_tree, then sts_op_adjust_logits, the target's choice for every node (sts_op_logprobs' first alternative, or a sample),
+ * sts_op_tree_accept, sts_op_tree_compact. */
+
+/* sts_op_rope of heads that are first divided by their root mean square: x / sqrt(mean(x^2) + eps) times the gain of each element, over the d elements of a head of
+ * Q and of K; V passes. All in 32 bits (squares and their sum too: elements below 2^60), rounded once, behind the rotation. d up to 512. */
+typedef struct {
+  int32_t dtype;                        /* of the gains */
+  int32_t offset_one;                   /* 1: gains are stored less 1 */
+  float eps;                            /* not negative */
+  const void *q_gain, *k_gain;          /* [d]; NULL: all 1 */
+} sts_head_norm;
+int sts_op_norm_rope(const sts_head_norm* norm, const sts_rope* rope, const sts_rope_rows* a, void* stream);
+
+/* Attention of a request's nodes: to its cached tokens, to a node's ancestors and to itself. Rows are the nodes, request after request, as
+ * sts_op_block_tables numbers them. A row whose parent is no earlier node of its request (-1: it follows the context) is no node, nor are those below it:
+ * their rows are padding, which gives zeros and an lse of -inf, and which nobody sees. Rows from row_starts[n_requests] on are left as they were. A request
+ * of more than 256 rows, one with cached < 0 or cached + rows behind max_pages, one whose table names a page outside the pool, and all rows if row_starts does not
+ * lead from 0 to at most max_rows in order, give NaN. What lies in a page behind the nodes is not looked at, and infinities and NaN in a node's K or V stay with those
+ * who see it.
+ * The plan is made once a step and serves all layers, as for sts_op_attn_shared; a workspace that holds no plan, or one of a batch of other sizes, gives NaN for
+ * all max_rows rows. Calls that may run at the same time need workspaces of their own. */
+typedef struct {
+  int32_t dtype;                        /* STS_BF16 or STS_F16: of q, pool and out */
+  int32_t n_requests, max_rows;         /* max_rows up to 65536: length of parents, positions, rows of q and out */
+  int32_t n_q, n_kv, d;                 /* n_q / n_kv up to 32, n_kv up to 256, d 64 or 128 */
+  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read; times (max_rows * n_q / n_kv / 128 + n_requests) up to 2^30 */
+  int64_t table_stride;                 /* >= max_pages */
+  const int32_t *tables, *cached;       /* [n_requests][table_stride], with the nodes' pages; [n_requests]: tokens before the nodes */
+  const int32_t *row_starts, *parents;  /* [n_requests + 1]; [max_rows]: number of a node's parent in its request, -1: none */
+  int32_t* positions;                   /* [max_rows]: cached + depth, -1 of padding; written by the plan; NULL: not wanted */
+  void* workspace; int64_t workspace_bytes;    /* 256-byte aligned, sts_attn_tree_workspace bytes */
+} sts_tree_batch;
+/* Host only, no GPU state: bytes of workspace; -1 for sizes out of range. */
+int64_t sts_attn_tree_workspace(int32_t n_requests, int32_t max_rows, int32_t n_q, int32_t n_kv, int32_t d);
+int sts_op_attn_tree_plan(const sts_tree_batch* b, void* stream);
+/* q and out [max_rows][n_q * d], strides in elements; pool: one layer's, 16-byte aligned, the nodes' K and V in it; lse [max_rows][n_q] or NULL. scale 0: 1 / sqrt(d). */
+int sts_op_attn_tree(const sts_tree_batch* b, const void* q, int64_t q_stride, const void* pool, void* out, int64_t out_stride, float* lse, float scale, void* stream);
+
+/* Logits before a token is chosen. With n the times that a token stands in the output of the row's request, and s whether it stands in its prompt or output:
+ *   y = x / repetition (x > 0) or x * repetition, where s;  y -= frequency * n;  y -= presence, where n > 0;  y += bias;  -inf, where the row's mask has a 0
+ * in 64 bits, rounded once. Elements that nothing applies to keep their bits. The output: tokens[prompt_len .. len) of the request, and of a drafted node's row the
+ * tokens of the node and its ancestors. */
+typedef struct {
+  int32_t dtype, rows, vocab, n_requests;      /* rows up to 65535, vocab up to 2^30 */
+  int64_t row_stride, out_stride;       /* elements from row to row */
+  const void* logits; void* out;        /* aligned to their elements; out = logits, with equal strides: in place */
+  const int32_t* requests;              /* [rows]: request of each row (outside 0 .. n_requests - 1: the row's mask alone applies); NULL: row i is request i */
+  int32_t n_biases, n_masks;            /* length of bias_tokens and bias_values; rows of masks */
+  int64_t token_stride, mask_stride;    /* tokens, and 32-bit words, from row to row */
+  const int32_t* tokens;                /* [n_requests][token_stride], NULL: no history; tokens outside the vocabulary do not count */
+  const int32_t *lens, *prompt_lens;    /* [n_requests]: tokens in all, up to token_stride (taken as that beyond it), and of the prompt (NULL: 0) */
+  const float *repetition, *frequency, *presence;       /* [n_requests]; NULL: 1, 0 and 0 */
+  const int32_t *row_starts, *parents, *drafted;        /* [n_requests + 1], [rows], [rows]: the nodes, as for sts_op_attn_tree, and their tokens; drafted NULL: no nodes */
+  const int32_t *bias_starts, *bias_tokens; const float* bias_values;       /* [n_requests + 1], entries of each request; of several of one token the last counts; NULL: none */
+  const uint32_t* masks;                /* [n_masks][mask_stride]: bit t % 32 of word t / 32 is 0 where token t is ruled out; NULL: none */
+  const int32_t* mask_rows;             /* [rows]: mask of each row; outside 0 .. n_masks - 1: none */
+} sts_adjust_logits;
+int sts_op_adjust_logits(const sts_adjust_logits* a, void* stream);
+
+/* The accepted path of each request: node 0, then as long as there is one the first child of the last node whose token is chosen[] of that node's row, which is what
+ * the target takes behind it. */
+typedef struct {
+  int32_t n_requests, max_rows;
+  const int32_t* cached;                /* [n_requests] */
+  const int32_t *row_starts, *parents;  /* as for sts_op_attn_tree */
+  const int32_t *tokens, *chosen;       /* [max_rows]: of each node, and the target's choice behind it */
+  int32_t *lens, *counts;               /* [n_requests]: cached + count, and the nodes on the path (0: no rows, more than 256, or node 0 is none; lens then cached) */
+  int32_t* path;                        /* [max_rows]: numbers of a request's nodes on the path, from its first row on, -1 behind them; rows of no request are left as they were */
+  int32_t* next_token;                  /* [n_requests]: chosen[] of the last; -1 without one */
+} sts_tree_accept;
+int sts_op_tree_accept(const sts_tree_accept* a, void* stream);
+/* K and V of the path's nodes to tokens cached, cached + 1, ... of their requests, in all layers' pools. The pages of tokens that move may not be another request's.
+ * Nodes whose place lies behind max_pages or outside the pool are not moved. */
+typedef struct {
+  int32_t n_requests, max_rows, n_kv, d;       /* n_kv up to 256, d 64 or 128; elements of 16 bits */
+  int32_t pool_pages, max_pages;
+  int64_t table_stride;
+  const int32_t *tables, *cached, *row_starts, *counts, *path;      /* as above, path as sts_op_tree_accept leaves it */
+} sts_tree_compact;
+/* pools: n_layers (up to 256) device addresses in HOST memory, each 16-byte aligned. */
+int sts_op_tree_compact(const sts_tree_compact* a, void* const* pools, int32_t n_layers, void* stream);
+
 /* ---- performance estimator (Section 3.2) — host only, integer arithmetic.
  * Wave quantisation (Section 2.2.1): g workgroups on n units, b workgroups per unit. */
 int sts_wave_quant(int64_t g, int64_t n, int64_t b, int64_t* waves, int64_t* tail, int64_t* idle_num, int64_t* idle_den);

@@ -1,0 +1,930 @@
+// Attention of drafted tokens over a paged cache: a request brings up to 256 nodes, each of which attends to the request's cached tokens, to its
+// ancestors among the nodes, and to itself (a chain is the tree whose nodes have one child each).
+//
+//   o_i = sum_t p_t v_t / l,   p_t = 2^(scale log2(e) q_i . k_t - m),   l = sum_t p_t,   over t < c and t = c + j, j on the path to node i
+//
+// computed in parts of the token range, each with its own maximum m, that a second kernel joins:
+//   m = max m_j,  l = sum l_j 2^(m_j - m),  o = sum o_j 2^(m_j - m) / l
+//
+// The rows of a KV head are a request's nodes times its query heads: they are cut into tiles of up to 128, and a tile over all the request's pages is a
+// segment. Up to 32 rows (narrow) a wave takes pages by itself; beyond that (wide) the waves of a workgroup share the pages through LDS. A KV element read serves
+// all rows of a tile, so few rows are bound by memory, and from some 230 rows (the card's operations a byte) the matrix cores are what bounds.
+//
+// The plan, made once a step on the device, does three things: it follows the parents up (each round doubles how far) and keeps for every node a bit
+// for each token of the pages that hold nodes; it writes the nodes' positions; and it lays the segments of each kind end to end (pages, and the start and end of
+// a segment counted as pages) and cuts each line into equal shares, one for each workgroup or wave. Piece p of segment s lies in share k: s + k is its number and
+// (first row) + (rows of a share's tile) * k the place of its partial result, both without a further scan.
+#include <algorithm>
+
+#include "attn_parts.h"
+
+namespace sts {
+namespace {
+
+constexpr int AT_ROWS = 32;                     // rows of a narrow segment: columns of a product
+constexpr int AT_TILE = 128;                    // rows of a wide one, at most
+constexpr int AT_SLOTS = 512;                   // workgroups of a launch: two on each CU
+constexpr int AT_NODES = 256;                   // of a request
+constexpr int AT_MASK = 32;                     // 16-bit words of a row's mask, one for each page from the first that holds a node: up to 17 are used
+constexpr int AT_MAX_ROWS = 1 << 16;
+constexpr int AT_PLAN_THREADS = 512;
+constexpr int AT_JOIN_ROWS = 1024;              // up to so many (row, head) pairs four waves join each, beyond it one
+// Start and end of a wide and of a narrow segment, and the smallest shares beyond them, in pages; what a page of a wide segment takes a workgroup, in
+// pages of a narrow one.
+constexpr int AT_WIDE_START = 8, AT_NARROW_START = 2, AT_WIDE_LEAST = 4, AT_NARROW_LEAST = 4;
+constexpr float AT_WIDE_WEIGHT = 1.25f;
+
+// A piece of a segment: rows row0 .. row0 + rows - 1 (node row * heads of a group + head) over the pages [pg0, pg1) of a request's table. part: number of its
+// first row's partial result, -1: it finishes its rows.
+struct Item { int row0, rows, request, pg0, pg1, part, cached, len; };
+struct Range { Item first; int next, end, pad[2]; };              // items of a wave: the first, and next .. end - 1; none if its rows are 0. The four of a workgroup with wide ones have the same
+// A request: where its tiles begin on the line of its kind, its pages (0: nothing of it is computed), first row and rows in all, and of a tile; wide or narrow
+struct Request { int at, pages, row0, rows, per, kind, bad, pad; };
+struct Header {
+  unsigned long long tag;                        // sizes_tag() of the batch that the plan was made for
+  Line lines[2];                                 // wide, narrow
+  int narrow_part;                               // first partial row of narrow segments
+  int rows;                                      // node rows; -1: row_starts out of order
+  int pad[4];
+};
+struct Plan {
+  Header* header;
+  Range* ranges;                                 // [slots][4]
+  Item* items;
+  Request* requests;                             // [n_requests]
+  int* owners;                                   // [max_rows]: request of a row, -1: no node
+  unsigned short* masks;                         // [max_rows][AT_MASK]: a bit for each token of a page
+  f32x2* stats;                                  // [partial row][kv head]: maximum (log2 units), sum
+  float* outs;                                   // [partial row][kv head][d]
+};
+
+int slots_of(int n_kv) { return std::max(1, AT_SLOTS / n_kv); }
+// tiles: all rows in whole ones, and one begun for each request
+int64_t max_segments(int n, int max_rows, int heads) { return (int64_t)max_rows * heads / AT_TILE + n; }
+int64_t max_items(int n, int max_rows, int n_q, int n_kv) { return max_segments(n, max_rows, n_q / n_kv) + 4 * slots_of(n_kv); }
+int64_t max_part_rows(int max_rows, int n_q, int n_kv) { return (int64_t)2 * max_rows * (n_q / n_kv) + (int64_t)slots_of(n_kv) * AT_TILE; }
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+// The workspace's parts behind each other; returns its size.
+size_t lay_out(unsigned char* base, int n, int max_rows, int n_q, int n_kv, int d, Plan* p) {
+  size_t at = 0;
+  auto take = [&](size_t bytes) { unsigned char* q = base + at; at += up256(bytes); return q; };
+  const size_t rows = (size_t)max_part_rows(max_rows, n_q, n_kv) * n_kv;
+  Plan q;
+  q.header = reinterpret_cast<Header*>(take(sizeof(Header)));
+  q.ranges = reinterpret_cast<Range*>(take(slots_of(n_kv) * 4 * sizeof(Range)));
+  q.items = reinterpret_cast<Item*>(take(max_items(n, max_rows, n_q, n_kv) * sizeof(Item)));
+  q.requests = reinterpret_cast<Request*>(take(n * sizeof(Request)));
+  q.owners = reinterpret_cast<int*>(take(max_rows * sizeof(int)));
+  q.masks = reinterpret_cast<unsigned short*>(take((size_t)max_rows * AT_MASK * sizeof(unsigned short)));
+  q.stats = reinterpret_cast<f32x2*>(take(rows * sizeof(f32x2)));
+  q.outs = reinterpret_cast<float*>(take(rows * d * sizeof(float)));
+  if (p) *p = q;
+  return at;
+}
+
+// The sizes on which the indexes of a plan's users depend, never 0. A workspace without a plan of the batch's sizes gives NaN: nothing in it is followed.
+unsigned long long sizes_tag(const sts_tree_batch& b) {
+  unsigned long long t = 2;
+  for (int32_t x : {b.n_requests, b.max_rows, b.n_q, b.n_kv, b.d, b.max_pages}) t = t * 0x9E3779B97F4A7C15ull + (uint32_t)x;
+  return t << 1 | 1;
+}
+
+// ---- the plan: workgroup 0 deals the pages out, workgroup 1 + i makes the masks of request i
+struct PlanCall { unsigned long long tag; int n, max_rows, heads, slots, max_pages; const int *cached, *row_starts, *parents; int* positions; Plan plan; };
+
+// Exclusive sums over the workgroup's threads, and the totals, of N values.
+template <int N>
+__device__ __forceinline__ void plan_scan(int (&v)[N], int (&total)[N], int (*waves)[AT_PLAN_THREADS / 64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int x[N];
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    x[i] = wave_sums_up(v[i]);
+    if (lane == 63) waves[i][wave] = x[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < AT_PLAN_THREADS / 64; w++) {
+      const int y = waves[i][w];
+      before += w < wave ? y : 0;
+      all += y;
+    }
+    total[i] = all;
+    v[i] = before + x[i] - v[i];
+  }
+  __syncthreads();
+}
+
+// Whether request i's rows and lengths are in range (row_starts as a whole may still be out of order).
+__device__ __forceinline__ bool request_ok(const PlanCall& c, int cached, int first, int end) {
+  return first >= 0 && end >= first && end <= c.max_rows && end - first <= AT_NODES && cached >= 0 && cached <= c.max_pages * (long long)OP_PAGE - (end - first);
+}
+
+__device__ void deal_out(const PlanCall& c) {
+  constexpr int N = OP_MAX_REQUESTS;
+  // by request: first row; places on the lines of wide and narrow segments, and the first wide and narrow segment (16 bits each would do for one kind: up
+  // to 2^16 rows of 32 heads are 2^14 tiles)
+  __shared__ int start[N + 1], line_at[2][N + 1], cached[N], waves[4][AT_PLAN_THREADS / 64];
+  __shared__ unsigned short seg0[2][N + 1];
+  const int n = c.n, tid = threadIdx.x;
+  bool malformed = false;
+  for (int i = tid; i <= n; i += AT_PLAN_THREADS) {
+    const int s = c.row_starts[i];
+    malformed |= s < 0 || s > c.max_rows || (i == 0 && s != 0) || (i < n && s > c.row_starts[i + 1]);
+    start[i] = s;
+    if (i < n) cached[i] = c.cached[i];
+  }
+  const bool ordered = !__syncthreads_or(malformed);
+  struct Shape { int rows, pages, per, tiles, kind; };
+  auto shape = [&](int i) {
+    const int nodes = start[i + 1] - start[i];
+    Shape s{0, 0, 0, 0, 0};
+    if (!ordered || nodes == 0 || !request_ok(c, cached[i], start[i], start[i + 1])) return s;
+    s.rows = nodes * c.heads;
+    s.pages = (cached[i] + nodes + OP_PAGE - 1) / OP_PAGE;
+    s.kind = s.rows <= AT_ROWS;
+    const int blocks = (s.rows + AT_ROWS - 1) / AT_ROWS, most = (blocks + 3) / 4;          // tiles of alike numbers of 32 rows
+    s.per = (blocks + most - 1) / most * AT_ROWS;
+    s.tiles = (s.rows + s.per - 1) / s.per;
+    return s;
+  };
+  auto tile_cost = [&](const Shape& s) { return s.pages + (s.kind ? AT_NARROW_START : AT_WIDE_START); };
+  const int per = (n + AT_PLAN_THREADS - 1) / AT_PLAN_THREADS, r0 = min(n, tid * per), r1 = min(n, r0 + per);
+  int sums[4] = {0, 0, 0, 0}, all[4];            // cost and segments, wide and narrow
+  for (int i = r0; i < r1; i++) {
+    const Shape s = shape(i);
+    if (s.tiles == 0) continue;
+    sums[s.kind] += s.tiles * tile_cost(s);
+    sums[2 + s.kind] += s.tiles;
+  }
+  plan_scan(sums, all, waves);
+  const float wide_work = AT_WIDE_WEIGHT * all[0];
+  int wide = all[0] == 0 ? 0 : (int)(c.slots * (wide_work / (wide_work + all[1])) + 0.5f);
+  wide = min(max(wide, (int)(all[0] > 0)), c.slots - (all[1] > 0));
+  const int narrow = 4 * (c.slots - wide);
+  auto line = [&](int total, int count, int start, int least, int granule) {
+    const int share = max((total + max(count, 1) - 1) / max(count, 1), start + least);
+    return Line{share, start, granule, 1.f / (float)share};
+  };
+  const Line lines[2] = {line(all[0], wide, AT_WIDE_START, AT_WIDE_LEAST, 4), line(all[1], narrow, AT_NARROW_START, AT_NARROW_LEAST, 2)};
+  const int narrow_part = c.max_rows * c.heads + wide * AT_TILE;
+  if (tid == 0) {
+    *c.plan.header = Header{c.tag, {lines[0], lines[1]}, narrow_part, ordered ? start[n] : -1, {0, 0, 0, 0}};
+    line_at[0][n] = all[0]; line_at[1][n] = all[1];
+  }
+  for (int i = r0; i < r1; i++) {
+    const Shape s = shape(i);
+    line_at[0][i] = sums[0]; line_at[1][i] = sums[1];
+    seg0[0][i] = (unsigned short)sums[2]; seg0[1][i] = (unsigned short)sums[3];
+    c.plan.requests[i] = Request{sums[s.kind], s.pages, start[i] * c.heads, s.rows, s.per, s.kind, s.tiles == 0, 0};
+    if (s.tiles == 0) continue;
+    sums[s.kind] += s.tiles * tile_cost(s);
+    sums[2 + s.kind] += s.tiles;
+  }
+  __syncthreads();
+  // The items of a share, by a thread of its own. Neighbouring narrow shares go to different workgroups.
+  for (int j = tid; j < wide + narrow; j += AT_PLAN_THREADS) {
+    const int kind = j >= wide, k = kind ? j - wide : j;
+    const Line& l = lines[kind];
+    const int begin = k * l.share, end = begin + l.share;
+    Range r{};
+    if (begin < all[kind]) {
+      int i = last_up_to(line_at[kind], n, begin);                // has tiles there: the last of several at one place
+      Shape s = shape(i);
+      int t = (begin - line_at[kind][i]) / tile_cost(s);
+      for (int from_at = line_at[kind][i] + t * tile_cost(s); from_at < end;) {
+        const int from = begin > from_at ? l.up_to(from_at, s.pages, k - 1) : 0, to = l.up_to(from_at, s.pages, k);
+        if (from < to) {
+          const int item = (kind ? all[2] + wide : 0) + seg0[kind][i] + t + k, v0 = start[i] * c.heads + t * s.per;
+          const bool done = to - from == s.pages;
+          const Item it{v0, min(s.per, s.rows - t * s.per), i, from, to, done ? -1 : kind ? narrow_part + v0 + AT_ROWS * k : v0 + AT_TILE * k, cached[i], cached[i] + start[i + 1] - start[i]};
+          if (r.first.rows == 0) {
+            r.first = it;
+            r.next = r.end = item + 1;
+          } else {
+            c.plan.items[item] = it;
+            r.end = item + 1;
+          }
+        }
+        from_at += tile_cost(s);
+        if (++t < s.tiles) continue;
+        do i++; while (i < n && line_at[kind][i + 1] == line_at[kind][i]);
+        if (i == n) break;
+        s = shape(i);
+        t = 0;
+      }
+    }
+    if (kind) {
+      const int others = c.slots - wide;
+      c.plan.ranges[(wide + k % others) * 4 + k / others] = r;
+    } else {
+      for (int w = 0; w < 4; w++) c.plan.ranges[k * 4 + w] = r;
+    }
+  }
+}
+
+__device__ void follow_parents(const PlanCall& c, int request) {
+  __shared__ unsigned up[2][AT_NODES][8];        // ancestors and the node itself
+  __shared__ short jump[2][AT_NODES];            // an ancestor further and further up, -1: none
+  __shared__ unsigned char lost[2][AT_NODES];    // no node, or below one that is none
+  const int first = c.row_starts[request], end = c.row_starts[request + 1], cached = c.cached[request], tid = threadIdx.x;
+  if (first < 0 || end <= first || end > c.max_rows) return;
+  const bool ok = request_ok(c, cached, first, end);
+  if (!ok) {
+    for (int row = first + tid; row < end; row += AT_PLAN_THREADS) {
+      c.plan.owners[row] = request;
+      if (c.positions) c.positions[row] = -1;
+    }
+    return;
+  }
+  // two threads a node, four words each
+  const int nodes = end - first, i = tid >> 1, w0 = (tid & 1) * 4;
+  if (i < nodes) {
+    const int p = c.parents[first + i];
+    const bool none = p < -1 || p >= i;
+#pragma unroll
+    for (int w = 0; w < 4; w++) up[0][i][w0 + w] = i >> 5 == w0 + w ? 1u << (i & 31) : 0u;
+    if (w0 == 0) { jump[0][i] = (short)(none ? -1 : p); lost[0][i] = none; }
+  }
+  int now = 0;
+  for (int reach = 1; reach < nodes; reach <<= 1, now ^= 1) {
+    __syncthreads();
+    const int j = i < nodes ? jump[now][i] : -1;
+    if (!__syncthreads_or(j >= 0)) break;
+    if (i < nodes) {
+#pragma unroll
+      for (int w = 0; w < 4; w++) up[now ^ 1][i][w0 + w] = up[now][i][w0 + w] | (j >= 0 ? up[now][j][w0 + w] : 0u);
+      if (w0 == 0) {
+        jump[now ^ 1][i] = j >= 0 ? jump[now][j] : (short)-1;
+        lost[now ^ 1][i] = lost[now][i] | (j >= 0 ? lost[now][j] : (unsigned char)0);
+      }
+    }
+  }
+  __syncthreads();
+  if (i >= nodes) return;
+  const bool node = !lost[now][i];
+  if (w0 == 0) {
+    int depth = -1;
+#pragma unroll
+    for (int w = 0; w < 8; w++) depth += __popc(up[now][i][w]);
+    if (c.positions) c.positions[first + i] = node ? cached + depth : -1;
+    c.plan.owners[first + i] = node ? request : -1;
+  }
+  // Bits of the tokens from the page of the first node on: those before it belong to the context. Words of two pages.
+  const int shift = cached % OP_PAGE;
+  unsigned* to = reinterpret_cast<unsigned*>(c.plan.masks + (size_t)(first + i) * AT_MASK);
+  for (int w = tid & 1; w < 9; w += 2) {
+    const unsigned here = w < 8 ? up[now][i][w] : 0u, before = w > 0 ? up[now][i][w - 1] : ~0u;
+    to[w] = !node ? 0u : shift ? here << shift | before >> (32 - shift) : here;
+  }
+}
+
+__global__ void __launch_bounds__(AT_PLAN_THREADS) attn_tree_plan_kernel(PlanCall c) {
+  if (blockIdx.x == 0) deal_out(c);
+  else follow_parents(c, blockIdx.x - 1);
+}
+
+// ---- the products
+template <typename T>
+struct TreeCall {
+  const T* q; long long q_stride; const T* pool; T* out; long long out_stride; float* lse;
+  const int* tables; long long table_stride;
+  int max_rows, n, n_q, n_kv, heads, pool_pages;
+  float scale_log2e;
+  bool q_vec, out_vec;                           // rows can be loaded 16 bytes, stored 8 bytes at a time
+  unsigned long long tag;                        // what the plan's header has to hold
+  Plan plan;
+};
+
+// What a row sees of an item's pages.
+struct Seen {
+  const unsigned short* mask;
+  int first, end;                                // the page of the first node; the item's last page + 1
+  __device__ __forceinline__ unsigned page(int pg) const { return pg >= end ? 0u : pg < first ? 0xFFFFu : mask[pg - first]; }
+};
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+
+// Adds what the elements of V that are no numbers bring to the rows that see them (the products took 0 for them: another branch's infinity must not
+// become 0 * inf in a row that does not see it). p > 0 times an infinity or NaN is that. Seldom. From page pg0 on; `table`: of the whole request.
+template <typename T, int D>
+__device__ __forceinline__ void add_odd(f32x16 (&o)[D / 32], const TreeCall<T>& c, const Item& it, int pg0, const int* table, const Seen& seen, int kvh, int lh) {
+  for (int t = pg0 * OP_PAGE; t < min(it.len, it.pg1 * OP_PAGE); t++) {
+    const int page = table[t / OP_PAGE];
+    if ((unsigned)page >= (unsigned)c.pool_pages) continue;
+    const bool here = seen.page(t / OP_PAGE) >> (t % OP_PAGE) & 1;
+    const T* v = c.pool + ((size_t)page * c.n_kv + kvh) * 2 * OP_PAGE * D + OP_PAGE * D + t % OP_PAGE;
+#pragma unroll
+    for (int b = 0; b < D / 32; b++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        const float x = (float)v[(b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)) * OP_PAGE];
+        if (here && !finite(x)) o[b][r] += x;
+      }
+  }
+}
+// V of a half page as the product may take it: 0 for what is no number, or lies behind the last node. True where the first was there.
+template <typename V, typename T>
+__device__ __forceinline__ bool without_odd(V& v, int tokens) {
+  bool odd = false;
+#pragma unroll
+  for (int e = 0; e < 8; e++) {
+    const bool no = !finite((float)v[e]);
+    odd |= no && e < tokens;
+    if (no || e >= tokens) v[e] = (T)0.f;
+  }
+  return odd;
+}
+
+template <int D>
+constexpr int attn_tree_lds() { return AS_LDS_BASE + 4 * 2 * 2 * 16 * D * 2; }   // two blocks of K for each wave; two tiles of K and V^T; 128 rows of output
+
+// A lane's four elements of a row, 4 d-elements in a row, rounded once.
+template <typename T>
+__device__ __forceinline__ void store4(T* to, f32x4 x, float f, bool vec) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 v;
+#pragma unroll
+  for (int e = 0; e < 4; e++) v[e] = (T)(x[e] * f);
+  if (vec) *reinterpret_cast<T4*>(to) = v;
+  else
+#pragma unroll
+    for (int e = 0; e < 4; e++) to[e] = v[e];
+}
+
+// ---- narrow items, one wave: blocks of two pages (32 tokens), K rows global -> LDS without passing through registers, V^T straight into the registers of
+// its product, both two blocks ahead, with the waits of attn_decode.hip, which explains the order of the tokens. Nobody else reads the pages:
+// non-temporal.
+template <typename T, int D>
+__device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T>& c, const Item& it, int kvh) {
+  typedef typename Mfma<T>::V V;
+  constexpr int KSTEPS = D / 16, DB = D / 32;
+  constexpr int ROWB = D * 2, CPR = D / 8, RPI = 64 / CPR, IPP = 16 / RPI;   // K row bytes, 16-byte chunks, rows per load, loads per page
+  constexpr int PAGE_KB = 16 * ROWB, STAGE = 2 * PAGE_KB;
+  constexpr int LOADS = 2 * IPP + 2 * DB;            // loads of a block: K to LDS, V^T to registers
+  const int tid = fresh(threadIdx.x), lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int npg = it.pg1 - it.pg0, nblk = (npg + 1) >> 1;
+  const int* table = c.tables + (long long)it.request * c.table_stride + it.pg0;
+  const size_t head_elems = (size_t)2 * OP_PAGE * D;
+  // Page numbers, 64 of them one per lane, and the next 64; past the end the last page again (fetched, left out). One outside the pool
+  // is not followed: page 0 is read for it, and the rows come out as NaN.
+  bool bad = false, odd = false;
+  auto load_pages = [&](int window) {
+    const int page = table[min(window * 64 + lane, npg - 1)];
+    const bool out = (unsigned)page >= (unsigned)c.pool_pages;
+    bad |= out;
+    return out ? 0 : page;
+  };
+  int window = 0, pages_now = load_pages(0), pages_next = npg > 64 ? load_pages(1) : 0;
+  auto page_base = [&](int i) -> const T* {           // windows are asked for in order
+    const int j = __builtin_amdgcn_readfirstlane(min(i, npg - 1));
+    if ((j >> 6) > window) { window++; pages_now = pages_next; pages_next = load_pages(window + 1); }
+    const int page = __builtin_amdgcn_readlane(pages_now, j & 63);
+    return c.pool + ((size_t)page * c.n_kv + kvh) * head_elems;
+  };
+  auto swz = [](int row) { return D == 128 ? (row & 15) : ((row >> 1) & 7); };
+  unsigned char* kbuf = smem + AS_LDS_BASE + wv * 2 * STAGE;
+  int ksrc[IPP];
+#pragma unroll
+  for (int j = 0; j < IPP; j++) {
+    const int row = j * RPI + lane / CPR;
+    ksrc[j] = row * D + ((lane % CPR) ^ swz(row)) * 8;
+  }
+  const T* base[2];                                   // the two pages of the block fetched last
+  auto issue_k = [&](int b, int stage) {
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      base[u] = page_base(2 * b + u);
+#pragma unroll
+      for (int j = 0; j < IPP; j++) load_to_lds16_nt(base[u] + ksrc[j], kbuf + stage * STAGE + u * PAGE_KB + j * 1024);
+    }
+  };
+  auto load_v = [&](u32x4 (&vr)[2][DB]) {
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++) vr[u][bb] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base[u] + (size_t)16 * D + (bb * 32 + l32) * 16 + lh * 8));
+  };
+
+  // Q^T operand: column l32 is row l32 of the item
+  V qf[KSTEPS];
+  const int vrow = it.row0 + min(l32, it.rows - 1), row = vrow / c.heads, head = kvh * c.heads + vrow % c.heads;
+  const Seen seen{c.plan.masks + (size_t)row * AT_MASK, it.cached / OP_PAGE, it.pg1};
+  const int mixed = min(max(it.cached / OP_PAGE - it.pg0, 0), npg) >> 1;         // the first block that is not two pages of context of the item's
+  {
+    const T* q = c.q + (long long)row * c.q_stride + head * D + lh * 8;
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++) {
+      if (c.q_vec) qf[kk] = *reinterpret_cast<const V*>(q + kk * 16);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; e++) qf[kk][e] = q[kk * 16 + e];
+    }
+  }
+  const int tok = (l32 & 3) | (((l32 >> 3) & 1) << 2) | (((l32 >> 2) & 1) << 3);
+  const int krow = (l32 >> 4) * PAGE_KB + tok * ROWB;
+  int kslot[KSTEPS];
+#pragma unroll
+  for (int kk = 0; kk < KSTEPS; kk++) kslot[kk] = krow + ((2 * kk + lh) ^ swz(tok)) * 16;
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int bb = 0; bb < DB; bb++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) o[bb][r] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f;
+
+  auto scores = [&](int stage, f32x16& s) {
+    const unsigned char* kst = kbuf + stage * STAGE;
+#pragma unroll
+    for (int r = 0; r < 16; r++) s[r] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk++) s = Mfma<T>::mul(*reinterpret_cast<const V*>(kst + kslot[kk]), qf[kk], s);
+  };
+  auto softmax_pv = [&](int b, f32x16& s, u32x4 (&vr)[2][DB]) {
+    if (b >= mixed) {                                 // wave-uniform
+      const int pg = it.pg0 + 2 * b;
+      const unsigned see = seen.page(pg) >> (8 * lh) & 0xFF | (seen.page(pg + 1) >> (8 * lh) & 0xFF) << 8;
+#pragma unroll
+      for (int r = 0; r < 16; r++)                    // register r: page r >> 3 of the pair, token 8 * half + (r & 7)
+        if (!(see >> r & 1)) s[r] = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 2; u++)
+#pragma unroll
+        for (int bb = 0; bb < DB; bb++) {
+          V v = __builtin_bit_cast(V, vr[u][bb]);
+          odd |= without_odd<V, T>(v, pg + u < it.pg1 ? it.len - (pg + u) * OP_PAGE - 8 * lh : 0);
+          vr[u][bb] = __builtin_bit_cast(u32x4, v);
+        }
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; r++) mx = fmaxf(mx, s[r]);
+    mx = half_swap_max_f(mx);
+    if (__any(mx > m_ref)) {                         // wave-uniform
+      const float m_new = fmaxf(m_ref, mx);
+      const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c.scale_log2e);
+      m_ref = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[bb][r] *= corr;
+    }
+    const float nm = m_ref == -INFINITY ? 0.f : fmaf(-m_ref, c.scale_log2e, AS_LIFT<T>);
+    float rs = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c.scale_log2e, nm));
+      s[r] = p;
+      rs += p;
+    }
+    l_run += rs;
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      V pb, pr;
+      in_two(s, 8 * u, pb, pr);
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++) o[bb] = Mfma<T>::mul(__builtin_bit_cast(V, vr[u][bb]), pb, o[bb]);
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++) o[bb] = Mfma<T>::mul(__builtin_bit_cast(V, vr[u][bb]), pr, o[bb]);
+    }
+  };
+  auto fence = [] { __asm__ volatile("" ::: "memory"); __builtin_amdgcn_sched_barrier(0); };
+  u32x4 va[2][DB], vb[2][DB];
+  auto step = [&](int i, int stage, u32x4 (&vr)[2][DB]) {
+    if (i + 1 < nblk) wait_vmem<LOADS>(); else wait_vmem<0>();
+    fence();
+    f32x16 s;
+    scores(stage, s);
+    if (i + 2 < nblk) {
+      __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): every K operand of this block has been read
+      fence();
+      issue_k(i + 2, stage);
+    }
+    softmax_pv(i, s, vr);
+    if (i + 2 < nblk) load_v(vr);
+  };
+  issue_k(0, 0); load_v(va);
+  if (nblk > 1) { issue_k(1, 1); load_v(vb); }
+  for (int i = 0; i < nblk; i += 2) {
+    step(i, 0, va);
+    if (i + 1 < nblk) step(i + 1, 1, vb);
+  }
+  if (__any(odd)) add_odd<T, D>(o, c, it, it.pg0 + 2 * mixed, table - it.pg0, seen, kvh, lh);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (__any(bad)) l_run = NAN;
+
+  // a lane has four elements in a row of its row's output, 32 bb + 8 r4 + 4 lh
+  if (l32 < it.rows) {
+    const float m2 = fmaf(m_ref, c.scale_log2e, -AS_LIFT<T>);
+    auto four = [&](int bb, int r4) { return f32x4{o[bb][4 * r4], o[bb][4 * r4 + 1], o[bb][4 * r4 + 2], o[bb][4 * r4 + 3]}; };
+    if (it.part < 0) {
+      T* out = c.out + (long long)row * c.out_stride + head * D + 4 * lh;
+      const float f = 1.f / ((1.f + AS_EXTRA<T>) * l_run);
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; r4++) store4(out + bb * 32 + 8 * r4, four(bb, r4), f, c.out_vec);
+      if (lh == 0 && c.lse) c.lse[(long long)row * c.n_q + head] = LN2 * (m2 + __builtin_amdgcn_logf(l_run));
+    } else {
+      const size_t at = (size_t)(it.part + l32) * c.n_kv + kvh;
+      float* out = c.plan.outs + at * D + 4 * lh;
+#pragma unroll
+      for (int bb = 0; bb < DB; bb++)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; r4++) *reinterpret_cast<f32x4*>(out + bb * 32 + 8 * r4) = four(bb, r4);
+      if (lh == 0) c.plan.stats[at] = f32x2{m2, l_run};
+    }
+  }
+}
+
+// ---- wide items, a workgroup: every wave takes 32 rows over all the pages. Tiles of four pages go global -> LDS, two stages deep, a page
+// a wave; products, order of the tokens and softmax as in attn_prefill.hip, whose queries lie in a row where these come from any node.
+template <typename T, int D>
+__device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>& c, const Item& it, int kvh) {
+  typedef typename Mfma<T>::V V;
+  constexpr int KSTEPS = D / 16, DB = D / 32;
+  constexpr int ROWB = D * 2, CPR = D / 8, RPI = 64 / CPR, IPP = 16 / RPI;     // K row bytes, 16-byte chunks, rows per load, loads per page
+  constexpr int PAGE = 16 * ROWB, TILE = 4 * PAGE, STAGE = 2 * TILE;           // bytes of a K (or V^T) page, tile; of a stage
+  const int tid = fresh(threadIdx.x), lane = tid & 63, l32 = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int npg = it.pg1 - it.pg0, tiles = (npg + 3) >> 2;
+  const int* table = c.tables + (long long)it.request * c.table_stride + it.pg0;
+  const int my_rows = min(it.rows - wave * 32, 32);                            // none or fewer: the wave only fetches
+
+  V qf[KSTEPS];
+  const int vrow = it.row0 + min(wave * 32 + l32, it.rows - 1);
+  const Seen seen{c.plan.masks + (size_t)(vrow / c.heads) * AT_MASK, it.cached / OP_PAGE, it.pg1};
+  {
+    const T* q = c.q + (long long)(vrow / c.heads) * c.q_stride + (kvh * c.heads + vrow % c.heads) * D + 8 * lh;
+#pragma unroll
+    for (int j = 0; j < KSTEPS; j++) {
+      if (c.q_vec) qf[j] = *reinterpret_cast<const V*>(q + 16 * j);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; e++) qf[j][e] = q[16 * j + e];
+    }
+  }
+  // This wave's page of tile kt; past the last page that page again, whose products are left out.
+  bool bad = false, odd = false;
+  const size_t page_stride = (size_t)c.n_kv * 2 * OP_PAGE * D;
+  const T* pool_h = c.pool + (size_t)kvh * 2 * OP_PAGE * D;
+  auto page_id = [&](int kt) {
+    const int page = table[min(kt * 4 + wave, npg - 1)];
+    const bool out = (unsigned)page >= (unsigned)c.pool_pages;
+    bad |= out;
+    return out ? 0 : page;
+  };
+  unsigned k_off[IPP];
+#pragma unroll
+  for (int j = 0; j < IPP; j++) {
+    const int row = j * RPI + lane / CPR, swz = D == 128 ? row : (row >> 1) & 7;
+    k_off[j] = (unsigned)row * ROWB + (unsigned)((lane % CPR) ^ swz) * 16u;
+  }
+  unsigned char* arena = smem + AS_LDS_BASE;
+  auto issue = [&](int stage, int page) {
+    const T* pb = pool_h + (size_t)__builtin_amdgcn_readfirstlane(page) * page_stride;
+    unsigned char* dst = arena + stage * STAGE + wave * PAGE;
+#pragma unroll
+    for (int j = 0; j < IPP; j++) lds_dma16(pb, k_off[j], dst + j * 1024);
+#pragma unroll
+    for (int j = 0; j < IPP; j++) lds_dma16(pb + (size_t)16 * D, (unsigned)(j * 1024 + lane * 16), dst + TILE + j * 1024);
+  };
+  const int tok = (l32 & 3) | (((l32 >> 3) & 1) << 2) | (((l32 >> 2) & 1) << 3);
+  const int k_row = (l32 >> 4) * PAGE + tok * ROWB;
+  int k_slot[KSTEPS];
+#pragma unroll
+  for (int j = 0; j < KSTEPS; j++) k_slot[j] = k_row + ((2 * j + lh) ^ (D == 128 ? tok : (tok >> 1) & 7)) * 16;
+  const int v_lane = TILE + l32 * 32 + lh * 16;          // V^T operand: d row l32 of a 32-row block, tokens 8 lh .. of a page
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int b = 0; b < DB; b++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) o[b][r] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f;
+  issue(0, page_id(0));
+  int next_page = page_id(1);
+  // whole: four pages of context; otherwise some hold nodes, or lie behind the item's
+  auto tile = [&](int kt, auto whole) {
+    const unsigned char* st = arena + (kt & 1) * STAGE;
+    const int here = decltype(whole)::value ? 4 : min(npg - kt * 4, 4);        // pages of the tile
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) s[kb][r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+    {
+      V kf[2][2];
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++) kf[0][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[0]);
+#pragma unroll
+      for (int j = 0; j < KSTEPS; j++) {
+        const int a = j & 1, b = a ^ 1;
+        if (j + 1 < KSTEPS) {
+#pragma unroll
+          for (int kb = 0; kb < 2; kb++) kf[b][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[j + 1]);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) s[kb] = Mfma<T>::mul(kf[a][kb], qf[j], s[kb]);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+      for (int j = 0; j + 1 < KSTEPS; j++) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+    }
+    V vf[2][DB];                                           // first V^T operands: in flight during the softmax arithmetic
+#pragma unroll
+    for (int b = 0; b < DB; b++) vf[0][b] = *reinterpret_cast<const V*>(st + v_lane + b * 1024);
+    if constexpr (!decltype(whole)::value) {
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++) {
+        const int pg = it.pg0 + kt * 4 + 2 * kb;
+        const unsigned see = seen.page(pg) >> (8 * lh) & 0xFF | (seen.page(pg + 1) >> (8 * lh) & 0xFF) << 8;
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          if (!(see >> r & 1)) s[kb][r] = -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[kb][r]);
+    mx = half_swap_max_f(mx);
+    // The reference moves when a score has outgrown it by 2^8, by which probabilities and their sums may then exceed 1: two numbers of the type, and 32 bits,
+    // hold them as well there.
+    if (__any((mx - m_ref) * c.scale_log2e > AS_RISE)) {                       // wave-uniform
+      const float m_new = fmaxf(m_ref, mx);
+      const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_ref - m_new) * c.scale_log2e);
+      m_ref = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int b = 0; b < DB; b++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[b][r] *= corr;
+    }
+    const float nm = (m_ref == -INFINITY) ? 0.f : fmaf(-m_ref, c.scale_log2e, AS_LIFT<T>);
+    float rs = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c.scale_log2e, nm));
+        s[kb][r] = p;
+        rs += p;
+      }
+    l_run += rs;                                                               // this half's keys; halves are added at the end
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      const int a = g & 1, b2 = a ^ 1;
+      if (g + 1 < 4) {
+#pragma unroll
+        for (int b = 0; b < DB; b++) vf[b2][b] = *reinterpret_cast<const V*>(st + v_lane + (g + 1) * PAGE + b * 1024);
+      }
+      if constexpr (!decltype(whole)::value) {
+#pragma unroll
+        for (int b = 0; b < DB; b++) odd |= without_odd<V, T>(vf[a][b], g < here ? it.len - (it.pg0 + kt * 4 + g) * OP_PAGE - 8 * lh : 0);
+      }
+      V pb, pr;
+      in_two(s[g >> 1], 8 * (g & 1), pb, pr);
+      if (decltype(whole)::value || g < here) {
+#pragma unroll
+        for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pb, o[b]);
+#pragma unroll
+        for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pr, o[b]);
+      }
+    }
+    if constexpr (decltype(whole)::value) {
+#pragma unroll
+      for (int g = 0; g + 1 < 4; g++) {
+        __builtin_amdgcn_sched_group_barrier(0x100, DB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * DB, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 2 * DB, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto landed = [&](int kt) {                              // every wave waits for its own page, and nobody reads the other stage any more
+    wait_vmem<0>();
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 1 < tiles) {
+      issue((kt + 1) & 1, next_page);
+      next_page = page_id(kt + 2);
+    }
+  };
+  const int whole = max(min(it.cached / OP_PAGE, it.pg1) - it.pg0, 0) >> 2;
+  for (int kt = 0; kt < whole; kt++) {
+    landed(kt);
+    if (my_rows > 0) tile(kt, std::true_type{});           // wave-uniform
+  }
+  for (int kt = whole; kt < tiles; kt++) {
+    landed(kt);
+    if (my_rows > 0) tile(kt, std::false_type{});
+  }
+  if (__any(odd)) add_odd<T, D>(o, c, it, it.pg0 + 4 * whole, table - it.pg0, seen, kvh, lh);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (__syncthreads_or(bad)) l_run = NAN;                // LDS now takes the output
+  if (my_rows > 0) {
+    // whole rows through LDS: 16-byte chunks, swizzled by row
+    constexpr int OROWB = D * 4, OCPR = OROWB / 16, ORPI = 64 / OCPR;
+    unsigned char* buf = arena + wave * 32 * OROWB;
+    const int lane = fresh(tid & 63), l32 = lane & 31, lh = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < DB; b++)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; r4++)
+        *reinterpret_cast<f32x4*>(buf + l32 * OROWB + ((b * 8 + 2 * r4 + lh) ^ (l32 % 16)) * 16) = f32x4{o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int r0 = lane / OCPR, ch = lane % OCPR;
+    const float m2 = fmaf(m_ref, c.scale_log2e, -AS_LIFT<T>), f = 1.f / ((1.f + AS_EXTRA<T>) * l_run);
+#pragma unroll
+    for (int i = 0; i < 32 / ORPI; i++) {
+      const int r = i * ORPI + r0;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(buf + r * OROWB + (ch ^ (r % 16)) * 16);
+      const float fr = __shfl(f, r, 64);
+      if (r >= my_rows) continue;
+      if (it.part < 0) {
+        const int v = it.row0 + wave * 32 + r;
+        store4(c.out + (long long)(v / c.heads) * c.out_stride + (kvh * c.heads + v % c.heads) * D + ch * 4, x, fr, c.out_vec);
+      } else {
+        *reinterpret_cast<f32x4*>(c.plan.outs + ((size_t)(it.part + wave * 32 + r) * c.n_kv + kvh) * D + ch * 4) = x;
+      }
+    }
+    if (lane < my_rows) {
+      if (it.part >= 0) c.plan.stats[(size_t)(it.part + wave * 32 + lane) * c.n_kv + kvh] = f32x2{m2, l_run};
+      else if (c.lse) c.lse[(long long)(vrow / c.heads) * c.n_q + kvh * c.heads + vrow % c.heads] = LN2 * (m2 + __builtin_amdgcn_logf(l_run));
+    }
+  }
+  __syncthreads();                                       // before the next item's K lands there
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 2) attn_tree_kernel(TreeCall<T> c) {
+  __shared__ __align__(16) unsigned char smem[attn_tree_lds<D>()];
+  // With 8 KV heads a head's workgroups are all on one XCD: the tiles of a request find each other's pages in its L2.
+  const int slot = blockIdx.x / c.n_kv, kvh = blockIdx.x % c.n_kv;
+  const Range r = c.plan.ranges[slot * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
+  if (c.plan.header->tag != c.tag || r.first.rows == 0) return;
+  Item it = r.first;
+  for (int i = r.next;; i++) {
+    if (it.rows > AT_ROWS) run_wide<T, D>(smem, c, it, kvh);
+    else run_narrow<T, D>(smem, c, it, kvh);
+    if (i >= r.end) break;
+    it = c.plan.items[i];
+  }
+}
+
+// Joins the partial results of a (row, query head): WAVES waves each, a lane four elements of every 256 / D-th part (of a wave's share).
+template <typename T, int D, int WAVES>
+__global__ void __launch_bounds__(256) attn_tree_join_kernel(TreeCall<T> c) {
+  constexpr int LANES = D / 4, APART = 64 / LANES * WAVES;       // lanes of a part, parts side by side
+  __shared__ f32x4 sums[WAVES > 1 ? WAVES : 1][LANES];
+  __shared__ float ls[WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + wave;
+  if (at >= c.max_rows * c.n_q) return;
+  const int row = at / c.n_q, head = at % c.n_q, kvh = head / c.heads, h = head % c.heads;
+  const Header& hd = *c.plan.header;
+  const bool planned = hd.tag == c.tag && hd.rows >= 0;
+  if (planned && row >= hd.rows) return;
+  const int owner = planned ? c.plan.owners[row] : 0;
+  int count = 0, base = 0, step = 0;
+  bool bad = !planned;
+  if (planned && owner >= 0) {
+    const Request q = c.plan.requests[owner];
+    bad = q.bad;
+    if (!bad) {
+      const Line& l = hd.lines[q.kind];
+      const int v = row * c.heads + h, at = q.at + (v - q.row0) / q.per * (q.pages + l.start);
+      count = l.pieces(at, q.pages);
+      if (count == 1) return;                                    // finished by its one piece
+      step = q.kind ? AT_ROWS : AT_TILE;
+      base = (q.kind ? hd.narrow_part : 0) + v + step * l.first(at, q.pages);
+    }
+  }
+  auto row_of = [&](int j) { return (size_t)(base + j * step) * c.n_kv + kvh; };
+  float m = -INFINITY;
+  for (int j = lane; j < count; j += 64) m = fmaxf(m, c.plan.stats[row_of(j)][0]);
+  m = wave_max(m);
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const int first = (WAVES > 1 ? wave * (64 / LANES) : 0) + lane / LANES, e4 = lane % LANES * 4;
+#pragma unroll 4
+  for (int j = first; j < count; j += APART) {
+    const size_t part = row_of(j);
+    const f32x2 st = c.plan.stats[part];
+    const f32x4 x = *reinterpret_cast<const f32x4*>(c.plan.outs + part * D + e4);
+    const float w = st[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - m);
+    l += st[0] == -INFINITY ? st[1] : st[1] * w;                 // 0 of a part without scores above -inf, or NaN
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] += x[e] * w;
+  }
+#pragma unroll
+  for (int s = LANES; s < 64; s <<= 1) {
+    l += __shfl_xor(l, s, 64);
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] += __shfl_xor(o[e], s, 64);
+  }
+  if constexpr (WAVES > 1) {
+    if (lane < LANES) sums[wave][lane] = o;
+    if (lane == 0) ls[wave] = l;
+    __syncthreads();
+    if (wave > 0) return;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) l += ls[w];
+    if (lane < LANES) {
+      o = sums[0][lane];
+#pragma unroll
+      for (int w = 1; w < WAVES; w++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] += sums[w][lane][e];
+    }
+  }
+  if (lane < LANES) {
+    const bool none = count == 0;                      // no node: zeros, and the logarithm of an empty sum
+    const f32x4 x = bad ? f32x4{NAN, NAN, NAN, NAN} : none ? f32x4{0.f, 0.f, 0.f, 0.f} : o;
+    store4(c.out + (long long)row * c.out_stride + head * D + e4, x, none ? 1.f : 1.f / ((1.f + AS_EXTRA<T>) * l), c.out_vec);
+    if (lane == 0 && c.lse) c.lse[(long long)row * c.n_q + head] = bad ? NAN : none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
+  }
+}
+
+template <typename T, int D>
+hipError_t launch_attn(hipStream_t s, const TreeCall<T>& c) {
+  hipError_t e = launch(attn_tree_kernel<T, D>, dim3(slots_of(c.n_kv) * c.n_kv), dim3(256), 0, s, c);
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)c.max_rows * c.n_q;
+  if (rows <= AT_JOIN_ROWS) return launch(attn_tree_join_kernel<T, D, 4>, dim3((unsigned)rows), dim3(256), 0, s, c);
+  return launch(attn_tree_join_kernel<T, D, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, c);
+}
+
+bool sizes_ok(int n, int max_rows, int n_q, int n_kv, int d) {
+  return n >= 0 && n <= OP_MAX_REQUESTS && max_rows >= 0 && max_rows <= AT_MAX_ROWS && n_kv >= 1 && n_kv <= AT_SLOTS / 2 && n_q >= n_kv && n_q % n_kv == 0 && n_q / n_kv <= AT_ROWS &&
+         (d == 64 || d == 128);
+}
+// The batch's description, without what a call of one layer adds.
+int check_batch(const sts_tree_batch* b, Plan* plan) {
+  if (!b || (b->dtype != STS_BF16 && b->dtype != STS_F16) || !sizes_ok(b->n_requests, b->max_rows, b->n_q, b->n_kv, b->d)) return STS_EINVAL;
+  if (b->pool_pages < 0 || b->max_pages < 0 || b->max_pages > (1 << 26) || b->table_stride < b->max_pages) return STS_EINVAL;
+  // the lines' lengths stay within 32 bits
+  if (max_segments(b->n_requests, b->max_rows, b->n_q / b->n_kv) * (b->max_pages + (int64_t)AT_WIDE_START) > (1 << 30)) return STS_EINVAL;
+  if (b->n_requests == 0 || b->max_rows == 0) return STS_OK;
+  if (!b->cached || !b->row_starts || !b->parents || (b->max_pages > 0 && !b->tables)) return STS_EINVAL;
+  if (b->positions && (b->positions == b->parents || b->positions == b->cached || b->positions == b->row_starts)) return STS_EINVAL;      // read by workgroups that start late
+  if (!b->workspace || !aligned(b->workspace, 256)) return STS_EINVAL;
+  if ((int64_t)lay_out(reinterpret_cast<unsigned char*>(b->workspace), b->n_requests, b->max_rows, b->n_q, b->n_kv, b->d, plan) > b->workspace_bytes) return STS_EINVAL;
+  return STS_OK;
+}
+
+template <typename T>
+int attn_tree(const sts_tree_batch* b, const Plan& plan, const void* q, int64_t q_stride, const void* pool, void* out, int64_t out_stride, float* lse, float scale, hipStream_t s) {
+  const bool q_vec = aligned(q, 16) && q_stride % 8 == 0, out_vec = aligned(out, 8) && out_stride % 4 == 0;
+  const TreeCall<T> c{reinterpret_cast<const T*>(q), q_stride, reinterpret_cast<const T*>(pool), reinterpret_cast<T*>(out), out_stride, lse, b->tables, b->table_stride,
+                      b->max_rows, b->n_requests, b->n_q, b->n_kv, b->n_q / b->n_kv, b->pool_pages, scale * LOG2E, q_vec, out_vec, sizes_tag(*b), plan};
+  return op_result(b->d == 128 ? launch_attn<T, 128>(s, c) : launch_attn<T, 64>(s, c));
+}
+
+}  // namespace
+}  // namespace sts
+
+using namespace sts;
+
+extern "C" int64_t sts_attn_tree_workspace(int32_t n_requests, int32_t max_rows, int32_t n_q, int32_t n_kv, int32_t d) {
+  if (!sizes_ok(n_requests, max_rows, n_q, n_kv, d)) return -1;
+  return (int64_t)lay_out(nullptr, n_requests, max_rows, n_q, n_kv, d, nullptr);
+}
+
+extern "C" int sts_op_attn_tree_plan(const sts_tree_batch* b, void* stream) {
+  Plan plan{};
+  const int rc = check_batch(b, &plan);
+  if (rc != STS_OK || b->n_requests == 0 || b->max_rows == 0) return rc;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  OnStreamDevice dev(s);
+  if (dev.error() != hipSuccess) return op_result(dev.error());
+  const PlanCall c{sizes_tag(*b), b->n_requests, b->max_rows, b->n_q / b->n_kv, slots_of(b->n_kv), b->max_pages, b->cached, b->row_starts, b->parents, b->positions, plan};
+  return op_result(launch(attn_tree_plan_kernel, dim3(1 + b->n_requests), dim3(AT_PLAN_THREADS), 0, s, c));
+}
+
+extern "C" int sts_op_attn_tree(const sts_tree_batch* b, const void* q, int64_t q_stride, const void* pool, void* out, int64_t out_stride, float* lse, float scale, void* stream) {
+  Plan plan{};
+  const int rc = check_batch(b, &plan);
+  if (rc != STS_OK || b->n_requests == 0 || b->max_rows == 0) return rc;
+  const int64_t row = (int64_t)b->n_q * b->d;
+  if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || !pool || !aligned(pool, 16) || b->pool_pages < 1 || (b->max_rows > 1 && (q_stride < row || out_stride < row))) return STS_EINVAL;
+  if (!(scale >= 0.f) || scale > 1e30f) return STS_EINVAL;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  OnStreamDevice dev(s);
+  if (dev.error() != hipSuccess) return op_result(dev.error());
+  const float sc = scale == 0.f ? 1.f / sqrtf((float)b->d) : scale;
+  return b->dtype == STS_BF16 ? attn_tree<bf16>(b, plan, q, q_stride, pool, out, out_stride, lse, sc, s) : attn_tree<f16>(b, plan, q, q_stride, pool, out, out_stride, lse, sc, s);
+}

@@ -1,4 +1,4 @@
-// Rotary positions of Q and K rows, and the append of K and V rows to their pages.
+// Rotary positions of Q and K rows, and the append of K and V rows to their pages; the same behind a norm of each head.
 //
 // Pair i of a head's first R elements -- (i, i + R/2), or (2i, 2i + 1) interleaved -- turns by the angle position * f_i, where f_i is
 // theta^(-2i/R) scaled for long contexts (rope_turns below); elements from R on pass. One pass: rows are read once and written once, to
@@ -8,6 +8,9 @@
 // whole turns exactly: the angle of position 2^20 is as good as that of position 1 (fp32 products are off by 0.06 radians there). The
 // host makes the fractions in 64 bits and hands them over as a kernel argument; a workgroup computes its rows' cosines and sines once
 // and keeps them in LDS for all heads.
+//
+// Norms of heads: y = x / sqrt(mean(x^2) + eps) * gain before the rotation, in 32 bits. A head's row is then a run of neighbouring lanes (a power of two of them; those
+// beyond its vectors hold none), which add up their squares; the rows are still read once. Rows that do not come in vectors take a wave each and are read twice.
 //
 // Bound by memory for prefills (8192 rows of 32 + 8 heads of 128: 201 MB in 44 us, 4.6 TB/s, where a plain copy takes 38), by latency for decodes
 // (64 rows 4 us). V columns stored 1 KB in a row by neighbouring lanes, both halves of a page at once, were level.
@@ -81,6 +84,9 @@ bool rope_turns(const sts_rope& r, RopeTurns* t) {
   return true;
 }
 
+constexpr int RP_NORM_D = 512;                        // elements of a head that is normed
+struct HeadNorms { const void *q_gain, *k_gain; int dtype, lanes; float eps, offset; };      // lanes: of a head's row
+
 struct RopeCall {
   sts_rope_rows a;
   int pairs, interleaved, turn_parts;
@@ -102,10 +108,19 @@ __device__ __forceinline__ f32x2 cos_sin(unsigned turn) {
 template <typename T, int N> struct VecOf { typedef T type __attribute__((ext_vector_type(N))); };
 template <typename T> struct VecOf<T, 1> { typedef T type; };
 
-// ROWS: rows of a workgroup (1, or a page's 16). E: elements at a time, in aligned vectors; pairs come in whole vectors.
-template <typename T, int ROWS, int E>
-__global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns turns) {
-  constexpr bool VEC = E > 1;
+__device__ __forceinline__ float gain_at(const void* gain, int dtype, int e) {
+  return !gain ? 1.f : dtype == STS_F32 ? reinterpret_cast<const float*>(gain)[e] : dtype == STS_BF16 ? (float)reinterpret_cast<const bf16*>(gain)[e] : (float)reinterpret_cast<const f16*>(gain)[e];
+}
+// The sum over runs of `lanes` neighbouring lanes.
+__device__ __forceinline__ float run_sum(float x, int lanes) {
+  for (int s = 1; s < lanes; s <<= 1) x += __shfl_xor(x, s, 64);
+  return x;
+}
+
+// ROWS: rows of a workgroup (1, or a page's 16). E: elements at a time, in aligned vectors; pairs come in whole vectors. N: HeadNorms, or none.
+template <typename T, int ROWS, int E, typename... N>
+__global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns turns, N... norms) {
+  constexpr bool VEC = E > 1, NORM = sizeof...(N) > 0;
   typedef typename VecOf<T, E>::type V;
   const sts_rope_rows& a = c.a;
   __shared__ f32x2 trig[ROWS * RP_MAX_PAIRS];          // [row][pair]: cosine, sine
@@ -123,7 +138,11 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
   if (turns_rows) {
     // Tasks of a head's row: a pair (of vectors), or one vector of neighbours or of elements that pass. The workgroup's part of all of them
     const int pair_tasks = !VEC ? P : c.interleaved ? d / E : P / E, tasks = !VEC ? P + d - R : c.interleaved ? pair_tasks : pair_tasks + (d - R) / E;
-    const int of_row = (a.n_q + a.n_kv) * tasks, t0 = (int)((long long)rows * of_row * blockIdx.y / c.turn_parts), t1 = (int)((long long)rows * of_row * (blockIdx.y + 1) / c.turn_parts);
+    int lanes = 1;                                     // of a head's row; whole ones are then a workgroup's
+    if constexpr (NORM) lanes = (norms.lanes, ...);
+    const int of_row = (a.n_q + a.n_kv) * (NORM ? lanes : tasks);
+    const long long units = (long long)rows * (NORM ? a.n_q + a.n_kv : of_row);
+    const int t0 = (int)(units * blockIdx.y / c.turn_parts) * lanes, t1 = (int)(units * (blockIdx.y + 1) / c.turn_parts) * lanes;
     const int r_first = t0 / of_row, r_end = (t1 + of_row - 1) / of_row;
     for (int i = tid + r_first * P; i < r_end * P; i += RP_THREADS) {
       const int r = ROWS == 1 ? 0 : i / P, p = i - r * P;
@@ -131,10 +150,23 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
       const f32x2 cs = cos_sin((unsigned)(phase >> 32));
       trig[i] = f32x2{cs[0] * c.magnitude, cs[1] * c.magnitude};
     }
+    __shared__ float gains[2][NORM ? RP_NORM_D : 1];
+    if constexpr (NORM) {
+      const HeadNorms n = (norms, ...);
+      for (int e = tid; e < d; e += RP_THREADS) {
+        gains[0][e] = n.q_gain ? gain_at(n.q_gain, n.dtype, e) + n.offset : 1.f;
+        gains[1][e] = n.k_gain ? gain_at(n.k_gain, n.dtype, e) + n.offset : 1.f;
+      }
+    }
+    auto root = [&](float squares) {
+      float eps = 0.f;
+      if constexpr (NORM) eps = (norms.eps, ...);
+      return __builtin_amdgcn_rsqf(squares / (float)d + eps);
+    };
     struct Task { int r, h, task; };                   // heads from n_q on are K's
     auto task_of = [&](int t) {
-      const int r = ROWS == 1 ? 0 : t / of_row, q = t - r * of_row, h = q / tasks;
-      return Task{r, h, q - h * tasks};
+      const int r = ROWS == 1 ? 0 : t / of_row, q = t - r * of_row, h = q / (NORM ? lanes : tasks);
+      return Task{r, h, q - h * (NORM ? lanes : tasks)};
     };
     auto source = [&](const Task& k) {
       return k.h < a.n_q ? reinterpret_cast<const T*>(a.q) + (row0 + k.r) * a.q_stride + k.h * d : reinterpret_cast<const T*>(a.k) + (row0 + k.r) * a.k_stride + (k.h - a.n_q) * d;
@@ -157,6 +189,9 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
         for (int u = 0; u < DEPTH; u++) {
           if (t + u * RP_THREADS >= t1) break;
           k[u] = task_of(t + u * RP_THREADS);
+          if constexpr (NORM) {
+            if (k[u].task >= tasks) continue;          // a lane beyond the vectors
+          }
           const T* src = source(k[u]) + place_in(k[u]);
           x[u] = *reinterpret_cast<const V*>(src);
           if (is_pair(k[u])) y[u] = *reinterpret_cast<const V*>(src + P);
@@ -172,7 +207,43 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
           const Targets to = targets(k[u]);
           const f32x2* tr = trig + k[u].r * P;
           const int at = place_in(k[u]);
-          if (is_pair(k[u])) {
+          if constexpr (NORM) {
+            const bool pair = is_pair(k[u]), here = k[u].task < tasks;
+            float v[E], w[E], squares = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+              v[e] = (float)x[u][e]; w[e] = (float)y[u][e];
+              squares += here ? v[e] * v[e] + (pair ? w[e] * w[e] : 0.f) : 0.f;
+            }
+            const float f = root(run_sum(squares, lanes));
+            if (!here) continue;
+            const float* g = gains[k[u].h >= a.n_q] + at;
+#pragma unroll
+            for (int e = 0; e < E; e++) v[e] = v[e] * f * g[e];
+            if (pair) {
+#pragma unroll
+              for (int e = 0; e < E; e++) {
+                w[e] = w[e] * f * g[P + e];
+                const f32x2 cs = tr[at + e];
+                float p, q;
+                rotate_pair(v[e], w[e], cs[0], cs[1], &p, &q);
+                x[u][e] = (T)p; y[u][e] = (T)q;
+              }
+              if (to.to_row) *reinterpret_cast<V*>(to.row + at + P) = y[u];
+              if (to.to_page) *reinterpret_cast<V*>(to.page + at + P) = y[u];
+            } else if (at < R) {
+#pragma unroll
+              for (int e = 0; e < E; e += 2) {
+                const f32x2 cs = tr[(at + e) / 2];
+                float p, q;
+                rotate_pair(v[e], v[e + 1], cs[0], cs[1], &p, &q);
+                x[u][e] = (T)p; x[u][e + 1] = (T)q;
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < E; e++) x[u][e] = (T)v[e];
+            }
+          } else if (is_pair(k[u])) {
 #pragma unroll
             for (int e = 0; e < E; e++) {
               float v, w;
@@ -193,6 +264,35 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
           }
           if (to.to_row) *reinterpret_cast<V*>(to.row + at) = x[u];
           if (to.to_page) *reinterpret_cast<V*>(to.page + at) = x[u];
+        }
+      }
+    } else if constexpr (NORM) {                       // 64 lanes a head's row
+      __syncthreads();
+      const int lane = tid & 63;
+      for (int t = t0 + tid; t < t1; t += RP_THREADS) {
+        Task k = task_of(t);
+        const T* src = source(k);
+        const Targets to = targets(k);
+        const float* g = gains[k.h >= a.n_q];
+        float squares = 0.f;
+        for (int e = lane; e < d; e += 64) squares += (float)src[e] * (float)src[e];
+        const float f = root(run_sum(squares, 64));
+        auto put = [&](int e, float v) {
+          if (to.to_row) to.row[e] = (T)v;
+          if (to.to_page) to.page[e] = (T)v;
+        };
+        for (k.task = lane; k.task < tasks; k.task += 64) {
+          if (k.task < P) {
+            const int e = c.interleaved ? 2 * k.task : k.task, w = c.interleaved ? e + 1 : e + P;
+            const f32x2 cs = trig[k.r * P + k.task];
+            float p, q;
+            rotate_pair((float)src[e] * f * g[e], (float)src[w] * f * g[w], cs[0], cs[1], &p, &q);
+            put(e, p);
+            put(w, q);
+          } else {
+            const int e = R + k.task - P;
+            put(e, (float)src[e] * f * g[e]);
+          }
         }
       }
     } else {
@@ -292,45 +392,47 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(RopeCall c, RopeTurns 
   }
 }
 
-template <typename T, int ROWS, int E>
-hipError_t launch_rope(hipStream_t s, const RopeCall& c, const RopeTurns& t) {
+template <typename T, int ROWS, int E, typename... N>
+hipError_t launch_rows(hipStream_t s, const RopeCall& c, const RopeTurns& t, const N&... norms) {
   const int blocks = (c.a.rows + ROWS - 1) / ROWS, heads = c.a.n_q + c.a.n_kv;
   RopeCall call = c;
   call.turn_parts = ROWS == 1 ? (heads + RP_HEADS - 1) / RP_HEADS : std::max(1, std::min({(RP_WORKGROUPS + blocks - 1) / blocks, heads, RP_PARTS}));
   const int v_parts = !c.a.pool ? 0 : ROWS == 1 ? 1 : std::max(1, std::min({(RP_WORKGROUPS + blocks - 1) / blocks / 2, c.a.n_kv, RP_PARTS}));
-  return launch(rope_kernel<T, ROWS, E>, dim3(blocks, call.turn_parts + v_parts), dim3(RP_THREADS), 0, s, call, t);
+  return launch(rope_kernel<T, ROWS, E, N...>, dim3(blocks, call.turn_parts + v_parts), dim3(RP_THREADS), 0, s, call, t, norms...);
 }
-template <typename T, int E>
-hipError_t launch_rope(hipStream_t s, const RopeCall& c, const RopeTurns& t) {
-  return c.a.rows < RP_PAGE_ROWS ? launch_rope<T, 1, E>(s, c, t) : launch_rope<T, OP_PAGE, E>(s, c, t);
+template <typename T, int E, typename... N>
+hipError_t launch_vectors(hipStream_t s, const RopeCall& c, const RopeTurns& t, const N&... norms) {
+  return c.a.rows < RP_PAGE_ROWS ? launch_rows<T, 1, E>(s, c, t, norms...) : launch_rows<T, OP_PAGE, E>(s, c, t, norms...);
 }
-template <typename T>
-hipError_t launch_rope(hipStream_t s, const RopeCall& c0, const RopeTurns& t) {
+// Lanes of a head's row in vectors of e elements: a power of two
+int norm_lanes(const RopeCall& c, int e) {
+  const int R = 2 * c.pairs, vectors = c.interleaved ? c.a.d / e : c.pairs / e + (c.a.d - R) / e;
+  int lanes = 1;
+  while (lanes < vectors) lanes *= 2;
+  return lanes;
+}
+template <typename T, typename... N>
+hipError_t launch_rope(hipStream_t s, const RopeCall& c0, const RopeTurns& t, N... norms) {
   RopeCall c = c0;
   const sts_rope_rows& a = c.a;
   auto rows_fit = [&](const void* p, int64_t stride, int e) { return !p || (aligned(p, e * sizeof(T)) && stride % e == 0); };
   // whole vectors of e elements: heads, pairs and rows
   auto fits = [&](int e) {
-    return a.d % e == 0 && (c.interleaved ? 2 * c.pairs : c.pairs) % e == 0 && rows_fit(a.q, a.q_stride, e) && rows_fit(a.q_out, a.q_out_stride, e) && rows_fit(a.k, a.k_stride, e) &&
+    bool lanes = true;
+    if constexpr (sizeof...(N) > 0) lanes = ((norms.lanes = norm_lanes(c, e)), ...) <= 64;
+    return lanes && a.d % e == 0 && (c.interleaved ? 2 * c.pairs : c.pairs) % e == 0 && rows_fit(a.q, a.q_stride, e) && rows_fit(a.q_out, a.q_out_stride, e) && rows_fit(a.k, a.k_stride, e) &&
            rows_fit(a.k_out, a.k_out_stride, e) && rows_fit(a.pool, 0, e);
   };
   c.v_vec = a.pool && sizeof(T) == 2 && aligned(a.pool, 16) && rows_fit(a.v, a.v_stride, 8);
-  if (fits(16 / sizeof(T))) return launch_rope<T, 16 / sizeof(T)>(s, c, t);
-  if (sizeof(T) == 2 && fits(4)) return launch_rope<T, 4>(s, c, t);
-  return launch_rope<T, 1>(s, c, t);
+  if (fits(16 / sizeof(T))) return launch_vectors<T, 16 / sizeof(T)>(s, c, t, norms...);
+  if (sizeof(T) == 2 && fits(4)) return launch_vectors<T, 4>(s, c, t, norms...);
+  if constexpr (sizeof...(N) > 0) ((norms.lanes = 64), ...);
+  return launch_vectors<T, 1>(s, c, t, norms...);
 }
 
-}  // namespace
-}  // namespace sts
-
-using namespace sts;
-
-extern "C" int sts_rope_frequencies(const sts_rope* rope, double* out) {
-  if (!rope || !out || !rope_frequencies(*rope, out)) return STS_EINVAL;
-  return STS_OK;
-}
-
-extern "C" int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* stream) {
+// sts_op_rope, with the norms of the heads or none.
+template <typename... N>
+int rope_rows(const sts_rope* rope, const sts_rope_rows* a, void* stream, const N&... norms) {
   RopeTurns turns;
   if (!rope || !a || !rope_turns(*rope, &turns)) return STS_EINVAL;
   if (a->dtype < STS_F32 || a->dtype > STS_F16 || a->rows < 0 || a->rows > (1 << 27) || a->n_q < 0 || a->n_kv < 0 || a->d < rope->rotary_dim || a->d > 1024 || a->n_q > 4096 || a->n_kv > 4096) return STS_EINVAL;
@@ -353,6 +455,24 @@ extern "C" int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* s
   if (rows.n_q == 0) rows.q = nullptr, rows.q_out = nullptr;
   if (rows.n_kv == 0) rows.k = nullptr, rows.k_out = nullptr;
   const RopeCall c{rows, rope->rotary_dim / 2, rope->interleaved, 0, false, rope->magnitude == 0.f ? 1.f : rope->magnitude};
-  const hipError_t e = a->dtype == STS_F32 ? launch_rope<float>(s, c, turns) : a->dtype == STS_BF16 ? launch_rope<bf16>(s, c, turns) : launch_rope<f16>(s, c, turns);
+  const hipError_t e = a->dtype == STS_F32 ? launch_rope<float>(s, c, turns, norms...) : a->dtype == STS_BF16 ? launch_rope<bf16>(s, c, turns, norms...) : launch_rope<f16>(s, c, turns, norms...);
   return op_result(e);
+}
+
+}  // namespace
+}  // namespace sts
+
+using namespace sts;
+
+extern "C" int sts_rope_frequencies(const sts_rope* rope, double* out) {
+  if (!rope || !out || !rope_frequencies(*rope, out)) return STS_EINVAL;
+  return STS_OK;
+}
+
+extern "C" int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* stream) { return rope_rows(rope, a, stream); }
+
+extern "C" int sts_op_norm_rope(const sts_head_norm* norm, const sts_rope* rope, const sts_rope_rows* a, void* stream) {
+  if (!norm || !a || norm->dtype < STS_F32 || norm->dtype > STS_F16 || (norm->offset_one != 0 && norm->offset_one != 1) || !(norm->eps >= 0.f) || !std::isfinite(norm->eps) || a->d > RP_NORM_D) return STS_EINVAL;
+  if (!aligned(norm->q_gain, dtype_bytes(norm->dtype)) || !aligned(norm->k_gain, dtype_bytes(norm->dtype))) return STS_EINVAL;
+  return rope_rows(rope, a, stream, HeadNorms{norm->q_gain, norm->k_gain, norm->dtype, 0, norm->eps, norm->offset_one ? 1.f : 0.f});
 }

@@ -122,6 +122,34 @@ class Logprobs(C.Structure):
         C.c_void_p, "logits tokens logprob entropy lse rank top_logprob top_token workspace") + _fields(C.c_int64, "workspace_bytes")
 
 
+class HeadNorm(C.Structure):
+    """sts_head_norm; dtype (of the gains): a value of DTYPES."""
+    _fields_ = _fields(C.c_int32, "dtype offset_one") + [("eps", C.c_float)] + _fields(C.c_void_p, "q_gain k_gain")
+
+
+class TreeBatch(C.Structure):
+    """sts_tree_batch"""
+    _fields_ = _fields(C.c_int32, "dtype n_requests max_rows n_q n_kv d pool_pages max_pages") + _fields(C.c_int64, "table_stride") + _fields(
+        C.c_void_p, "tables cached row_starts parents positions workspace") + _fields(C.c_int64, "workspace_bytes")
+
+
+class AdjustLogits(C.Structure):
+    """sts_adjust_logits"""
+    _fields_ = _fields(C.c_int32, "dtype rows vocab n_requests") + _fields(C.c_int64, "row_stride out_stride") + _fields(C.c_void_p, "logits out requests") + _fields(
+        C.c_int32, "n_biases n_masks") + _fields(C.c_int64, "token_stride mask_stride") + _fields(
+        C.c_void_p, "tokens lens prompt_lens repetition frequency presence row_starts parents drafted bias_starts bias_tokens bias_values masks mask_rows")
+
+
+class TreeAccept(C.Structure):
+    """sts_tree_accept"""
+    _fields_ = _fields(C.c_int32, "n_requests max_rows") + _fields(C.c_void_p, "cached row_starts parents tokens chosen lens counts path next_token")
+
+
+class TreeCompact(C.Structure):
+    """sts_tree_compact"""
+    _fields_ = _fields(C.c_int32, "n_requests max_rows n_kv d pool_pages max_pages") + _fields(C.c_int64, "table_stride") + _fields(C.c_void_p, "tables cached row_starts counts path")
+
+
 EXPORTS = [
     "sts_strerror", "sts_last_hip_error", "sts_init", "sts_destroy", "sts_release_streams", "sts_load_weights", "sts_read_weights",
     "sts_seq_create", "sts_seq_free", "sts_seq_length", "sts_seq_truncate", "sts_seq_reserve", "sts_pages_free", "sts_seq_set_block_table",
@@ -134,6 +162,7 @@ EXPORTS = [
     "sts_latency_roofline", "sts_sched_decide", "sts_sched_replay", "sts_max_pages_per_seq_limit", "sts_decode_chunk_plan", "sts_decode_gemm_plan", "sts_decode_layer_plan", "sts_decode_layer_all_rows", "sts_decode_gemm_all_rows", "sts_probe_read", "sts_set_stream_model", "sts_profile_stream_model", "sts_op_gemm_noalloc", "sts_op_gemm_cols", "sts_weight_packed_index", "sts_probe_gemm", "sts_set_tile_model",
     "sts_profile_tile_model", "sts_op_block_tables", "sts_rope_frequencies", "sts_op_rope", "sts_attn_shared_workspace", "sts_op_attn_shared_plan",
     "sts_op_attn_shared", "sts_op_logprobs_workspace", "sts_op_logprobs", "sts_read_logprobs", "sts_set_rope",
+    "sts_op_norm_rope", "sts_attn_tree_workspace", "sts_op_attn_tree_plan", "sts_op_attn_tree", "sts_op_adjust_logits", "sts_op_tree_accept", "sts_op_tree_compact",
 ]
 
 
@@ -150,7 +179,11 @@ def lib():
         # called once a step or layer: declared types are converted in a third of the time that wrapping each argument takes
         _lib.sts_op_block_tables.argtypes = _lib.sts_op_attn_shared_plan.argtypes = _lib.sts_op_logprobs.argtypes = [C.c_void_p, C.c_void_p]
         _lib.sts_op_rope.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
-        _lib.sts_op_attn_shared.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c_void_p]
+        _lib.sts_attn_tree_workspace.restype = C.c_int64
+        _lib.sts_op_attn_tree_plan.argtypes = _lib.sts_op_adjust_logits.argtypes = _lib.sts_op_tree_accept.argtypes = [C.c_void_p, C.c_void_p]
+        _lib.sts_op_norm_rope.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        _lib.sts_op_tree_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        _lib.sts_op_attn_tree.argtypes = _lib.sts_op_attn_shared.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_float, C.c_void_p]
     return _lib
 
 
@@ -523,6 +556,36 @@ def op_logprobs_workspace(dtype, rows, vocab, top_k):
 
 def op_logprobs(a: Logprobs, stream=None):
     _ck(lib().sts_op_logprobs(C.byref(a), stream), "sts_op_logprobs")
+
+
+def op_norm_rope(norm: HeadNorm, rope: Rope, a: RopeRows, stream=None):
+    _ck(lib().sts_op_norm_rope(C.byref(norm), C.byref(rope), C.byref(a), stream), "sts_op_norm_rope")
+
+
+def attn_tree_workspace(n_requests, max_rows, n_q, n_kv, d):
+    """Bytes of workspace of a batch; host only."""
+    return lib().sts_attn_tree_workspace(n_requests, max_rows, n_q, n_kv, d)
+
+
+def op_attn_tree_plan(b: TreeBatch, stream=None):
+    _ck(lib().sts_op_attn_tree_plan(C.byref(b), stream), "sts_op_attn_tree_plan")
+
+
+def op_attn_tree(b: TreeBatch, q, q_stride, pool, out, out_stride, lse=None, scale=0.0, stream=None):
+    _ck(lib().sts_op_attn_tree(C.byref(b), q, q_stride, pool, out, out_stride, lse, scale, stream), "sts_op_attn_tree")
+
+
+def op_adjust_logits(a: AdjustLogits, stream=None):
+    _ck(lib().sts_op_adjust_logits(C.byref(a), stream), "sts_op_adjust_logits")
+
+
+def op_tree_accept(a: TreeAccept, stream=None):
+    _ck(lib().sts_op_tree_accept(C.byref(a), stream), "sts_op_tree_accept")
+
+
+def op_tree_compact(a: TreeCompact, pools, stream=None):
+    """pools: the layers' device addresses."""
+    _ck(lib().sts_op_tree_compact(C.byref(a), (C.c_void_p * len(pools))(*pools), len(pools), stream), "sts_op_tree_compact")
 
 
 def release_streams():
