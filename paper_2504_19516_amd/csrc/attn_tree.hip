@@ -28,7 +28,8 @@ constexpr int AT_NODES = 256;                   // of a request
 constexpr int AT_MASK = 32;                     // 16-bit words of a row's mask, one for each page from the first that holds a node: up to 17 are used
 constexpr int AT_MAX_ROWS = 1 << 16;
 constexpr int AT_PLAN_THREADS = 512;
-constexpr int AT_JOIN_ROWS = 1024;              // up to so many (row, head) pairs four waves join each, beyond it one
+constexpr int AT_JOIN_ROWS = 1024;              // up to so many (row, head) pairs four waves join each, beyond it a run of lanes
+constexpr int AT_JOIN_BATCH = 4;                // parts of a run under way
 // Start and end of a wide and of a narrow segment, and the smallest shares beyond them, in pages; what a page of a wide segment takes a workgroup, in
 // pages of a narrow one.
 constexpr int AT_WIDE_START = 8, AT_NARROW_START = 2, AT_WIDE_LEAST = 4, AT_NARROW_LEAST = 4;
@@ -38,21 +39,19 @@ constexpr float AT_WIDE_WEIGHT = 1.25f;
 // first row's partial result, -1: it finishes its rows.
 struct Item { int row0, rows, request, pg0, pg1, part, cached, len; };
 struct Range { Item first; int next, end, pad[2]; };              // items of a wave: the first, and next .. end - 1; none if its rows are 0. The four of a workgroup with wide ones have the same
-// A request: where its tiles begin on the line of its kind, its pages (0: nothing of it is computed), first row and rows in all, and of a tile; wide or narrow
-struct Request { int at, pages, row0, rows, per, kind, bad, pad; };
+// Where a node row's partial results are: head h of a group in base + h + j * step, j < count. One: its one piece finishes it. count -1: gives NaN.
+struct Parts { int base, count, step, pad; };
 struct Header {
   unsigned long long tag;                        // sizes_tag() of the batch that the plan was made for
-  Line lines[2];                                 // wide, narrow
-  int narrow_part;                               // first partial row of narrow segments
   int rows;                                      // node rows; -1: row_starts out of order
-  int pad[4];
+  int pad;
 };
 struct Plan {
   Header* header;
   Range* ranges;                                 // [slots][4]
   Item* items;
-  Request* requests;                             // [n_requests]
-  int* owners;                                   // [max_rows]: request of a row, -1: no node
+  Parts* parts;                                  // [max_rows]
+  int* nodes;                                    // [max_rows]: 0: the row is no node
   unsigned short* masks;                         // [max_rows][AT_MASK]: a bit for each token of a page
   f32x2* stats;                                  // [partial row][kv head]: maximum (log2 units), sum
   float* outs;                                   // [partial row][kv head][d]
@@ -74,8 +73,8 @@ size_t lay_out(unsigned char* base, int n, int max_rows, int n_q, int n_kv, int 
   q.header = reinterpret_cast<Header*>(take(sizeof(Header)));
   q.ranges = reinterpret_cast<Range*>(take(slots_of(n_kv) * 4 * sizeof(Range)));
   q.items = reinterpret_cast<Item*>(take(max_items(n, max_rows, n_q, n_kv) * sizeof(Item)));
-  q.requests = reinterpret_cast<Request*>(take(n * sizeof(Request)));
-  q.owners = reinterpret_cast<int*>(take(max_rows * sizeof(int)));
+  q.parts = reinterpret_cast<Parts*>(take(max_rows * sizeof(Parts)));
+  q.nodes = reinterpret_cast<int*>(take(max_rows * sizeof(int)));
   q.masks = reinterpret_cast<unsigned short*>(take((size_t)max_rows * AT_MASK * sizeof(unsigned short)));
   q.stats = reinterpret_cast<f32x2*>(take(rows * sizeof(f32x2)));
   q.outs = reinterpret_cast<float*>(take(rows * d * sizeof(float)));
@@ -147,8 +146,9 @@ __device__ void deal_out(const PlanCall& c) {
     s.rows = nodes * c.heads;
     s.pages = (cached[i] + nodes + OP_PAGE - 1) / OP_PAGE;
     s.kind = s.rows <= AT_ROWS;
-    const int blocks = (s.rows + AT_ROWS - 1) / AT_ROWS, most = (blocks + 3) / 4;          // tiles of alike numbers of 32 rows
-    s.per = (blocks + most - 1) / most * AT_ROWS;
+    // tiles of alike numbers of 32 rows, of whole nodes
+    const int blocks = (s.rows + AT_ROWS - 1) / AT_ROWS, most = (blocks + 3) / 4;
+    s.per = (blocks + most - 1) / most * AT_ROWS / c.heads * c.heads;
     s.tiles = (s.rows + s.per - 1) / s.per;
     return s;
   };
@@ -173,19 +173,31 @@ __device__ void deal_out(const PlanCall& c) {
   const Line lines[2] = {line(all[0], wide, AT_WIDE_START, AT_WIDE_LEAST, 4), line(all[1], narrow, AT_NARROW_START, AT_NARROW_LEAST, 2)};
   const int narrow_part = c.max_rows * c.heads + wide * AT_TILE;
   if (tid == 0) {
-    *c.plan.header = Header{c.tag, {lines[0], lines[1]}, narrow_part, ordered ? start[n] : -1, {0, 0, 0, 0}};
+    *c.plan.header = Header{c.tag, ordered ? start[n] : -1, 0};
     line_at[0][n] = all[0]; line_at[1][n] = all[1];
   }
   for (int i = r0; i < r1; i++) {
     const Shape s = shape(i);
     line_at[0][i] = sums[0]; line_at[1][i] = sums[1];
     seg0[0][i] = (unsigned short)sums[2]; seg0[1][i] = (unsigned short)sums[3];
-    c.plan.requests[i] = Request{sums[s.kind], s.pages, start[i] * c.heads, s.rows, s.per, s.kind, s.tiles == 0, 0};
     if (s.tiles == 0) continue;
     sums[s.kind] += s.tiles * tile_cost(s);
     sums[2 + s.kind] += s.tiles;
   }
   __syncthreads();
+  for (int row = tid; row < (ordered ? start[n] : 0); row += AT_PLAN_THREADS) {
+    const int i = last_up_to(start, n, row);
+    const Shape s = shape(i);
+    Parts p{0, -1, 0, 0};
+    if (s.tiles > 0) {
+      const Line& l = lines[s.kind];
+      const int at = line_at[s.kind][i] + (row - start[i]) * c.heads / s.per * tile_cost(s);
+      p.step = s.kind ? AT_ROWS : AT_TILE;
+      p.count = l.pieces(at, s.pages);
+      p.base = (s.kind ? narrow_part : 0) + row * c.heads + p.step * l.first(at, s.pages);
+    }
+    c.plan.parts[row] = p;
+  }
   // The items of a share, by a thread of its own. Neighbouring narrow shares go to different workgroups.
   for (int j = tid; j < wide + narrow; j += AT_PLAN_THREADS) {
     const int kind = j >= wide, k = kind ? j - wide : j;
@@ -236,7 +248,7 @@ __device__ void follow_parents(const PlanCall& c, int request) {
   const bool ok = request_ok(c, cached, first, end);
   if (!ok) {
     for (int row = first + tid; row < end; row += AT_PLAN_THREADS) {
-      c.plan.owners[row] = request;
+      c.plan.nodes[row] = 1;
       if (c.positions) c.positions[row] = -1;
     }
     return;
@@ -272,7 +284,7 @@ __device__ void follow_parents(const PlanCall& c, int request) {
 #pragma unroll
     for (int w = 0; w < 8; w++) depth += __popc(up[now][i][w]);
     if (c.positions) c.positions[first + i] = node ? cached + depth : -1;
-    c.plan.owners[first + i] = node ? request : -1;
+    c.plan.nodes[first + i] = node;
   }
   // Bits of the tokens from the page of the first node on: those before it belong to the context. Words of two pages.
   const int shift = cached % OP_PAGE;
@@ -326,16 +338,28 @@ __device__ __forceinline__ void add_odd(f32x16 (&o)[D / 32], const TreeCall<T>& 
       }
   }
 }
-// V of a half page as the product may take it: 0 for what is no number, or lies behind the last node. True where the first was there.
-template <typename V, typename T>
-__device__ __forceinline__ bool without_odd(V& v, int tokens) {
+// Whether some of eight elements are no numbers: an exponent of ones carries into the sign's place.
+template <typename T>
+__device__ __forceinline__ unsigned odd_bits(u32x4 x) {
+  constexpr unsigned EXP = std::is_same<T, f16>::value ? 0x7C007C00u : 0x7F807F80u, ONE = std::is_same<T, f16>::value ? 0x04000400u : 0x00800080u;
+  unsigned any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; i++) any |= (x[i] & EXP) + ONE;
+  return any & 0x80008000u;
+}
+// Those as 0, as the products may take them. True if one of the first `tokens` elements was there.
+template <typename T>
+__device__ __forceinline__ bool without_odd(u32x4& x, int tokens) {
+  typedef typename Mfma<T>::V V;
+  V v = __builtin_bit_cast(V, x);
   bool odd = false;
 #pragma unroll
-  for (int e = 0; e < 8; e++) {
-    const bool no = !finite((float)v[e]);
-    odd |= no && e < tokens;
-    if (no || e >= tokens) v[e] = (T)0.f;
-  }
+  for (int e = 0; e < 8; e++)
+    if (!finite((float)v[e])) {
+      odd |= e < tokens;
+      v[e] = (T)0.f;
+    }
+  x = __builtin_bit_cast(u32x4, v);
   return odd;
 }
 
@@ -452,14 +476,16 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
 #pragma unroll
       for (int r = 0; r < 16; r++)                    // register r: page r >> 3 of the pair, token 8 * half + (r & 7)
         if (!(see >> r & 1)) s[r] = -INFINITY;
+      unsigned bits = 0;                              // what lies behind the nodes may be anything: 0 * V must be 0
 #pragma unroll
       for (int u = 0; u < 2; u++)
 #pragma unroll
-        for (int bb = 0; bb < DB; bb++) {
-          V v = __builtin_bit_cast(V, vr[u][bb]);
-          odd |= without_odd<V, T>(v, pg + u < it.pg1 ? it.len - (pg + u) * OP_PAGE - 8 * lh : 0);
-          vr[u][bb] = __builtin_bit_cast(u32x4, v);
-        }
+        for (int bb = 0; bb < DB; bb++) bits |= odd_bits<T>(vr[u][bb]);
+      if (__any(bits != 0))
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+          for (int bb = 0; bb < DB; bb++) odd |= without_odd<T>(vr[u][bb], pg + u < it.pg1 ? it.len - (pg + u) * OP_PAGE - 8 * lh : 0);
     }
     float mx = s[0];
 #pragma unroll
@@ -543,9 +569,10 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
   }
 }
 
-// ---- wide items, a workgroup: every wave takes 32 rows over all the pages. Tiles of four pages go global -> LDS, two stages deep, a page
-// a wave; products, order of the tokens and softmax as in attn_prefill.hip, whose queries lie in a row where these come from any node.
-template <typename T, int D>
+// ---- wide items, a workgroup: tiles of four pages go global -> LDS, two stages deep, a page a wave. KB = 2: every wave takes 32 rows over all the pages;
+// KB = 1 (up to 64 rows): waves w and w + 2 take the same 32 rows over two of each tile's pages, and join what they have at the end. Products, order of the tokens and softmax
+// as in attn_prefill.hip, whose queries lie in a row where these come from any node.
+template <typename T, int D, int KB>
 __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>& c, const Item& it, int kvh) {
   typedef typename Mfma<T>::V V;
   constexpr int KSTEPS = D / 16, DB = D / 32;
@@ -555,10 +582,23 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int npg = it.pg1 - it.pg0, tiles = (npg + 3) >> 2;
   const int* table = c.tables + (long long)it.request * c.table_stride + it.pg0;
-  const int my_rows = min(it.rows - wave * 32, 32);                            // none or fewer: the wave only fetches
+  const int block = KB == 2 ? wave : wave & 1, my_pages = KB == 2 ? 0 : wave & 2;       // of 32 rows; the wave's first page of a tile
+  const int my_rows = min(it.rows - block * 32, 32);                           // none or fewer: the wave only fetches
 
+  // This wave's page of tile kt; past the last page that page again, whose products are left out.
+  bool bad = false, odd = false;
+  const size_t page_stride = (size_t)c.n_kv * 2 * OP_PAGE * D;
+  const T* pool_h = c.pool + (size_t)kvh * 2 * OP_PAGE * D;
+  auto page_id = [&](int kt) {
+    const int page = table[min(kt * 4 + wave, npg - 1)];
+    const bool out = (unsigned)page >= (unsigned)c.pool_pages;
+    bad |= out;
+    return out ? 0 : page;
+  };
+  int next_page = page_id(0);
+  const int page1 = page_id(1);
   V qf[KSTEPS];
-  const int vrow = it.row0 + min(wave * 32 + l32, it.rows - 1);
+  const int vrow = it.row0 + min(block * 32 + l32, it.rows - 1);
   const Seen seen{c.plan.masks + (size_t)(vrow / c.heads) * AT_MASK, it.cached / OP_PAGE, it.pg1};
   {
     const T* q = c.q + (long long)(vrow / c.heads) * c.q_stride + (kvh * c.heads + vrow % c.heads) * D + 8 * lh;
@@ -570,16 +610,6 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
         for (int e = 0; e < 8; e++) qf[j][e] = q[16 * j + e];
     }
   }
-  // This wave's page of tile kt; past the last page that page again, whose products are left out.
-  bool bad = false, odd = false;
-  const size_t page_stride = (size_t)c.n_kv * 2 * OP_PAGE * D;
-  const T* pool_h = c.pool + (size_t)kvh * 2 * OP_PAGE * D;
-  auto page_id = [&](int kt) {
-    const int page = table[min(kt * 4 + wave, npg - 1)];
-    const bool out = (unsigned)page >= (unsigned)c.pool_pages;
-    bad |= out;
-    return out ? 0 : page;
-  };
   unsigned k_off[IPP];
 #pragma unroll
   for (int j = 0; j < IPP; j++) {
@@ -596,11 +626,11 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
     for (int j = 0; j < IPP; j++) lds_dma16(pb + (size_t)16 * D, (unsigned)(j * 1024 + lane * 16), dst + TILE + j * 1024);
   };
   const int tok = (l32 & 3) | (((l32 >> 3) & 1) << 2) | (((l32 >> 2) & 1) << 3);
-  const int k_row = (l32 >> 4) * PAGE + tok * ROWB;
+  const int k_row = my_pages * PAGE + (l32 >> 4) * PAGE + tok * ROWB;
   int k_slot[KSTEPS];
 #pragma unroll
   for (int j = 0; j < KSTEPS; j++) k_slot[j] = k_row + ((2 * j + lh) ^ (D == 128 ? tok : (tok >> 1) & 7)) * 16;
-  const int v_lane = TILE + l32 * 32 + lh * 16;          // V^T operand: d row l32 of a 32-row block, tokens 8 lh .. of a page
+  const int v_lane = TILE + my_pages * PAGE + l32 * 32 + lh * 16;              // V^T operand: d row l32 of a 32-row block, tokens 8 lh .. of a page
 
   f32x16 o[DB];
 #pragma unroll
@@ -608,56 +638,58 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
 #pragma unroll
     for (int r = 0; r < 16; r++) o[b][r] = 0.f;
   float m_ref = -INFINITY, l_run = 0.f;
-  issue(0, page_id(0));
-  int next_page = page_id(1);
-  // whole: four pages of context; otherwise some hold nodes, or lie behind the item's
-  auto tile = [&](int kt, auto whole) {
+  const int mixed = max(min(it.cached / OP_PAGE, it.pg1) - it.pg0, 0) >> 2;    // the first tile that is not four pages of context of the item's
+  issue(0, next_page);
+  next_page = page1;
+  auto tile = [&](int kt) {
     const unsigned char* st = arena + (kt & 1) * STAGE;
-    const int here = decltype(whole)::value ? 4 : min(npg - kt * 4, 4);        // pages of the tile
-    f32x16 s[2];
+    unsigned see[KB];                                      // a bit for each of a lane's scores
+    if (kt >= mixed)                                       // wave-uniform, as below
 #pragma unroll
-    for (int kb = 0; kb < 2; kb++)
+      for (int kb = 0; kb < KB; kb++) {
+        const int pg = it.pg0 + kt * 4 + my_pages + 2 * kb;
+        see[kb] = seen.page(pg) >> (8 * lh) & 0xFF | (seen.page(pg + 1) >> (8 * lh) & 0xFF) << 8;
+      }
+    f32x16 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; kb++)
 #pragma unroll
       for (int r = 0; r < 16; r++) s[kb][r] = 0.f;
     __builtin_amdgcn_sched_barrier(0);
     {
-      V kf[2][2];
+      V kf[2][KB];
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++) kf[0][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[0]);
+      for (int kb = 0; kb < KB; kb++) kf[0][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[0]);
 #pragma unroll
       for (int j = 0; j < KSTEPS; j++) {
         const int a = j & 1, b = a ^ 1;
         if (j + 1 < KSTEPS) {
 #pragma unroll
-          for (int kb = 0; kb < 2; kb++) kf[b][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[j + 1]);
+          for (int kb = 0; kb < KB; kb++) kf[b][kb] = *reinterpret_cast<const V*>(st + kb * 2 * PAGE + k_slot[j + 1]);
         }
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++) s[kb] = Mfma<T>::mul(kf[a][kb], qf[j], s[kb]);
+        for (int kb = 0; kb < KB; kb++) s[kb] = Mfma<T>::mul(kf[a][kb], qf[j], s[kb]);
       }
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);
 #pragma unroll
       for (int j = 0; j + 1 < KSTEPS; j++) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, KB, 0);
     }
     V vf[2][DB];                                           // first V^T operands: in flight during the softmax arithmetic
 #pragma unroll
     for (int b = 0; b < DB; b++) vf[0][b] = *reinterpret_cast<const V*>(st + v_lane + b * 1024);
-    if constexpr (!decltype(whole)::value) {
+    if (kt >= mixed)
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++) {
-        const int pg = it.pg0 + kt * 4 + 2 * kb;
-        const unsigned see = seen.page(pg) >> (8 * lh) & 0xFF | (seen.page(pg + 1) >> (8 * lh) & 0xFF) << 8;
+      for (int kb = 0; kb < KB; kb++)
 #pragma unroll
         for (int r = 0; r < 16; r++)
-          if (!(see >> r & 1)) s[kb][r] = -INFINITY;
-      }
-    }
+          if (!(see[kb] >> r & 1)) s[kb][r] = -INFINITY;
     float mx = -INFINITY;
 #pragma unroll
-    for (int kb = 0; kb < 2; kb++)
+    for (int kb = 0; kb < KB; kb++)
 #pragma unroll
       for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[kb][r]);
     mx = half_swap_max_f(mx);
@@ -676,7 +708,7 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
     const float nm = (m_ref == -INFINITY) ? 0.f : fmaf(-m_ref, c.scale_log2e, AS_LIFT<T>);
     float rs = 0.f;
 #pragma unroll
-    for (int kb = 0; kb < 2; kb++)
+    for (int kb = 0; kb < KB; kb++)
 #pragma unroll
       for (int r = 0; r < 16; r++) {
         const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c.scale_log2e, nm));
@@ -685,84 +717,108 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
       }
     l_run += rs;                                                               // this half's keys; halves are added at the end
 #pragma unroll
-    for (int g = 0; g < 4; g++) {
+    for (int g = 0; g < 2 * KB; g++) {
       const int a = g & 1, b2 = a ^ 1;
-      if (g + 1 < 4) {
+      if (g + 1 < 2 * KB) {
 #pragma unroll
         for (int b = 0; b < DB; b++) vf[b2][b] = *reinterpret_cast<const V*>(st + v_lane + (g + 1) * PAGE + b * 1024);
       }
-      if constexpr (!decltype(whole)::value) {
-#pragma unroll
-        for (int b = 0; b < DB; b++) odd |= without_odd<V, T>(vf[a][b], g < here ? it.len - (it.pg0 + kt * 4 + g) * OP_PAGE - 8 * lh : 0);
-      }
       V pb, pr;
       in_two(s[g >> 1], 8 * (g & 1), pb, pr);
-      if (decltype(whole)::value || g < here) {
 #pragma unroll
-        for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pb, o[b]);
+      for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pb, o[b]);
 #pragma unroll
-        for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pr, o[b]);
-      }
+      for (int b = 0; b < DB; b++) o[b] = Mfma<T>::mul(vf[a][b], pr, o[b]);
     }
-    if constexpr (decltype(whole)::value) {
 #pragma unroll
-      for (int g = 0; g + 1 < 4; g++) {
-        __builtin_amdgcn_sched_group_barrier(0x100, DB, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 2 * DB, 0);
-      }
+    for (int g = 0; g + 1 < 2 * KB; g++) {
+      __builtin_amdgcn_sched_group_barrier(0x100, DB, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, 2 * DB, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(0x008, 2 * DB, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto landed = [&](int kt) {                              // every wave waits for its own page, and nobody reads the other stage any more
-    wait_vmem<0>();
+  for (int kt = 0; kt < tiles; kt++) {
+    wait_vmem<0>();                                        // every wave waits for its own page, and nobody reads the other stage any more
     __syncthreads();
     __builtin_amdgcn_sched_barrier(0);
     if (kt + 1 < tiles) {
       issue((kt + 1) & 1, next_page);
       next_page = page_id(kt + 2);
     }
-  };
-  const int whole = max(min(it.cached / OP_PAGE, it.pg1) - it.pg0, 0) >> 2;
-  for (int kt = 0; kt < whole; kt++) {
-    landed(kt);
-    if (my_rows > 0) tile(kt, std::true_type{});           // wave-uniform
+    if (kt >= mixed) {                                     // what lies behind the nodes may be anything: 0 * V must be 0
+      bool here = false;
+      unsigned char* vt = arena + (kt & 1) * STAGE + TILE;
+      for (int i = tid; i < TILE / 16; i += 256) {
+        u32x4 x = *reinterpret_cast<const u32x4*>(vt + i * 16);
+        if (odd_bits<T>(x)) {
+          const int pg = it.pg0 + kt * 4 + i / (PAGE / 16);
+          here |= without_odd<T>(x, pg < it.pg1 ? it.len - pg * OP_PAGE - 8 * (i & 1) : 0);
+          *reinterpret_cast<u32x4*>(vt + i * 16) = x;
+        }
+      }
+      odd |= __syncthreads_or(here);
+    }
+    if (my_rows > 0) tile(kt);                             // wave-uniform
   }
-  for (int kt = whole; kt < tiles; kt++) {
-    landed(kt);
-    if (my_rows > 0) tile(kt, std::false_type{});
-  }
-  if (__any(odd)) add_odd<T, D>(o, c, it, it.pg0 + 4 * whole, table - it.pg0, seen, kvh, lh);
   l_run += __shfl_xor(l_run, 32, 64);
   if (__syncthreads_or(bad)) l_run = NAN;                // LDS now takes the output
-  if (my_rows > 0) {
-    // whole rows through LDS: 16-byte chunks, swizzled by row
-    constexpr int OROWB = D * 4, OCPR = OROWB / 16, ORPI = 64 / OCPR;
-    unsigned char* buf = arena + wave * 32 * OROWB;
-    const int lane = fresh(tid & 63), l32 = lane & 31, lh = lane >> 5;
+  // whole rows through LDS: 16-byte chunks, swizzled by row
+  constexpr int OROWB = D * 4, OCPR = OROWB / 16, ORPI = 64 / OCPR;
+  unsigned char* buf = arena + block * 32 * OROWB;
+  auto slot = [&](int row, int chunk) { return reinterpret_cast<f32x4*>(buf + row * OROWB + (chunk ^ (row % 16)) * 16); };
+  f32x2* other = reinterpret_cast<f32x2*>(arena + 2 * 32 * OROWB) + block * 32;         // KB = 1: maximum and sum of the waves of the second pages
+  const int lane2 = fresh(tid & 63), r32 = lane2 & 31, rh = lane2 >> 5;
+  if (KB == 1) {
+    if (my_pages != 0 && my_rows > 0) {
+#pragma unroll
+      for (int b = 0; b < DB; b++)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; r4++) *slot(r32, b * 8 + 2 * r4 + rh) = f32x4{o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]};
+      if (rh == 0) other[r32] = f32x2{m_ref, l_run};
+    }
+    __syncthreads();
+    if (my_pages == 0 && my_rows > 0) {
+      const f32x2 st = other[r32];
+      const float m = fmaxf(m_ref, st[0]);
+      const float fa = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_ref - m) * c.scale_log2e), fb = st[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((st[0] - m) * c.scale_log2e);
+      // an empty side's sum is 0, or NaN for a page that is none
+      l_run = (m_ref == -INFINITY ? l_run : l_run * fa) + (st[0] == -INFINITY ? st[1] : st[1] * fb);
+      m_ref = m;
+#pragma unroll
+      for (int b = 0; b < DB; b++)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; r4++) {
+          const f32x4 x = *slot(r32, b * 8 + 2 * r4 + rh);
+#pragma unroll
+          for (int e = 0; e < 4; e++) o[b][4 * r4 + e] = o[b][4 * r4 + e] * fa + x[e] * fb;
+        }
+    }
+  }
+  if (my_rows > 0 && my_pages == 0) {
+    if (odd) add_odd<T, D>(o, c, it, it.pg0 + 4 * mixed, table - it.pg0, seen, kvh, rh);
 #pragma unroll
     for (int b = 0; b < DB; b++)
 #pragma unroll
-      for (int r4 = 0; r4 < 4; r4++)
-        *reinterpret_cast<f32x4*>(buf + l32 * OROWB + ((b * 8 + 2 * r4 + lh) ^ (l32 % 16)) * 16) = f32x4{o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]};
+      for (int r4 = 0; r4 < 4; r4++) *slot(r32, b * 8 + 2 * r4 + rh) = f32x4{o[b][4 * r4], o[b][4 * r4 + 1], o[b][4 * r4 + 2], o[b][4 * r4 + 3]};
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int r0 = lane / OCPR, ch = lane % OCPR;
+    const int r0 = lane2 / OCPR, ch = lane2 % OCPR;
     const float m2 = fmaf(m_ref, c.scale_log2e, -AS_LIFT<T>), f = 1.f / ((1.f + AS_EXTRA<T>) * l_run);
 #pragma unroll
     for (int i = 0; i < 32 / ORPI; i++) {
       const int r = i * ORPI + r0;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(buf + r * OROWB + (ch ^ (r % 16)) * 16);
+      const f32x4 x = *slot(r, ch);
       const float fr = __shfl(f, r, 64);
       if (r >= my_rows) continue;
       if (it.part < 0) {
-        const int v = it.row0 + wave * 32 + r;
+        const int v = it.row0 + block * 32 + r;
         store4(c.out + (long long)(v / c.heads) * c.out_stride + (kvh * c.heads + v % c.heads) * D + ch * 4, x, fr, c.out_vec);
       } else {
-        *reinterpret_cast<f32x4*>(c.plan.outs + ((size_t)(it.part + wave * 32 + r) * c.n_kv + kvh) * D + ch * 4) = x;
+        *reinterpret_cast<f32x4*>(c.plan.outs + ((size_t)(it.part + block * 32 + r) * c.n_kv + kvh) * D + ch * 4) = x;
       }
     }
-    if (lane < my_rows) {
-      if (it.part >= 0) c.plan.stats[(size_t)(it.part + wave * 32 + lane) * c.n_kv + kvh] = f32x2{m2, l_run};
+    if (lane2 < my_rows) {
+      if (it.part >= 0) c.plan.stats[(size_t)(it.part + block * 32 + lane2) * c.n_kv + kvh] = f32x2{m2, l_run};
       else if (c.lse) c.lse[(long long)(vrow / c.heads) * c.n_q + kvh * c.heads + vrow % c.heads] = LN2 * (m2 + __builtin_amdgcn_logf(l_run));
     }
   }
@@ -778,49 +834,54 @@ __global__ void __launch_bounds__(256, 2) attn_tree_kernel(TreeCall<T> c) {
   if (c.plan.header->tag != c.tag || r.first.rows == 0) return;
   Item it = r.first;
   for (int i = r.next;; i++) {
-    if (it.rows > AT_ROWS) run_wide<T, D>(smem, c, it, kvh);
+    if (it.rows > 2 * AT_ROWS) run_wide<T, D, 2>(smem, c, it, kvh);
+    else if (it.rows > AT_ROWS) run_wide<T, D, 1>(smem, c, it, kvh);
     else run_narrow<T, D>(smem, c, it, kvh);
     if (i >= r.end) break;
     it = c.plan.items[i];
   }
 }
 
-// Joins the partial results of a (row, query head): WAVES waves each, a lane four elements of every 256 / D-th part (of a wave's share).
-template <typename T, int D, int WAVES>
-__global__ void __launch_bounds__(256) attn_tree_join_kernel(TreeCall<T> c) {
-  constexpr int LANES = D / 4, APART = 64 / LANES * WAVES;       // lanes of a part, parts side by side
-  __shared__ f32x4 sums[WAVES > 1 ? WAVES : 1][LANES];
+// Where the partial results of a (row, query head) are.
+struct Pieces { int count, base, step; bool bad, done; };          // done: finished by its one piece, or behind the last row
+template <typename T>
+__device__ __forceinline__ Pieces pieces_of(const TreeCall<T>& c, int row, int h) {
+  const Header hd = *c.plan.header;
+  const Parts p = c.plan.parts[row];                     // whatever they hold where there is no plan
+  const int node = c.plan.nodes[row];
+  if (hd.tag != c.tag || hd.rows < 0) return Pieces{0, 0, 0, true, false};
+  if (row >= hd.rows) return Pieces{0, 0, 0, false, true};
+  if (p.count < 0) return Pieces{0, 0, 0, true, false};
+  return Pieces{node ? p.count : 0, p.base + h, p.step, false, node && p.count == 1};
+}
+// A lane's four elements from e4 on; lse by the lane of the first.
+template <typename T, int D>
+__device__ __forceinline__ void finish_row(const TreeCall<T>& c, int row, int head, int e4, const Pieces& p, float m, float l, f32x4 o) {
+  const bool none = p.count == 0;                        // no node: zeros, and the logarithm of an empty sum
+  const f32x4 x = p.bad ? f32x4{NAN, NAN, NAN, NAN} : none ? f32x4{0.f, 0.f, 0.f, 0.f} : o;
+  store4(c.out + (long long)row * c.out_stride + head * D + e4, x, none ? 1.f : 1.f / ((1.f + AS_EXTRA<T>) * l), c.out_vec);
+  if (e4 == 0 && c.lse) c.lse[(long long)row * c.n_q + head] = p.bad ? NAN : none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
+}
+
+// Joins the partial results of a (row, query head), where there are few of these: four waves each, a lane four elements of every 1024 / D-th part.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attn_tree_join_few_kernel(TreeCall<T> c) {
+  constexpr int LANES = D / 4, WAVES = 4, APART = 64 / LANES * WAVES;       // lanes of a part, parts side by side
+  __shared__ f32x4 sums[WAVES][LANES];
   __shared__ float ls[WAVES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + wave;
-  if (at >= c.max_rows * c.n_q) return;
-  const int row = at / c.n_q, head = at % c.n_q, kvh = head / c.heads, h = head % c.heads;
-  const Header& hd = *c.plan.header;
-  const bool planned = hd.tag == c.tag && hd.rows >= 0;
-  if (planned && row >= hd.rows) return;
-  const int owner = planned ? c.plan.owners[row] : 0;
-  int count = 0, base = 0, step = 0;
-  bool bad = !planned;
-  if (planned && owner >= 0) {
-    const Request q = c.plan.requests[owner];
-    bad = q.bad;
-    if (!bad) {
-      const Line& l = hd.lines[q.kind];
-      const int v = row * c.heads + h, at = q.at + (v - q.row0) / q.per * (q.pages + l.start);
-      count = l.pieces(at, q.pages);
-      if (count == 1) return;                                    // finished by its one piece
-      step = q.kind ? AT_ROWS : AT_TILE;
-      base = (q.kind ? hd.narrow_part : 0) + v + step * l.first(at, q.pages);
-    }
-  }
-  auto row_of = [&](int j) { return (size_t)(base + j * step) * c.n_kv + kvh; };
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = blockIdx.x / c.n_q, head = blockIdx.x % c.n_q, kvh = head / c.heads;
+  const Pieces p = pieces_of(c, row, head % c.heads);
+  if (p.done) return;
+  auto row_of = [&](int j) { return (size_t)(p.base + j * p.step) * c.n_kv + kvh; };
   float m = -INFINITY;
-  for (int j = lane; j < count; j += 64) m = fmaxf(m, c.plan.stats[row_of(j)][0]);
+  for (int j = lane; j < p.count; j += 64) m = fmaxf(m, c.plan.stats[row_of(j)][0]);
   m = wave_max(m);
   float l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  const int first = (WAVES > 1 ? wave * (64 / LANES) : 0) + lane / LANES, e4 = lane % LANES * 4;
+  const int first = wave * (64 / LANES) + lane / LANES, e4 = lane % LANES * 4;
 #pragma unroll 4
-  for (int j = first; j < count; j += APART) {
+  for (int j = first; j < p.count; j += APART) {
     const size_t part = row_of(j);
     const f32x2 st = c.plan.stats[part];
     const f32x4 x = *reinterpret_cast<const f32x4*>(c.plan.outs + part * D + e4);
@@ -835,28 +896,66 @@ __global__ void __launch_bounds__(256) attn_tree_join_kernel(TreeCall<T> c) {
 #pragma unroll
     for (int e = 0; e < 4; e++) o[e] += __shfl_xor(o[e], s, 64);
   }
-  if constexpr (WAVES > 1) {
-    if (lane < LANES) sums[wave][lane] = o;
-    if (lane == 0) ls[wave] = l;
-    __syncthreads();
-    if (wave > 0) return;
-    l = 0.f;
+  if (lane < LANES) sums[wave][lane] = o;
+  if (lane == 0) ls[wave] = l;
+  __syncthreads();
+  if (wave > 0 || lane >= LANES) return;
+  l = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; w++) l += ls[w];
-    if (lane < LANES) {
-      o = sums[0][lane];
+  for (int w = 0; w < WAVES; w++) l += ls[w];
+  o = sums[0][lane];
 #pragma unroll
-      for (int w = 1; w < WAVES; w++)
+  for (int w = 1; w < WAVES; w++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) o[e] += sums[w][lane][e];
+    for (int e = 0; e < 4; e++) o[e] += sums[w][lane][e];
+  finish_row<T, D>(c, row, head, e4, p, m, l, o);
+}
+
+// Joins the partial results of many: a run of D / 4 lanes each, which take the parts in order, their statistics as many at a time as there are lanes.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attn_tree_join_kernel(TreeCall<T> c) {
+  constexpr int LANES = D / 4, RUNS = 256 / LANES;
+  const int lane = threadIdx.x % LANES, at = blockIdx.x * RUNS + threadIdx.x / LANES;
+  if (at >= c.max_rows * c.n_q) return;
+  const int row = at / c.n_q, head = at % c.n_q, kvh = head / c.heads;
+  const Pieces p = pieces_of(c, row, head % c.heads);
+  if (p.done) return;
+  auto row_of = [&](int j) { return (size_t)(p.base + j * p.step) * c.n_kv + kvh; };
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int j0 = 0; j0 < p.count; j0 += LANES) {
+    const f32x2 st = j0 + lane < p.count ? c.plan.stats[row_of(j0 + lane)] : f32x2{-INFINITY, 0.f};
+    float now = st[0];
+#pragma unroll
+    for (int s = 1; s < LANES; s <<= 1) now = fmaxf(now, __shfl_xor(now, s, 64));
+    now = fmaxf(now, m);
+    if (now > m) {                                       // the same for the run
+      const float f = __builtin_amdgcn_exp2f(m - now);
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < 4; e++) o[e] *= f;
+      m = now;
+    }
+    const float w = st[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - m);
+    float z = st[0] == -INFINITY ? st[1] : st[1] * w;            // 0 of a part without scores above -inf, or NaN
+#pragma unroll
+    for (int s = 1; s < LANES; s <<= 1) z += __shfl_xor(z, s, 64);
+    l += z;
+    const int n = min(LANES, p.count - j0);
+    for (int j = 0; j < n; j += AT_JOIN_BATCH) {
+      f32x4 x[AT_JOIN_BATCH];
+#pragma unroll
+      for (int u = 0; u < AT_JOIN_BATCH; u++) x[u] = *reinterpret_cast<const f32x4*>(c.plan.outs + row_of(j0 + min(j + u, n - 1)) * D + lane * 4);
+#pragma unroll
+      for (int u = 0; u < AT_JOIN_BATCH; u++) {
+        const float wj = __shfl(w, j + u, LANES);
+        if (j + u < n)
+#pragma unroll
+          for (int e = 0; e < 4; e++) o[e] += x[u][e] * wj;
+      }
     }
   }
-  if (lane < LANES) {
-    const bool none = count == 0;                      // no node: zeros, and the logarithm of an empty sum
-    const f32x4 x = bad ? f32x4{NAN, NAN, NAN, NAN} : none ? f32x4{0.f, 0.f, 0.f, 0.f} : o;
-    store4(c.out + (long long)row * c.out_stride + head * D + e4, x, none ? 1.f : 1.f / ((1.f + AS_EXTRA<T>) * l), c.out_vec);
-    if (lane == 0 && c.lse) c.lse[(long long)row * c.n_q + head] = bad ? NAN : none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
-  }
+  finish_row<T, D>(c, row, head, lane * 4, p, m, l, o);
 }
 
 template <typename T, int D>
@@ -864,8 +963,9 @@ hipError_t launch_attn(hipStream_t s, const TreeCall<T>& c) {
   hipError_t e = launch(attn_tree_kernel<T, D>, dim3(slots_of(c.n_kv) * c.n_kv), dim3(256), 0, s, c);
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)c.max_rows * c.n_q;
-  if (rows <= AT_JOIN_ROWS) return launch(attn_tree_join_kernel<T, D, 4>, dim3((unsigned)rows), dim3(256), 0, s, c);
-  return launch(attn_tree_join_kernel<T, D, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, c);
+  if (rows <= AT_JOIN_ROWS) return launch(attn_tree_join_few_kernel<T, D>, dim3((unsigned)rows), dim3(256), 0, s, c);
+  constexpr int RUNS = 256 / (D / 4);
+  return launch(attn_tree_join_kernel<T, D>, dim3((unsigned)((rows + RUNS - 1) / RUNS)), dim3(256), 0, s, c);
 }
 
 bool sizes_ok(int n, int max_rows, int n_q, int n_kv, int d) {
