@@ -17,101 +17,176 @@
 namespace sts {
 namespace {
 
-constexpr int AL_THREADS = 256, AL_NODES = 256;
+constexpr int AL_THREADS = 512, AL_NODES = 256;
 constexpr int AL_BATCH = 4;                            // groups of elements of a thread under way
 constexpr int AL_ROWS = 8;                             // rows of a workgroup, at most: a bit each
 constexpr int AL_PART = 4096, AL_LEAST = 1024, AL_WORKGROUPS = 1024;       // tokens of a part, fewer where there are fewer workgroups than that
 constexpr unsigned AL_PROMPT = 1u << 31;               // beside the count of the output
 
+constexpr int AL_MASK_THREADS = 256, AL_MASK_BATCH = 4;
+
 struct AdjustCall {
   sts_adjust_logits a;
   int part, rows_per;                                  // tokens of a part (a multiple of 32), rows of a workgroup
   bool in_place, tokens_vec;                           // tokens can be loaded 16 bytes at a time
+  bool parts_first;                                    // the launch's x counts parts, not workgroups' rows
+  __device__ __forceinline__ int first_token() const { return (parts_first ? blockIdx.x : blockIdx.y) * part; }
+  __device__ __forceinline__ int first_row() const { return (parts_first ? blockIdx.y : blockIdx.x) * rows_per; }
 };
 
-// E: elements of a group, in aligned vectors
+// A group of elements, 16 bytes that may begin at any element: rows of odd lengths lie one behind the other as often as aligned ones.
+template <typename T, int E> struct Group {
+  typedef T V __attribute__((ext_vector_type(E)));
+  typedef V InMemory __attribute__((aligned(sizeof(T))));
+};
+// Up to E elements of a row, those behind its end left out.
+template <typename T, int E>
+__device__ __forceinline__ void load_group(typename Group<T, E>::V& x, const T* from, int left) {
+  if (left < E) {
+#pragma unroll
+    for (int e = 0; e < E; e++)
+      if (e < left) x[e] = from[e];
+  } else {
+    x = *reinterpret_cast<const typename Group<T, E>::InMemory*>(from);
+  }
+}
+template <typename T, int E>
+__device__ __forceinline__ void store_group(T* to, typename Group<T, E>::V x, unsigned out, int left) {      // out: elements that are ruled out
+#pragma unroll
+  for (int e = 0; e < E; e++)
+    if (out >> e & 1) x[e] = (T)-INFINITY;
+  if (left < E) {
+#pragma unroll
+    for (int e = 0; e < E; e++)
+      if (e < left) to[e] = x[e];
+  } else {
+    *reinterpret_cast<typename Group<T, E>::InMemory*>(to) = x;
+  }
+}
+
+// Rows to which nothing but their masks applies: a part of a row a workgroup.
+template <typename T, int E>
+__global__ void __launch_bounds__(AL_MASK_THREADS) mask_logits_kernel(AdjustCall c) {
+  typedef typename Group<T, E>::V V;
+  const sts_adjust_logits& a = c.a;
+  const int row = c.first_row(), lo = c.first_token(), size = min(a.vocab - lo, c.part), m = a.masks ? a.mask_rows[row] : -1;
+  const bool masked = (unsigned)m < (unsigned)a.n_masks;
+  if (c.in_place && !masked) return;
+  const T* from = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride + lo;
+  T* to = reinterpret_cast<T*>(a.out) + (long long)row * a.out_stride + lo;
+  const unsigned* mask = a.masks + (masked ? m * a.mask_stride + lo / 32 : 0);
+  constexpr unsigned ALL = (1u << E) - 1;
+  V x[AL_MASK_BATCH];
+  unsigned out[AL_MASK_BATCH];
+  auto at = [&](int u) { return ((int)threadIdx.x + u * AL_MASK_THREADS) * E; };
+#pragma unroll
+  for (int u = 0; u < AL_MASK_BATCH; u++) out[u] = masked && at(u) < size ? ~mask[at(u) >> 5] >> (at(u) & 31) & ALL : 0u;
+#pragma unroll
+  for (int u = 0; u < AL_MASK_BATCH; u++)
+    if (at(u) < size && out[u] != ALL && (out[u] || !c.in_place)) load_group<T, E>(x[u], from + at(u), size - at(u));
+#pragma unroll
+  for (int u = 0; u < AL_MASK_BATCH; u++)
+    if (at(u) < size && (out[u] || !c.in_place)) store_group<T, E>(to + at(u), x[u], out[u], size - at(u));
+}
+
 template <typename T, int E>
 __global__ void __launch_bounds__(AL_THREADS) adjust_logits_kernel(AdjustCall c) {
-  typedef T V __attribute__((ext_vector_type(E)));
+  typedef typename Group<T, E>::V V;
   extern __shared__ unsigned lds[];
   __shared__ short parents[AL_NODES];
   __shared__ int drafted[AL_NODES], mask_of[AL_ROWS];
   const sts_adjust_logits& a = c.a;
-  const int tid = threadIdx.x, lo = blockIdx.y * c.part, size = min(a.vocab - lo, c.part);
-  const bool counted = a.tokens || a.drafted, any = counted || a.bias_tokens;
+  const int tid = threadIdx.x, lo = c.first_token(), size = min(a.vocab - lo, c.part);
+  const bool counted = a.tokens || a.drafted;
   // a bit for each token that something applies to; counts; the bias' entry + 1, 0 without one; a bit for each of the rows on whose path a token is
   unsigned *touched = lds, *count = lds + c.part / 32, *bias = count + (counted ? c.part : 0), *on_path = bias + (a.bias_tokens ? c.part : 0);
   const int words = c.part / 32 + (counted ? c.part : 0) + (a.bias_tokens ? c.part : 0) + (a.drafted ? c.part / 4 : 0);
+  auto clear = [&] {
+    for (int i = tid; i < words / 4; i += AL_THREADS) reinterpret_cast<u32x4*>(lds)[i] = u32x4{0u, 0u, 0u, 0u};
+  };
   auto mark = [&](int t) { atomicOr(&touched[t >> 5], 1u << (t & 31)); };
   auto request_of = [&](int row) {
     const int r = a.requests ? a.requests[row] : row;
     return (unsigned)r < (unsigned)a.n_requests ? r : -1;
   };
-  const int end = min(a.rows, ((int)blockIdx.x + 1) * c.rows_per);
-  for (int row0 = blockIdx.x * c.rows_per, row1; row0 < end; row0 = row1) {
+  const int end = min(a.rows, c.first_row() + c.rows_per);
+  const int lane = tid & 63;
+  for (int row0 = c.first_row(), rows; row0 < end; row0 += rows) {
     // the next rows of one request
-    const int request = request_of(row0);
-    row1 = row0 + 1;
-    while (row1 < end && request_of(row1) == request) row1++;
-    const int rows = row1 - row0;
-    int first = 0, nodes = 0;
+    const int mine = row0 + lane < end ? request_of(row0 + lane) : -2, request = __builtin_amdgcn_readfirstlane(mine);
+    rows = __builtin_ctzll(~__ballot(mine == request) | 1ull << AL_ROWS);
+    // A thread's groups, neighbours of neighbouring threads', the rows one behind the other: four under way, the first ones of a copy from here on
+    struct At { int row, t; };
+    auto next = [&](At at) {
+      if (++at.row == rows) { at.row = 0; at.t += AL_THREADS * E; }
+      return at;
+    };
+    V x[AL_BATCH];
+    At at{0, tid * E}, ats[AL_BATCH];
+    auto load = [&](V& x, const At& at) {
+      load_group<T, E>(x, reinterpret_cast<const T*>(a.logits) + (long long)(row0 + at.row) * a.row_stride + lo + at.t, size - at.t);
+    };
+    auto begin = [&] {
+#pragma unroll
+      for (int u = 0; u < AL_BATCH; u++) {
+        ats[u] = at;
+        at = next(at);
+        if (!c.in_place && ats[u].t < size) load(x[u], ats[u]);
+      }
+    };
+    begin();
+    // what there is of the request: on the way together
+    const bool some = request >= 0;
+    const int held = some && a.tokens ? a.lens[request] : 0, prompt = some && a.tokens && a.prompt_lens ? a.prompt_lens[request] : 0;
+    const int bias0 = some && a.bias_tokens ? a.bias_starts[request] : 0, bias1 = some && a.bias_tokens ? a.bias_starts[request + 1] : 0;
+    const int first = some && a.drafted ? a.row_starts[request] : 0, behind = some && a.drafted ? a.row_starts[request + 1] : 0;
+    const float r = some && a.repetition ? a.repetition[request] : 1.f, f = some && a.frequency ? a.frequency[request] : 0.f, w = some && a.presence ? a.presence[request] : 0.f;
     __syncthreads();                                   // nobody reads the rows before any more
     if (tid < rows) mask_of[tid] = a.masks ? a.mask_rows[row0 + tid] : -1;
-    if (!any) __syncthreads();
-    if (any) {
-      for (int i = tid; i < words; i += AL_THREADS) lds[i] = 0;
-      if (a.drafted && request >= 0) {
-        first = a.row_starts[request];
-        const int behind = a.row_starts[request + 1];
-        nodes = first >= 0 && behind >= first && behind <= a.rows ? min(behind - first, AL_NODES) : 0;
-        if (tid < nodes) {
-          const int p = a.parents[first + tid];
-          parents[tid] = (short)(p >= 0 && p < tid ? p : -1);
-          drafted[tid] = a.drafted[first + tid];
-        }
-      }
-      __syncthreads();
-      if (request >= 0 && a.tokens) {
-        const int* tokens = a.tokens + (long long)request * a.token_stride;
-        const int len = (int)min((long long)a.lens[request], (long long)a.token_stride), prompt = a.prompt_lens ? a.prompt_lens[request] : 0;
-        auto one = [&](int t, int i) {
-          t -= lo;
-          if ((unsigned)t >= (unsigned)size) return;
-          if (i < prompt) atomicOr(&count[t], AL_PROMPT); else atomicAdd(&count[t], 1u);
-          mark(t);
-        };
-        int i = 0;
-        if (c.tokens_vec) {
-          const int whole = max(len, 0) / 4;
-#pragma unroll 4
-          for (int v = tid; v < whole; v += AL_THREADS) {
-            const i32x4 t = reinterpret_cast<const i32x4*>(tokens)[v];
-#pragma unroll
-            for (int e = 0; e < 4; e++) one(t[e], 4 * v + e);
-          }
-          i = whole * 4;
-        }
-        for (i += tid; i < len; i += AL_THREADS) one(tokens[i], i);
-      }
-      if (request >= 0 && a.bias_tokens) {
-        const int behind = min(a.bias_starts[request + 1], a.n_biases);
-        for (int i = max(a.bias_starts[request], 0) + tid; i < behind; i += AL_THREADS) {
-          const int t = a.bias_tokens[i] - lo;
-          if ((unsigned)t >= (unsigned)size) continue;
-          atomicMax(&bias[t], (unsigned)i + 1);
-          mark(t);
-        }
-      }
-      if (tid < rows && row0 + tid >= first && row0 + tid < first + nodes)       // a thread for each row's path
-        for (int j = row0 + tid - first; j >= 0; j = parents[j]) {
-          const int t = drafted[j] - lo;
-          if ((unsigned)t >= (unsigned)size) continue;
-          atomicOr(&on_path[t >> 2], 1u << (t % 4 * 8 + tid));
-          mark(t);
-        }
-      __syncthreads();
+    clear();
+    const int nodes = first >= 0 && behind >= first && behind <= a.rows ? min(behind - first, AL_NODES) : 0;
+    if (tid < nodes) {
+      const int p = a.parents[first + tid];
+      parents[tid] = (short)(p >= 0 && p < tid ? p : -1);
+      drafted[tid] = a.drafted[first + tid];
     }
-    const double r = request >= 0 && a.repetition ? a.repetition[request] : 1.f, f = request >= 0 && a.frequency ? a.frequency[request] : 0.f, w = request >= 0 && a.presence ? a.presence[request] : 0.f;
+    __syncthreads();
+    if (held > 0) {
+      const int* tokens = a.tokens + (long long)request * a.token_stride;
+      const int len = (int)min((long long)held, (long long)a.token_stride);
+      auto one = [&](int t, int i) {
+        t = (int)((unsigned)t - (unsigned)lo);
+        if ((unsigned)t >= (unsigned)size) return;
+        if (i < prompt) atomicOr(&count[t], AL_PROMPT); else atomicAdd(&count[t], 1u);
+        mark(t);
+      };
+      int i = 0;
+      if (c.tokens_vec) {
+        const int whole = len / 4;
+#pragma unroll 4
+        for (int v = tid; v < whole; v += AL_THREADS) {
+          const i32x4 t = reinterpret_cast<const i32x4*>(tokens)[v];
+#pragma unroll
+          for (int e = 0; e < 4; e++) one(t[e], 4 * v + e);
+        }
+        i = whole * 4;
+      }
+      for (i += tid; i < len; i += AL_THREADS) one(tokens[i], i);
+    }
+    for (int i = max(bias0, 0) + tid; i < min(bias1, a.n_biases); i += AL_THREADS) {
+      const int t = (int)((unsigned)a.bias_tokens[i] - (unsigned)lo);
+      if ((unsigned)t >= (unsigned)size) continue;
+      atomicMax(&bias[t], (unsigned)i + 1);
+      mark(t);
+    }
+    if (tid < rows && row0 + tid >= first && row0 + tid < first + nodes)       // a thread for each row's path
+      for (int j = row0 + tid - first; j >= 0; j = parents[j]) {
+        const int t = (int)((unsigned)drafted[j] - (unsigned)lo);
+        if ((unsigned)t >= (unsigned)size) continue;
+        atomicOr(&on_path[t >> 2], 1u << (t % 4 * 8 + tid));
+        mark(t);
+      }
+    __syncthreads();
     const double inverse = 1.0 / r;
     constexpr unsigned ALL = (1u << E) - 1;
     auto changed = [&](T x, int t, int row) {          // an element that something may apply to, but for the mask
@@ -121,46 +196,18 @@ __global__ void __launch_bounds__(AL_THREADS) adjust_logits_kernel(AdjustCall c)
       const unsigned b = a.bias_tokens ? bias[t] : 0u;
       if (n == 0 && b == 0) return x;                  // on another row's path
       double y = (float)x;
-      if (n) y *= y > 0.0 ? inverse : r;
-      if (n & ~AL_PROMPT) y -= f * (n & ~AL_PROMPT) + w;
+      if (n) y *= y > 0.0 ? inverse : (double)r;
+      if (n & ~AL_PROMPT) y -= (double)f * (n & ~AL_PROMPT) + w;
       if (b) y += a.bias_values[b - 1];
       return (T)(float)y;
     };
-    // A thread's groups, neighbours of neighbouring threads', the rows one behind the other: four under way
-    struct At { int row, t; };
-    auto next = [&](At at) {
-      if (++at.row == rows) { at.row = 0; at.t += AL_THREADS * E; }
-      return at;
-    };
     auto group = [&](const At& at) {                   // bits of its elements: something may apply; ruled out
       const int m = __builtin_amdgcn_readfirstlane(mask_of[at.row]);
-      const unsigned apply = any ? touched[at.t >> 5] >> (at.t & 31) & ALL : 0u;
+      const unsigned apply = touched[at.t >> 5] >> (at.t & 31) & ALL;
       return u32x2{apply, (unsigned)m < (unsigned)a.n_masks ? ~a.masks[(long long)m * a.mask_stride + ((lo + at.t) >> 5)] >> (at.t & 31) & ALL : 0u};
     };
-    auto load = [&](V& x, const At& at) {
-      const T* from = reinterpret_cast<const T*>(a.logits) + (long long)(row0 + at.row) * a.row_stride + lo + at.t;
-      if (E > 1 && at.t + E > size) {
-#pragma unroll
-        for (int e = 0; e < E; e++)
-          if (at.t + e < size) x[e] = from[e];
-      } else {
-        x = *reinterpret_cast<const V*>(from);
-      }
-    };
-    At at{0, tid * E};
-    while (at.t < size) {
-      V x[AL_BATCH];
+    while (ats[0].t < size) {
       u32x2 bits[AL_BATCH];
-      At ats[AL_BATCH];
-#pragma unroll
-      for (int u = 0; u < AL_BATCH; u++) {
-        ats[u] = at;
-        at = next(at);
-      }
-      if (!c.in_place)
-#pragma unroll
-        for (int u = 0; u < AL_BATCH; u++)
-          if (ats[u].t < size) load(x[u], ats[u]);
 #pragma unroll
       for (int u = 0; u < AL_BATCH; u++) bits[u] = ats[u].t < size ? group(ats[u]) : u32x2{0u, 0u};
       if (c.in_place)                                  // only what changes, and is not ruled out as a whole
@@ -177,40 +224,46 @@ __global__ void __launch_bounds__(AL_THREADS) adjust_logits_kernel(AdjustCall c)
 #pragma unroll
           for (int e = 0; e < E; e++)
             if (ours >> e & 1) x[u][e] = changed(x[u][e], t + e, row);
-#pragma unroll
-        for (int e = 0; e < E; e++)
-          if (out >> e & 1) x[u][e] = (T)-INFINITY;
-        T* to = reinterpret_cast<T*>(a.out) + (long long)(row0 + row) * a.out_stride + lo + t;
-        if (E > 1 && t + E > size) {
-#pragma unroll
-          for (int e = 0; e < E; e++)
-            if (t + e < size) to[e] = x[u][e];
-        } else {
-          *reinterpret_cast<V*>(to) = x[u];
-        }
+        store_group<T, E>(reinterpret_cast<T*>(a.out) + (long long)(row0 + row) * a.out_stride + lo + t, x[u], out, size - t);
       }
+      begin();
     }
   }
 }
 
-template <typename T, int E>
-hipError_t launch_adjust(hipStream_t s, const AdjustCall& c) {
-  const bool counted = c.a.tokens || c.a.drafted;
-  const size_t lds = ((size_t)c.part / 32 + (counted ? c.part : 0) + (c.a.bias_tokens ? c.part : 0) + (c.a.drafted ? c.part / 4 : 0)) * sizeof(unsigned);
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(adjust_logits_kernel<T, E>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  const dim3 grid((c.a.rows + c.rows_per - 1) / c.rows_per, (unsigned)(((int64_t)c.a.vocab + c.part - 1) / c.part));
-  return launch(adjust_logits_kernel<T, E>, grid, dim3(AL_THREADS), lds, s, c);
-}
 template <typename T>
-hipError_t launch_adjust(hipStream_t s, const AdjustCall& c) {
+hipError_t launch_adjust(hipStream_t s, const AdjustCall& c0) {
   constexpr int E = 16 / sizeof(T);
-  auto fits = [&](const void* p, int64_t stride) { return aligned(p, 16) && (stride % E == 0 || c.a.rows == 1); };
-  return fits(c.a.logits, c.a.row_stride) && fits(c.a.out, c.a.out_stride) ? launch_adjust<T, E>(s, c) : launch_adjust<T, 1>(s, c);
+  AdjustCall c = c0;
+  const sts_adjust_logits& a = c.a;
+  auto parts = [&] { return ((int64_t)a.vocab + c.part - 1) / c.part; };
+  auto groups = [&] { return ((int64_t)a.rows + c.rows_per - 1) / c.rows_per; };
+  auto workgroups = [&] { return parts() * groups(); };
+  // All rows' first parts first: a text's tokens have low numbers more often than others, and what takes longest had better not begin last. The launch's y ends
+  // at 65535.
+  auto grid = [&] {
+    c.parts_first = parts() > 65535;
+    return c.parts_first ? dim3((unsigned)parts(), (unsigned)groups()) : dim3((unsigned)groups(), (unsigned)parts());
+  };
+  const bool counted = a.tokens || a.drafted;
+  c.rows_per = 1;
+  if (!counted && !a.bias_tokens) {
+    c.part = AL_MASK_BATCH * AL_MASK_THREADS * E;
+    while (c.part > AL_LEAST && workgroups() < AL_WORKGROUPS) c.part /= 2;
+    const dim3 g = grid();
+    return launch(mask_logits_kernel<T, E>, g, dim3(AL_MASK_THREADS), 0, s, c);
+  }
+  c.part = AL_PART;
+  if (a.drafted && a.n_requests > 0) {                 // equal shares of a request's rows, where they have alike numbers
+    const int mean = std::max(1, (a.rows + a.n_requests / 2) / a.n_requests), shares = (mean + AL_ROWS - 1) / AL_ROWS;
+    c.rows_per = (mean + shares - 1) / shares;
+    while (c.rows_per > 1 && workgroups() < AL_WORKGROUPS) c.rows_per = (c.rows_per + 1) / 2;
+  }
+  while (c.part > AL_LEAST && workgroups() < AL_WORKGROUPS) c.part /= 2;
+  const size_t lds = ((size_t)c.part / 32 + (counted ? c.part : 0) + (a.bias_tokens ? c.part : 0) + (a.drafted ? c.part / 4 : 0)) * sizeof(unsigned);
+  const dim3 g = grid();
+  return launch(adjust_logits_kernel<T, E>, g, dim3(AL_THREADS), lds, s, c);
 }
-
 }  // namespace
 }  // namespace sts
 
@@ -233,10 +286,6 @@ extern "C" int sts_op_adjust_logits(const sts_adjust_logits* a, void* stream) {
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   OnStreamDevice dev(s);
   if (dev.error() != hipSuccess) return op_result(dev.error());
-  const int rows_per = a->drafted ? AL_ROWS : 1;
-  const int64_t blocks = (a->rows + rows_per - 1) / rows_per;
-  int part = AL_PART;
-  while (part > AL_LEAST && blocks * ((a->vocab + (int64_t)part - 1) / part) < AL_WORKGROUPS) part /= 2;
-  const AdjustCall c{*a, part, rows_per, in_place, a->tokens && aligned(a->tokens, 16) && a->token_stride % 4 == 0};
+  const AdjustCall c{*a, 1, 1, in_place, a->tokens && aligned(a->tokens, 16) && a->token_stride % 4 == 0, false};
   return op_result(a->dtype == STS_F32 ? launch_adjust<float>(s, c) : a->dtype == STS_BF16 ? launch_adjust<bf16>(s, c) : launch_adjust<f16>(s, c));
 }

@@ -314,53 +314,50 @@ struct TreeCall {
 
 // What a row sees of an item's pages.
 struct Seen {
-  const unsigned short* mask;
-  int first, end;                                // the page of the first node; the item's last page + 1
-  __device__ __forceinline__ unsigned page(int pg) const { return pg >= end ? 0u : pg < first ? 0xFFFFu : mask[pg - first]; }
+  const unsigned short* masks;
+  int row, first, end;                           // node row, the page of the first node, the item's last page + 1
+  __device__ __forceinline__ unsigned page(int pg) const { return pg >= end ? 0u : pg < first ? 0xFFFFu : masks[row * AT_MASK + pg - first]; }
 };
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
-// Adds what the elements of V that are no numbers bring to the rows that see them (the products took 0 for them: another branch's infinity must not
-// become 0 * inf in a row that does not see it). p > 0 times an infinity or NaN is that. Seldom. From page pg0 on; `table`: of the whole request.
-template <typename T, int D>
-__device__ __forceinline__ void add_odd(f32x16 (&o)[D / 32], const TreeCall<T>& c, const Item& it, int pg0, const int* table, const Seen& seen, int kvh, int lh) {
-  for (int t = pg0 * OP_PAGE; t < min(it.len, it.pg1 * OP_PAGE); t++) {
-    const int page = table[t / OP_PAGE];
-    if ((unsigned)page >= (unsigned)c.pool_pages) continue;
-    const bool here = seen.page(t / OP_PAGE) >> (t % OP_PAGE) & 1;
-    const T* v = c.pool + ((size_t)page * c.n_kv + kvh) * 2 * OP_PAGE * D + OP_PAGE * D + t % OP_PAGE;
-#pragma unroll
-    for (int b = 0; b < D / 32; b++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) {
-        const float x = (float)v[(b * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)) * OP_PAGE];
-        if (here && !finite(x)) o[b][r] += x;
-      }
-  }
-}
-// Whether some of eight elements are no numbers: an exponent of ones carries into the sign's place.
+// Eight elements as the products may take them, those that are no numbers as 0: an exponent of ones carries into the sign's place. True if there were some.
 template <typename T>
-__device__ __forceinline__ unsigned odd_bits(u32x4 x) {
+__device__ __forceinline__ bool without_odd(u32x4& x) {
   constexpr unsigned EXP = std::is_same<T, f16>::value ? 0x7C007C00u : 0x7F807F80u, ONE = std::is_same<T, f16>::value ? 0x04000400u : 0x00800080u;
   unsigned any = 0;
 #pragma unroll
-  for (int i = 0; i < 4; i++) any |= (x[i] & EXP) + ONE;
-  return any & 0x80008000u;
+  for (int i = 0; i < 4; i++) {
+    const unsigned odd = ((x[i] & EXP) + ONE) >> 15 & 0x00010001u;
+    x[i] &= ~(odd * 0xFFFFu);
+    any |= odd;
+  }
+  return any != 0;
 }
-// Those as 0, as the products may take them. True if one of the first `tokens` elements was there.
-template <typename T>
-__device__ __forceinline__ bool without_odd(u32x4& x, int tokens) {
-  typedef typename Mfma<T>::V V;
-  V v = __builtin_bit_cast(V, x);
-  bool odd = false;
-#pragma unroll
-  for (int e = 0; e < 8; e++)
-    if (!finite((float)v[e])) {
-      odd |= e < tokens;
-      v[e] = (T)0.f;
+// Adds what those elements of V bring to the rows that see them, where the wave has stored its rows (first, .. of the item's): another branch's infinity must
+// not become 0 * inf in a row that does not see it. p > 0 times an infinity or NaN is that. Seldom. The item's pages from pg0 on; `table`: of the whole request.
+template <typename T, int D>
+__device__ __forceinline__ void add_odd(const TreeCall<T>& c, const Item& it, int first, int rows, int pg0, const int* table, int kvh) {
+  wait_vmem<0>();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+  const int lane = threadIdx.x & 63;
+#pragma unroll 1
+  for (int t = pg0 * OP_PAGE; t < min(it.len, it.pg1 * OP_PAGE); t++) {
+    const int page = table[t / OP_PAGE];
+    if ((unsigned)page >= (unsigned)c.pool_pages) continue;
+    const T* v = c.pool + ((size_t)page * c.n_kv + kvh) * 2 * OP_PAGE * D + OP_PAGE * D + t % OP_PAGE;
+#pragma unroll 1
+    for (int i = lane; i < rows * D; i += 64) {
+      const int r = first + i / D, d = i % D, row = (it.row0 + r) / c.heads, head = kvh * c.heads + (it.row0 + r) % c.heads;
+      const float x = (float)v[d * OP_PAGE];
+      if (finite(x) || !(Seen{c.plan.masks, row, it.cached / OP_PAGE, it.pg1}.page(t / OP_PAGE) >> (t % OP_PAGE) & 1)) continue;
+      if (it.part >= 0) {
+        c.plan.outs[((size_t)(it.part + r) * c.n_kv + kvh) * D + d] += x;
+      } else {
+        T* to = c.out + (long long)row * c.out_stride + head * D + d;
+        *to = (T)((float)*to + x);
+      }
     }
-  x = __builtin_bit_cast(u32x4, v);
-  return odd;
+  }
 }
 
 template <int D>
@@ -437,7 +434,7 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
   // Q^T operand: column l32 is row l32 of the item
   V qf[KSTEPS];
   const int vrow = it.row0 + min(l32, it.rows - 1), row = vrow / c.heads, head = kvh * c.heads + vrow % c.heads;
-  const Seen seen{c.plan.masks + (size_t)row * AT_MASK, it.cached / OP_PAGE, it.pg1};
+  const Seen seen{c.plan.masks, row, it.cached / OP_PAGE, it.pg1};
   const int mixed = min(max(it.cached / OP_PAGE - it.pg0, 0), npg) >> 1;         // the first block that is not two pages of context of the item's
   {
     const T* q = c.q + (long long)row * c.q_stride + head * D + lh * 8;
@@ -476,16 +473,10 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
 #pragma unroll
       for (int r = 0; r < 16; r++)                    // register r: page r >> 3 of the pair, token 8 * half + (r & 7)
         if (!(see >> r & 1)) s[r] = -INFINITY;
-      unsigned bits = 0;                              // what lies behind the nodes may be anything: 0 * V must be 0
 #pragma unroll
-      for (int u = 0; u < 2; u++)
+      for (int u = 0; u < 2; u++)                     // what lies behind the nodes may be anything: 0 * V must be 0
 #pragma unroll
-        for (int bb = 0; bb < DB; bb++) bits |= odd_bits<T>(vr[u][bb]);
-      if (__any(bits != 0))
-#pragma unroll
-        for (int u = 0; u < 2; u++)
-#pragma unroll
-          for (int bb = 0; bb < DB; bb++) odd |= without_odd<T>(vr[u][bb], pg + u < it.pg1 ? it.len - (pg + u) * OP_PAGE - 8 * lh : 0);
+        for (int bb = 0; bb < DB; bb++) odd |= without_odd<T>(vr[u][bb]);
     }
     float mx = s[0];
 #pragma unroll
@@ -541,7 +532,6 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
     step(i, 0, va);
     if (i + 1 < nblk) step(i + 1, 1, vb);
   }
-  if (__any(odd)) add_odd<T, D>(o, c, it, it.pg0 + 2 * mixed, table - it.pg0, seen, kvh, lh);
   l_run += __shfl_xor(l_run, 32, 64);
   if (__any(bad)) l_run = NAN;
 
@@ -567,6 +557,7 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
       if (lh == 0) c.plan.stats[at] = f32x2{m2, l_run};
     }
   }
+  if (__any(odd)) add_odd<T, D>(c, it, 0, it.rows, it.pg0 + 2 * mixed, table - it.pg0, kvh);
 }
 
 // ---- wide items, a workgroup: tiles of four pages go global -> LDS, two stages deep, a page a wave. KB = 2: every wave takes 32 rows over all the pages;
@@ -599,7 +590,7 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
   const int page1 = page_id(1);
   V qf[KSTEPS];
   const int vrow = it.row0 + min(block * 32 + l32, it.rows - 1);
-  const Seen seen{c.plan.masks + (size_t)(vrow / c.heads) * AT_MASK, it.cached / OP_PAGE, it.pg1};
+  const Seen seen{c.plan.masks, vrow / c.heads, it.cached / OP_PAGE, it.pg1};
   {
     const T* q = c.q + (long long)(vrow / c.heads) * c.q_stride + (kvh * c.heads + vrow % c.heads) * D + 8 * lh;
 #pragma unroll
@@ -751,11 +742,9 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
       unsigned char* vt = arena + (kt & 1) * STAGE + TILE;
       for (int i = tid; i < TILE / 16; i += 256) {
         u32x4 x = *reinterpret_cast<const u32x4*>(vt + i * 16);
-        if (odd_bits<T>(x)) {
-          const int pg = it.pg0 + kt * 4 + i / (PAGE / 16);
-          here |= without_odd<T>(x, pg < it.pg1 ? it.len - pg * OP_PAGE - 8 * (i & 1) : 0);
-          *reinterpret_cast<u32x4*>(vt + i * 16) = x;
-        }
+        if (!without_odd<T>(x)) continue;
+        here = true;
+        *reinterpret_cast<u32x4*>(vt + i * 16) = x;
       }
       odd |= __syncthreads_or(here);
     }
@@ -796,7 +785,6 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
     }
   }
   if (my_rows > 0 && my_pages == 0) {
-    if (odd) add_odd<T, D>(o, c, it, it.pg0 + 4 * mixed, table - it.pg0, seen, kvh, rh);
 #pragma unroll
     for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -819,8 +807,12 @@ __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>&
     }
     if (lane2 < my_rows) {
       if (it.part >= 0) c.plan.stats[(size_t)(it.part + block * 32 + lane2) * c.n_kv + kvh] = f32x2{m2, l_run};
-      else if (c.lse) c.lse[(long long)(vrow / c.heads) * c.n_q + kvh * c.heads + vrow % c.heads] = LN2 * (m2 + __builtin_amdgcn_logf(l_run));
+      else if (c.lse) {
+        const int v = it.row0 + block * 32 + lane2;
+        c.lse[(long long)(v / c.heads) * c.n_q + kvh * c.heads + v % c.heads] = LN2 * (m2 + __builtin_amdgcn_logf(l_run));
+      }
     }
+    if (odd) add_odd<T, D>(c, it, block * 32, my_rows, it.pg0 + 4 * mixed, table - it.pg0, kvh);
   }
   __syncthreads();                                       // before the next item's K lands there
 }
@@ -830,15 +822,18 @@ __global__ void __launch_bounds__(256, 2) attn_tree_kernel(TreeCall<T> c) {
   __shared__ __align__(16) unsigned char smem[attn_tree_lds<D>()];
   // With 8 KV heads a head's workgroups are all on one XCD: the tiles of a request find each other's pages in its L2.
   const int slot = blockIdx.x / c.n_kv, kvh = blockIdx.x % c.n_kv;
-  const Range r = c.plan.ranges[slot * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
-  if (c.plan.header->tag != c.tag || r.first.rows == 0) return;
-  Item it = r.first;
-  for (int i = r.next;; i++) {
+  const Range& r = c.plan.ranges[slot * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
+  auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  auto take = [&](const Item& x) { return Item{scalar(x.row0), scalar(x.rows), scalar(x.request), scalar(x.pg0), scalar(x.pg1), scalar(x.part), scalar(x.cached), scalar(x.len)}; };
+  Item it = take(r.first);
+  const int next = scalar(r.next), end = scalar(r.end);
+  if (c.plan.header->tag != c.tag || it.rows == 0) return;
+  for (int i = next;; i++) {
     if (it.rows > 2 * AT_ROWS) run_wide<T, D, 2>(smem, c, it, kvh);
     else if (it.rows > AT_ROWS) run_wide<T, D, 1>(smem, c, it, kvh);
     else run_narrow<T, D>(smem, c, it, kvh);
-    if (i >= r.end) break;
-    it = c.plan.items[i];
+    if (i >= end) break;
+    it = take(c.plan.items[i]);
   }
 }
 
