@@ -466,7 +466,8 @@ typedef struct {
   int32_t dtype;                        /* STS_BF16 or STS_F16: of q, pool and out */
   int32_t n_requests, max_rows;         /* max_rows up to 65536: length of parents, positions, rows of q and out */
   int32_t n_q, n_kv, d;                 /* n_q / n_kv up to 32, n_kv up to 256, d 64 or 128 */
-  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read; times (max_rows * n_q / n_kv / 128 + n_requests) up to 2^30 */
+  int32_t pool_pages, max_pages;        /* max_pages: entries of a table row that may be read; (max_pages + 8) times (max_rows / (128 / (n_q / n_kv)) + n_requests), in whole
+                                           numbers, up to 2^30 */
   int64_t table_stride;                 /* >= max_pages */
   const int32_t *tables, *cached;       /* [n_requests][table_stride], with the nodes' pages; [n_requests]: tokens before the nodes */
   const int32_t *row_starts, *parents;  /* [n_requests + 1]; [max_rows]: number of a node's parent in its request, -1: none */

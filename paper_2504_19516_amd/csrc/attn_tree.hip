@@ -58,8 +58,8 @@ struct Plan {
 };
 
 int slots_of(int n_kv) { return std::max(1, AT_SLOTS / n_kv); }
-// tiles: all rows in whole ones, and one begun for each request
-int64_t max_segments(int n, int max_rows, int heads) { return (int64_t)max_rows * heads / AT_TILE + n; }
+// tiles: of whole nodes, and for each request one that is not full
+int64_t max_segments(int n, int max_rows, int heads) { return (int64_t)max_rows / (AT_TILE / heads) + n; }
 int64_t max_items(int n, int max_rows, int n_q, int n_kv) { return max_segments(n, max_rows, n_q / n_kv) + 4 * slots_of(n_kv); }
 int64_t max_part_rows(int max_rows, int n_q, int n_kv) { return (int64_t)2 * max_rows * (n_q / n_kv) + (int64_t)slots_of(n_kv) * AT_TILE; }
 
@@ -146,10 +146,10 @@ __device__ void deal_out(const PlanCall& c) {
     s.rows = nodes * c.heads;
     s.pages = (cached[i] + nodes + OP_PAGE - 1) / OP_PAGE;
     s.kind = s.rows <= AT_ROWS;
-    // tiles of alike numbers of 32 rows, of whole nodes
-    const int blocks = (s.rows + AT_ROWS - 1) / AT_ROWS, most = (blocks + 3) / 4;
-    s.per = (blocks + most - 1) / most * AT_ROWS / c.heads * c.heads;
-    s.tiles = (s.rows + s.per - 1) / s.per;
+    // tiles of alike numbers of whole nodes
+    const int most = AT_TILE / c.heads, tiles = (nodes + most - 1) / most, of_tile = (nodes + tiles - 1) / tiles;
+    s.per = of_tile * c.heads;
+    s.tiles = (nodes + of_tile - 1) / of_tile;
     return s;
   };
   auto tile_cost = [&](const Shape& s) { return s.pages + (s.kind ? AT_NARROW_START : AT_WIDE_START); };

@@ -260,6 +260,8 @@ TREES = [
     (256, 256, 64, [(32, "tree", 3), (5, "chain", 2)]),
     (32, 8, 128, [(3, "tree", 255), (2047, "tree", 200)]),
     (2, 2, 64, [(1 + i % 37, "tree" if i % 3 else "chain", 1 + i % 5) for i in range(1000)]),
+    (58, 2, 64, [(30, "tree", 256), (5, "chain", 200), (77, "tree", 1), (0, "star", 5)]),
+    (14, 2, 128, [(300, "tree", 256), (17, "tree", 19)]),
 ]
 KINDS = {"chain": lambda rng, m: chain(m), "tree": random_tree, "star": lambda rng, m: star(m), "forest": lambda rng, m: random_tree(rng, m, min(m, 3))}
 
