@@ -483,7 +483,7 @@ int sts_op_attn_tree(const sts_tree_batch* b, const void* q, int64_t q_stride, c
 /* Logits before a token is chosen. With n the times that a token stands in the output of the row's request, and s whether it stands in its prompt or output:
  *   y = x / repetition (x > 0) or x * repetition, where s;  y -= frequency * n;  y -= presence, where n > 0;  y += bias;  -inf, where the row's mask has a 0
  * in 64 bits, rounded once. Elements that nothing applies to keep their bits. The output: tokens[prompt_len .. len) of the request, and of a drafted node's row the
- * tokens of the node and its ancestors. */
+ * tokens of the node and its ancestors (of a request's first 256 rows). */
 typedef struct {
   int32_t dtype, rows, vocab, n_requests;      /* rows up to 65535, vocab up to 2^30 */
   int64_t row_stride, out_stride;       /* elements from row to row */
@@ -511,6 +511,12 @@ typedef struct {
   int32_t *lens, *counts;               /* [n_requests]: cached + count, and the nodes on the path (0: no rows, more than 256, or node 0 is none; lens then cached) */
   int32_t* path;                        /* [max_rows]: numbers of a request's nodes on the path, from its first row on, -1 behind them; rows of no request are left as they were */
   int32_t* next_token;                  /* [n_requests]: chosen[] of the last; -1 without one */
+  /* The pages behind the path, which sts_op_block_tables gave to the nodes, go back onto the end of free_pages in the requests' order (tables NULL: they stay with
+   * the requests). None does if n_free is out of range or they do not fit. Their K and V may still be moved: sts_op_tree_compact comes before the next append. */
+  int32_t max_pages, free_capacity;     /* as for sts_op_block_tables, as are the following */
+  int64_t table_stride;
+  const int32_t* tables;
+  int32_t *free_pages, *n_free;         /* n_free [1]: raised by their number */
 } sts_tree_accept;
 int sts_op_tree_accept(const sts_tree_accept* a, void* stream);
 /* K and V of the path's nodes to tokens cached, cached + 1, ... of their requests, in all layers' pools. The pages of tokens that move may not be another request's.

@@ -13,7 +13,7 @@
 namespace sts {
 namespace {
 
-constexpr int TA_NODES = 256, TA_LAYERS = 256;
+constexpr int TA_NODES = 256, TA_LAYERS = 256, TA_THREADS = 256;
 constexpr int TA_ROWS = 4;                             // rows of a wave under way
 
 // Rows of a request; none where row_starts is out of range.
@@ -64,6 +64,45 @@ __global__ void __launch_bounds__(256) tree_accept_kernel(sts_tree_accept a) {
   }
 }
 
+// Pages behind the paths, back onto the stack of free ones. One workgroup: a thread has neighbouring requests.
+__global__ void __launch_bounds__(TA_THREADS) tree_release_kernel(sts_tree_accept a) {
+  __shared__ int waves[TA_THREADS / 64];
+  const int n = a.n_requests, tid = threadIdx.x, per = (n + TA_THREADS - 1) / TA_THREADS, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  auto pages_of = [](int tokens) { return (tokens + OP_PAGE - 1) / OP_PAGE; };
+  // of a request: the first page behind its path, and how many the nodes' rows had
+  auto behind = [&](int i, int* page) {
+    int first;
+    const int nodes = nodes_of(a.row_starts, i, a.max_rows, &first), c = a.cached[i];
+    *page = 0;
+    if (c < 0 || c > a.max_pages * (long long)OP_PAGE - nodes) return 0;
+    *page = pages_of(c + a.counts[i]);
+    return pages_of(c + nodes) - *page;
+  };
+  int sum = 0, page;
+  for (int i = i0; i < i1; i++) sum += behind(i, &page);
+  int x = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if ((tid & 63) >= o) x += y;
+  }
+  if ((tid & 63) == 63) waves[tid >> 6] = x;
+  const int free = *a.n_free;
+  __syncthreads();
+  int at = x - sum, total = 0;
+#pragma unroll
+  for (int w = 0; w < TA_THREADS / 64; w++) {
+    if (w < tid >> 6) at += waves[w];
+    total += waves[w];
+  }
+  if (free < 0 || free > a.free_capacity - total) return;
+  for (int i = i0; i < i1; i++) {
+    const int m = behind(i, &page);
+    for (int e = 0; e < m; e++) a.free_pages[free + at++] = a.tables[i * a.table_stride + page + e];
+  }
+  if (tid == 0) *a.n_free = free + total;
+}
+
 struct CompactCall { sts_tree_compact a; void* pools[TA_LAYERS]; };
 
 template <int D>
@@ -87,8 +126,8 @@ __global__ void __launch_bounds__(256) tree_compact_kernel(CompactCall c) {
   constexpr int CPR = D / 8, VPL = D / 64;             // 16-byte chunks of a K row; elements of a V column a lane
   for (int j0 = 0; j0 < count; j0 += 64) {             // 64 rows' places, one a lane
     const int j = j0 + lane, node = j < count ? a.path[first + j] : -1;
-    const long long src = node > j ? place(node) : -1, dst = src >= 0 ? place(j) : -1;
-    const bool moves = src >= 0 && dst >= 0;
+    const long long dst = place(j), src = place(node);              // on the way together
+    const bool moves = node > j && src >= 0 && dst >= 0;
     unsigned long long left = __ballot(moves);
     while (left) {                                     // the next rows that move, four at most
       u32x4 k[TA_ROWS];
@@ -132,10 +171,13 @@ extern "C" int sts_op_tree_accept(const sts_tree_accept* a, void* stream) {
   if (a->n_requests == 0) return STS_OK;
   if (!a->cached || !a->row_starts || !a->lens || !a->counts || !a->next_token) return STS_EINVAL;
   if (a->max_rows > 0 && (!a->parents || !a->tokens || !a->chosen || !a->path)) return STS_EINVAL;
+  if (a->tables && (!a->free_pages || !a->n_free || a->max_pages < 0 || a->max_pages > (1 << 26) || a->free_capacity < 0 || a->table_stride < a->max_pages)) return STS_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   OnStreamDevice dev(s);
   if (dev.error() != hipSuccess) return op_result(dev.error());
-  return op_result(launch(tree_accept_kernel, dim3((a->n_requests + 3) / 4), dim3(256), 0, s, *a));
+  hipError_t e = launch(tree_accept_kernel, dim3((a->n_requests + 3) / 4), dim3(256), 0, s, *a);
+  if (e == hipSuccess && a->tables) e = launch(tree_release_kernel, dim3(1), dim3(TA_THREADS), 0, s, *a);
+  return op_result(e);
 }
 
 extern "C" int sts_op_tree_compact(const sts_tree_compact* a, void* const* pools, int32_t n_layers, void* stream) {

@@ -142,7 +142,8 @@ class AdjustLogits(C.Structure):
 
 class TreeAccept(C.Structure):
     """sts_tree_accept"""
-    _fields_ = _fields(C.c_int32, "n_requests max_rows") + _fields(C.c_void_p, "cached row_starts parents tokens chosen lens counts path next_token")
+    _fields_ = _fields(C.c_int32, "n_requests max_rows") + _fields(C.c_void_p, "cached row_starts parents tokens chosen lens counts path next_token") + _fields(
+        C.c_int32, "max_pages free_capacity") + _fields(C.c_int64, "table_stride") + _fields(C.c_void_p, "tables free_pages n_free")
 
 
 class TreeCompact(C.Structure):

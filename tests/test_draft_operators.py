@@ -82,6 +82,9 @@ def test_tree_accept_refuses(sts):  # noqa: F811
     good = dict(n_requests=3, max_rows=20, cached=A, row_starts=2 * A, parents=3 * A, tokens=4 * A, chosen=5 * A, lens=6 * A, counts=7 * A, path=8 * A, next_token=9 * A)
     for change in [dict(n_requests=-1), dict(n_requests=4097), dict(max_rows=-1)] + [{k: None} for k in good if k not in ("n_requests", "max_rows")]:
         refused(sts, sts.op_tree_accept, sts.TreeAccept, good, **change)
+    pages = dict(good, max_pages=4, free_capacity=9, table_stride=4, tables=10 * A, free_pages=11 * A, n_free=12 * A)
+    for change in [dict(free_pages=None), dict(n_free=None), dict(max_pages=-1), dict(max_pages=(1 << 26) + 1, table_stride=1 << 27), dict(free_capacity=-1), dict(table_stride=3)]:
+        refused(sts, sts.op_tree_accept, sts.TreeAccept, pages, **change)
     sts.op_tree_accept(sts.TreeAccept(**{**good, "n_requests": 0}))
     assert sts.lib().sts_op_tree_accept(None, None) == sts.EINVAL
 

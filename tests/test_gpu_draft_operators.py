@@ -760,6 +760,36 @@ def test_tree_accept_of_rows_that_are_no_nodes(sts):  # noqa: F811
         assert got["counts"] == [1, 0, 0] and got["path"] == [0, 777, 777]
 
 
+@pytest.mark.parametrize("sizes", [[40], [40, 0, 1, 200, 16, 256], [3] * 700])
+def test_tree_accept_gives_pages_back(sts, sizes):  # noqa: F811
+    """The pages behind the paths, in the requests' order; where they do not fit, or the number of free ones is out of range, none."""
+    rng = np.random.default_rng(len(sizes))
+    trees, n = [random_tree(rng, m) for m in sizes], len(sizes)
+    tokens = [rng.integers(0, 3, m).tolist() for m in sizes]
+    chosen = [rng.integers(0, 3, m).tolist() for m in sizes]
+    cached = rng.integers(0, 100, n).tolist()
+    width = max(-(-(c + m) // 16) for c, m in zip(cached, sizes))
+    tables = np.arange(n * width, dtype=np.int32).reshape(n, width) + 1000
+    counts = [len(accept_reference(*x)[0]) for x in zip(trees, tokens, chosen)]
+    back = [int(p) for c, m, k, row in zip(cached, sizes, counts, tables) for p in row[-(-(c + k) // 16):-(-(c + m) // 16)]]
+    assert back
+    old = list(range(5))
+    for free, capacity, given in ((5, 5 + len(back), back), (0, 900 + len(back), back), (5, 4 + len(back), []), (-1, 900 + len(back), []), (901, 900, [])):
+        with Device() as dev:
+            _, d, a = run_accept(sts, dev, cached, trees, tokens, chosen)
+            stack, number = dev.ints(old[:max(free, 0)] + [-7] * (capacity - min(max(free, 0), 5))), dev.ints([free])
+            a.max_pages, a.table_stride, a.tables, a.free_pages, a.free_capacity, a.n_free = width, width, dev.ints(tables), stack, capacity, number
+            sts.op_tree_accept(a)
+            dev.sync()
+            got = dev.get(stack, capacity, "i32").tolist()
+            assert dev.get(number, 1, "i32")[0] == free + len(given)
+            if given:
+                assert got == old[:free] + back + [-7] * (capacity - free - len(back))
+            else:
+                assert back[0] not in got
+            assert dev.get(d["counts"], n, "i32").tolist() == counts
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("n_kv,d,sizes,layers", [(8, 128, [26], 3), (2, 64, [5, 1, 0, 64, 40], 2), (4, 64, [256, 200], 1), (1, 128, [9] * 70, 2), (3, 64, [30] * 5, 4)])
 def test_tree_compact(sts, dtype, n_kv, d, sizes, layers):  # noqa: F811
@@ -809,3 +839,148 @@ def test_tree_compact_moves_nothing_out_of_range(sts):  # noqa: F811
             moved[name] = np.unique(np.argwhere(dev.get(pool, old.shape, "bf16") != old)[:, 0]).tolist()
     assert moved.pop("none") == [0, 4] and moved.pop("starts behind") == [0]
     assert all(m == [4] for m in moved.values()), moved
+
+
+# ------------------------------------------------------------------------------------------ all together
+def test_steps_that_verify_drafts_eager_and_replayed(sts):  # noqa: F811
+    """Four requests whose trees of drafted tokens are verified step by step -- pages and places, positions, head norms with rotation and append, attention, logits (the library's GEMM),
+    penalties, biases and a mask, the target's choice, the accepted path with its pages, the cache rows -- eagerly and as a graph of two steps that hand lengths, tables, free
+    pages and the cache to each other on the device. Everything is checked behind every step against 64 bits and against a host's model of the cache."""
+    rng = np.random.default_rng(88)
+    n_q, n_kv, d, vocab, dtype, layers = 8, 2, 64, 256, "bf16", 2
+    heads, ld, width, pages, eps = n_q // n_kv, (n_q + 2 * n_kv) * d, 14, 80, 1e-6
+    trees = [random_tree(rng, 7), chain(4), [-1, 0, 0, 1, 1, -2, 2], star(5)]
+    n, rows, starts = len(trees), sum(map(len, trees)), starts_of(trees)
+    rope = rope_of(sts, "bands", d, 0)
+    gains = gains_of(rng, d, dtype, 0)
+    w = rounded(rng.standard_normal((vocab, n_q * d)) / 8, dtype)
+    history = rng.integers(0, vocab, (n, 32)).astype(np.int32)
+    held, prompts = np.array([32, 7, 0, 20], np.int32), np.array([10, 7, 0, 0], np.int32)
+    penalties = [np.float32([1.2, 1.0, 1.5, 2.0]), np.float32([0.1, 0.0, 0.3, 0.2]), np.float32([0.5, 0.2, 0.0, 0.1])]
+    biases = [[(t, 30.0 + t) for t in range(3)] + [(200, -5.0)]] * n           # some few tokens are likely: drafts are right now and then
+    masks, mask_rows = rng.random((1, vocab)) < 0.9, np.where(np.arange(rows) % 5 == 1, 0, -1).astype(np.int32)
+    masks[0, :3] = True
+    with Device() as dev:
+        s = dev.stream()
+        free = rng.permutation(pages).astype(np.int32)
+        free_dev, count = dev.put(free), [dev.ints([pages]), dev.ints([0])]
+        lens, tables = [dev.ints([0] * n), dev.ints([0] * n)], dev.ints(np.full((n, width), -1))
+        pools = [dev.put(np.zeros((pages, n_kv, 32 * d), np.uint16)) for _ in range(layers)]
+        counts_of_rows, parents = dev.ints([len(t) for t in trees]), dev.ints([p for t in trees for p in t])
+        norm = sts.HeadNorm(dtype=1, eps=eps, q_gain=dev.put(gains[0], dtype), k_gain=dev.put(gains[1], dtype))
+        size = sts.attn_tree_workspace(n, rows, n_q, n_kv, d)
+        ws, w_dev, lp_ws = dev.alloc(size), dev.put(w, dtype), dev.alloc(max(sts.op_logprobs_workspace(0, rows, vocab, 1), 16))
+        flat = [e for b in biases for e in b]
+        fixed = dict(tokens=dev.ints(history), token_stride=32, lens=dev.ints(held), prompt_lens=dev.ints(prompts), repetition=dev.put(penalties[0]), frequency=dev.put(penalties[1]),
+                     presence=dev.put(penalties[2]), bias_starts=dev.ints(starts_of(biases)), bias_tokens=dev.ints([t for t, _ in flat]), bias_values=dev.put(np.float32([b for _, b in flat])),
+                     n_biases=len(flat), masks=dev.ints(words_of(masks)), n_masks=1, mask_stride=vocab // 32, mask_rows=dev.ints(mask_rows))
+        halves = []
+        for _ in range(2):                                                     # each of a graph's two steps has buffers of its own
+            b = {k: dev.ints([0] * rows) for k in ("requests", "places", "positions", "drafted", "chosen", "path", "behind")}
+            b.update({k: dev.ints([9] * n) for k in ("full", "counts", "next")}, starts=dev.ints([0] * (n + 1)), status=dev.ints([9]),
+                     qkv=[dev.alloc(rows * ld * 2) for _ in range(layers)], q=[dev.alloc(rows * n_q * d * 2) for _ in range(layers)],
+                     k=[dev.alloc(rows * n_kv * d * 2) for _ in range(layers)], out=[dev.alloc(rows * n_q * d * 2) for _ in range(layers)], logits=dev.alloc(rows * vocab * 4),
+                     adjusted=dev.alloc(rows * vocab * 4), chance=dev.alloc(rows * 4))
+            halves.append(b)
+
+        def step(a):
+            b, x = 1 - a, halves[a]
+            sts.op_block_tables(sts.BlockTables(n_requests=n, max_pages=width, max_rows=rows, free_capacity=pages, table_stride=width, cached=lens[a], added=counts_of_rows, free_pages=free_dev,
+                                                n_free=count[a], tables=tables, lens=x["full"], row_starts=x["starts"], requests=x["requests"], positions=x["behind"], places=x["places"],
+                                                n_free_left=count[b], status=x["status"]), s)
+            batch = sts.TreeBatch(dtype=1, n_requests=n, max_rows=rows, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, max_pages=width, table_stride=width, tables=tables, cached=lens[a],
+                                  row_starts=x["starts"], parents=parents, positions=x["positions"], workspace=ws, workspace_bytes=size)
+            sts.op_attn_tree_plan(batch, s)
+            for i in range(layers):
+                sts.op_norm_rope(norm, rope, sts.RopeRows(dtype=1, rows=rows, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, q=x["qkv"][i], q_stride=ld, q_out=x["q"][i], q_out_stride=n_q * d,
+                                                          k=x["qkv"][i] + n_q * d * 2, k_stride=ld, k_out=x["k"][i], k_out_stride=n_kv * d, v=x["qkv"][i] + (n_q + n_kv) * d * 2, v_stride=ld,
+                                                          pool=pools[i], positions=x["positions"], places=x["places"]), s)
+                sts.op_attn_tree(batch, x["q"][i], n_q * d, pools[i], x["out"][i], n_q * d, None, 0.0, s)
+            sts.op_gemm_noalloc(x["out"][-1], w_dev, x["logits"], rows, vocab, n_q * d, "64x128", 1, 0, s)
+            sts.op_adjust_logits(sts.AdjustLogits(dtype=0, rows=rows, vocab=vocab, n_requests=n, row_stride=vocab, out_stride=vocab, logits=x["logits"], out=x["adjusted"],
+                                                  requests=x["requests"], row_starts=x["starts"], parents=parents, drafted=x["drafted"], **fixed), s)
+            sts.op_logprobs(sts.Logprobs(dtype=0, rows=rows, vocab=vocab, top_k=1, row_stride=vocab, logits=x["adjusted"], top_logprob=x["chance"], top_token=x["chosen"], workspace=lp_ws,
+                                         workspace_bytes=max(sts.op_logprobs_workspace(0, rows, vocab, 1), 16)), s)
+            sts.op_tree_accept(sts.TreeAccept(n_requests=n, max_rows=rows, cached=lens[a], row_starts=x["starts"], parents=parents, tokens=x["drafted"], chosen=x["chosen"], lens=lens[b],
+                                              counts=x["counts"], path=x["path"], next_token=x["next"], max_pages=width, free_capacity=pages, table_stride=width, tables=tables,
+                                              free_pages=free_dev, n_free=count[b]), s)
+            sts.op_tree_compact(sts.TreeCompact(n_requests=n, max_rows=rows, n_kv=n_kv, d=d, pool_pages=pages, max_pages=width, table_stride=width, tables=tables, cached=lens[a],
+                                                row_starts=x["starts"], counts=x["counts"], path=x["path"]), pools, s)
+
+        kv = [[[np.zeros((0, n_kv, d), np.float32)] * 2 for _ in range(n)] for _ in range(layers)]       # the host's cache: by layer and request K and V
+        accepted = []
+
+        def fill(a):
+            x, qkv = halves[a], [rounded(rng.standard_normal((rows, ld)), dtype) for _ in range(layers)]
+            drafted = rng.integers(0, 3, rows).astype(np.int32)
+            for p, y in zip(x["qkv"], qkv):
+                dev.write(p, stored(y, dtype))
+            dev.write(x["drafted"], drafted)
+            return qkv, drafted
+
+        def check(a, qkv, drafted, last):
+            """Step a's buffers against the cache before it, which then takes the path in; `last`: nothing ran behind it."""
+            x, cached = halves[a], [len(kv[0][r][0]) for r in range(n)]
+            assert dev.get(x["status"], 1, "i32")[0] == 0 and dev.get(x["starts"], n + 1, "i32").tolist() == starts.tolist()
+            positions = dev.get(x["positions"], rows, "i32")
+            ups = [up for t in trees for up in ancestors(t)]
+            owner = np.repeat(np.arange(n), [len(t) for t in trees])
+            assert positions.tolist() == [-1 if up is None else cached[r] + len(up) - 1 for r, up in zip(owner, ups)]
+            for i in range(layers):
+                y = qkv[i].reshape(rows, n_q + 2 * n_kv, d).astype(np.float64)
+                got_q, got_k = dev.get(x["q"][i], (rows, n_q, d), dtype), dev.get(x["k"][i], (rows, n_kv, d), dtype)
+                for got, part, g in ((got_q, y[:, :n_q], gains[0]), (got_k, y[:, n_q:n_q + n_kv], gains[1])):
+                    want, sz = norm_rope_reference(sts, rope, part, g, np.float64(np.float32(eps)), 0, positions)
+                    near(got, want, norm_rope_bound(want, sz, dtype))
+                at = [slice(starts[r], starts[r + 1]) for r in range(n)]
+                new = [[np.concatenate([kv[i][r][0], got_k[at[r]]]), np.concatenate([kv[i][r][1], qkv[i].reshape(rows, -1, d)[at[r], n_q + n_kv:]])] for r in range(n)]
+                got = dev.get(x["out"][i], (rows, n_q, d), dtype)
+                want, bound, _, _ = tree_reference(got_q, [m[0] for m in new], [m[1] for m in new], cached, trees, heads, d ** -0.5, dtype)
+                near(got, want, bound)
+                kv[i] = new
+            logits = dev.get(x["logits"], (rows, vocab), "f32")
+            wide = got.reshape(rows, -1).astype(np.float64)
+            near(logits, wide @ w.T, n_q * d * 2.0 ** -23 * np.abs(wide) @ np.abs(w.T) + 1e-6)
+            adjusted, chosen = dev.get(x["adjusted"], (rows, vocab), "f32"), dev.get(x["chosen"], rows, "i32")
+            real = [r for r, up in enumerate(ups) if up is not None]
+            padded = [t if None not in ancestors(t) else [p if p >= -1 else -1 for p in t] for t in trees]       # rows that are no nodes: looked at by nobody
+            c = dict(x=logits, requests=owner, tokens=history, lens=held, prompts=prompts, penalties=penalties, trees=padded, drafted=drafted, biases=biases, masks=masks, mask_rows=mask_rows)
+            want = adjust_reference(logits.astype(np.float64), *[c[k] for k in ("requests", "tokens", "lens", "prompts", "penalties", "trees", "drafted", "biases", "masks", "mask_rows")])[real]
+            fine = np.isfinite(want)
+            assert np.array_equal(adjusted[real][~fine], want[~fine])
+            near(adjusted[real][fine], want[fine], np.abs(want[fine]) * 2.0 ** -23 + 1e-38)
+            assert np.array_equal(chosen, adjusted.argmax(1))
+            counts, path = dev.get(x["counts"], n, "i32"), dev.get(x["path"], rows, "i32")
+            for r in range(n):
+                want, token = accept_reference(trees[r], drafted[starts[r]:starts[r + 1]], chosen[starts[r]:starts[r + 1]])
+                assert counts[r] == len(want) and path[starts[r]:starts[r + 1]].tolist() == want + [-1] * (len(trees[r]) - len(want)) and dev.get(x["next"], n, "i32")[r] == token
+                keep = list(range(cached[r])) + [cached[r] + j for j in want]
+                for i in range(layers):
+                    kv[i][r] = [m[keep] for m in kv[i][r]]
+                accepted.append(len(want))
+            if last:
+                length, t = [len(kv[0][r][0]) for r in range(n)], dev.get(tables, (n, width), "i32")
+                own = [p for r in range(n) for p in t[r, :-(-length[r] // 16)]]
+                left = dev.get(count[1 - a], 1, "i32")[0]
+                assert dev.get(lens[1 - a], n, "i32").tolist() == length and left == pages - len(own)
+                assert sorted(own + dev.get(free_dev, pages, "i32")[:left].tolist()) == list(range(pages))       # no page is lost or held twice
+                for i in range(layers):
+                    p = dev.get(pools[i], (pages, n_kv, 32 * d), dtype)
+                    for r in range(n):
+                        q = p[t[r, :-(-length[r] // 16)]]
+                        assert np.array_equal(q[..., :16 * d].reshape(-1, n_kv, 16, d).transpose(0, 2, 1, 3).reshape(-1, n_kv, d)[:length[r]], kv[i][r][0])
+                        assert np.array_equal(q[..., 16 * d:].reshape(-1, n_kv, d, 16).transpose(0, 3, 1, 2).reshape(-1, n_kv, d)[:length[r]], kv[i][r][1])
+
+        for a in range(2):
+            inputs = fill(a)
+            step(a)
+            dev.sync()
+            check(a, *inputs, last=True)
+        replay = dev.graph(s, lambda: (step(0), step(1)))
+        for _ in range(8):
+            inputs = [fill(0), fill(1)]
+            replay()
+            dev.sync()
+            check(0, *inputs[0], last=False)
+            check(1, *inputs[1], last=True)
+        assert max(accepted) >= 3 and min(accepted) == 1 and max(len(x[0]) for x in kv[0]) > 32
