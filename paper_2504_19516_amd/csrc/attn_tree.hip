@@ -863,46 +863,43 @@ template <typename T, int D>
 __global__ void __launch_bounds__(256) attn_tree_join_few_kernel(TreeCall<T> c) {
   constexpr int LANES = D / 4, WAVES = 4, APART = 64 / LANES * WAVES;       // lanes of a part, parts side by side
   __shared__ f32x4 sums[WAVES][LANES];
-  __shared__ float ls[WAVES];
+  __shared__ f32x2 ls[WAVES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = blockIdx.x / c.n_q, head = blockIdx.x % c.n_q, kvh = head / c.heads;
   const Pieces p = pieces_of(c, row, head % c.heads);
   if (p.done) return;
   auto row_of = [&](int j) { return (size_t)(p.base + j * p.step) * c.n_kv + kvh; };
-  float m = -INFINITY;
-  for (int j = lane; j < p.count; j += 64) m = fmaxf(m, c.plan.stats[row_of(j)][0]);
-  m = wave_max(m);
-  float l = 0.f;
+  float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](float m1, float l1, f32x4 o1) {         // another part's maximum, sum (0 of one without scores above -inf, or NaN) and output
+    const float now = fmaxf(m, m1), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now), f1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - now);
+    l = (m == -INFINITY ? l : l * f) + (m1 == -INFINITY ? l1 : l1 * f1);
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = o[e] * f + o1[e] * f1;
+    m = now;
+  };
   const int first = wave * (64 / LANES) + lane / LANES, e4 = lane % LANES * 4;
-#pragma unroll 4
-  for (int j = first; j < p.count; j += APART) {
-    const size_t part = row_of(j);
-    const f32x2 st = c.plan.stats[part];
-    const f32x4 x = *reinterpret_cast<const f32x4*>(c.plan.outs + part * D + e4);
-    const float w = st[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - m);
-    l += st[0] == -INFINITY ? st[1] : st[1] * w;                 // 0 of a part without scores above -inf, or NaN
+  for (int j0 = first; j0 < p.count; j0 += AT_JOIN_BATCH * APART) {
+    f32x2 st[AT_JOIN_BATCH];
+    f32x4 x[AT_JOIN_BATCH];
 #pragma unroll
-    for (int e = 0; e < 4; e++) o[e] += x[e] * w;
+    for (int u = 0; u < AT_JOIN_BATCH; u++) {
+      const size_t part = row_of(min(j0 + u * APART, p.count - 1));
+      st[u] = c.plan.stats[part];
+      x[u] = *reinterpret_cast<const f32x4*>(c.plan.outs + part * D + e4);
+    }
+#pragma unroll
+    for (int u = 0; u < AT_JOIN_BATCH; u++)
+      if (j0 + u * APART < p.count) add(st[u][0], st[u][1], x[u]);
   }
 #pragma unroll
-  for (int s = LANES; s < 64; s <<= 1) {
-    l += __shfl_xor(l, s, 64);
-#pragma unroll
-    for (int e = 0; e < 4; e++) o[e] += __shfl_xor(o[e], s, 64);
-  }
+  for (int s = LANES; s < 64; s <<= 1) add(__shfl_xor(m, s, 64), __shfl_xor(l, s, 64), f32x4{__shfl_xor(o[0], s, 64), __shfl_xor(o[1], s, 64), __shfl_xor(o[2], s, 64), __shfl_xor(o[3], s, 64)});
   if (lane < LANES) sums[wave][lane] = o;
-  if (lane == 0) ls[wave] = l;
+  if (lane == 0) ls[wave] = f32x2{m, l};
   __syncthreads();
   if (wave > 0 || lane >= LANES) return;
-  l = 0.f;
 #pragma unroll
-  for (int w = 0; w < WAVES; w++) l += ls[w];
-  o = sums[0][lane];
-#pragma unroll
-  for (int w = 1; w < WAVES; w++)
-#pragma unroll
-    for (int e = 0; e < 4; e++) o[e] += sums[w][lane][e];
+  for (int w = 1; w < WAVES; w++) add(ls[w][0], ls[w][1], sums[w][lane]);
   finish_row<T, D>(c, row, head, e4, p, m, l, o);
 }
 
@@ -917,7 +914,12 @@ __global__ void __launch_bounds__(256) attn_tree_join_kernel(TreeCall<T> c) {
   if (p.done) return;
   auto row_of = [&](int j) { return (size_t)(p.base + j * p.step) * c.n_kv + kvh; };
   float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  f32x4 o = {0.f, 0.f, 0.f, 0.f}, x[AT_JOIN_BATCH];
+  auto fetch = [&](int j) {                              // past the last the last again, which counts for nothing
+#pragma unroll
+    for (int u = 0; u < AT_JOIN_BATCH; u++) x[u] = *reinterpret_cast<const f32x4*>(c.plan.outs + row_of(min(j + u, p.count - 1)) * D + lane * 4);
+  };
+  if (p.count > 0) fetch(0);
   for (int j0 = 0; j0 < p.count; j0 += LANES) {
     const f32x2 st = j0 + lane < p.count ? c.plan.stats[row_of(j0 + lane)] : f32x2{-INFINITY, 0.f};
     float now = st[0];
@@ -938,9 +940,7 @@ __global__ void __launch_bounds__(256) attn_tree_join_kernel(TreeCall<T> c) {
     l += z;
     const int n = min(LANES, p.count - j0);
     for (int j = 0; j < n; j += AT_JOIN_BATCH) {
-      f32x4 x[AT_JOIN_BATCH];
-#pragma unroll
-      for (int u = 0; u < AT_JOIN_BATCH; u++) x[u] = *reinterpret_cast<const f32x4*>(c.plan.outs + row_of(j0 + min(j + u, n - 1)) * D + lane * 4);
+      if (j0 + j > 0) fetch(j0 + j);
 #pragma unroll
       for (int u = 0; u < AT_JOIN_BATCH; u++) {
         const float wj = __shfl(w, j + u, LANES);

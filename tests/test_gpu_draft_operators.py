@@ -984,3 +984,74 @@ def test_steps_that_verify_drafts_eager_and_replayed(sts):  # noqa: F811
             check(0, *inputs[0], last=False)
             check(1, *inputs[1], last=True)
         assert max(accepted) >= 3 and min(accepted) == 1 and max(len(x[0]) for x in kv[0]) > 32
+
+
+def test_drafts_behind_32_bits(sts):  # noqa: F811
+    """A pool of more than 2^31 elements and 2^32 bytes: its last pages are written by the append, read by the attention, and their rows moved."""
+    rng = np.random.default_rng(23)
+    n_kv, heads, d, pages = 16, 2, 128, 34000
+    n_q, cached, trees = heads * n_kv, [17, 40, 3], [random_tree(rng, 20), chain(9), random_tree(rng, 40)]
+    lens, width = [c + len(t) for c, t in zip(cached, trees)], 4
+    tables = np.array([[pages - 1, 5, pages - 2, 9], [pages - 3, pages - 4, 0, pages - 7], [1, pages - 5, pages - 6, 4]], np.int32)
+    assert pages * n_kv * 32 * d > 2 ** 31
+    everything = sum(lens)
+    qkv = rounded(rng.standard_normal((everything, (n_q + 2 * n_kv) * d)), "bf16")
+    places = np.array([tables[r, t // 16] * 16 + t % 16 for r in range(3) for t in range(lens[r])], np.int32)
+    rope, ld, starts = sts.Rope(rotary_dim=2, theta=1e4), qkv.shape[1], starts_of(trees)
+    with Device() as dev:
+        pool, base = dev.alloc(pages * n_kv * 32 * d * 2), dev.put(qkv, "bf16")
+        k_out, q_out = dev.alloc(everything * n_kv * d * 2), dev.alloc(everything * n_q * d * 2)
+        sts.op_norm_rope(sts.HeadNorm(eps=1e-6), rope, sts.RopeRows(dtype=1, rows=everything, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, q=base, q_stride=ld, q_out=q_out, q_out_stride=n_q * d,
+                                                                    k=base + n_q * d * 2, k_stride=ld, k_out=k_out, k_out_stride=n_kv * d, v=base + (n_q + n_kv) * d * 2, v_stride=ld,
+                                                                    pool=pool, positions=dev.ints([0] * everything), places=dev.put(places)))
+        rows, size = int(starts[-1]), sts.attn_tree_workspace(3, int(starts[-1]), n_q, n_kv, d)
+        q = rounded(rng.standard_normal((rows, n_q, d)), "bf16")
+        out, table = dev.alloc(rows * n_q * d * 2), dev.ints(tables)
+        common = dict(n_requests=3, max_rows=rows, n_kv=n_kv, d=d, pool_pages=pages, max_pages=width, table_stride=width, tables=table, cached=dev.ints(cached), row_starts=dev.ints(starts))
+        batch = sts.TreeBatch(dtype=1, n_q=n_q, parents=dev.ints([p for t in trees for p in t]), workspace=dev.alloc(size), workspace_bytes=size, **common)
+        sts.op_attn_tree_plan(batch)
+        sts.op_attn_tree(batch, dev.put(q, "bf16"), n_q * d, pool, out, n_q * d)
+        paths = [[0, 3, 19], [0, 8], [0, 1, 2, 30, 39]]
+        path = [x for p, t in zip(paths, trees) for x in p + [-1] * (len(t) - len(p))]
+        sts.op_tree_compact(sts.TreeCompact(counts=dev.ints([3, 2, 5]), path=dev.ints(path), **common), [pool])
+        dev.sync()
+        got, got_k = dev.get(out, (rows, n_q, d), "bf16"), dev.get(k_out, (everything, n_kv, d), "bf16")
+        page = np.stack([[dev.get(pool + int(p) * n_kv * 32 * d * 2, (n_kv, 32 * d), "bf16") for p in row] for row in tables])
+    first = np.concatenate([[0], np.cumsum(lens)])
+    k = [got_k[first[r]:first[r + 1]] for r in range(3)]
+    v = [qkv.reshape(everything, -1, d)[first[r]:first[r + 1], n_q + n_kv:] for r in range(3)]
+    want, bound, _, _ = tree_reference(q, k, v, cached, trees, heads, d ** -0.5, "bf16")
+    near(got, want, bound)
+    for r in range(3):
+        keep = list(range(cached[r])) + [cached[r] + j for j in paths[r]]
+        pk = page[r, :, :, :16 * d].reshape(width, n_kv, 16, d).transpose(0, 2, 1, 3).reshape(-1, n_kv, d)[:len(keep)]
+        pv = page[r, :, :, 16 * d:].reshape(width, n_kv, d, 16).transpose(0, 3, 1, 2).reshape(-1, n_kv, d)[:len(keep)]
+        assert np.array_equal(pk, k[r][keep]) and np.array_equal(pv, v[r][keep])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_adjust_logits_behind_32_bits(sts, dtype):  # noqa: F811
+    """Rows, histories and masks whose offsets pass 32 bits, out of place and in place."""
+    rng = np.random.default_rng(9)
+    vocab, rows, stride = 5003, 3, (1 << 31) // 2 + 7                     # the last row begins behind 2^31 elements
+    c = adjust_case(rng, dtype, vocab, [[-1]] * rows, 40, 3, 1.0)
+    c.update(trees=None, mask_rows=np.int32([2, 0, 1]))
+    size = 4 if dtype == "f32" else 2
+    with Device() as dev:
+        far = dev.alloc(2 * stride * size + vocab * size)
+        tokens, token_stride = dev.alloc(((2 << 30) + 40) * 4), 1 << 30
+        words = words_of(c["masks"])
+        masks, mask_stride = dev.alloc(((2 << 30) + words.shape[1]) * 4), 1 << 30
+        for r in range(rows):
+            dev.write(far + r * stride * size, stored(c["x"][r], dtype))
+            dev.write(tokens + r * token_stride * 4, c["tokens"][r])
+            dev.write(masks + r * mask_stride * 4, words[r])
+        a, out = adjust_description(sts, dev, dtype, c)
+        a.logits, a.row_stride, a.tokens, a.token_stride, a.masks, a.mask_stride = far, stride, tokens, token_stride, masks, mask_stride
+        sts.op_adjust_logits(a)
+        dev.sync()
+        check_adjusted(dev.get(out, (rows, vocab), dtype), c, dtype)
+        a.out, a.out_stride = far, stride
+        sts.op_adjust_logits(a)
+        dev.sync()
+        check_adjusted(np.stack([dev.get(far + r * stride * size, vocab, dtype) for r in range(rows)]), c, dtype)
