@@ -20,7 +20,7 @@ namespace {
 constexpr int AL_THREADS = 512, AL_NODES = 256;
 constexpr int AL_BATCH = 4;                            // groups of elements of a thread under way
 constexpr int AL_ROWS = 8;                             // rows of a workgroup, at most: a bit each
-constexpr int AL_PART = 4096, AL_LEAST = 1024, AL_WORKGROUPS = 1024;       // tokens of a part, fewer where there are fewer workgroups than that
+constexpr int AL_PART = 4096, AL_LEAST = 1024, AL_WORKGROUPS = 256;       // tokens of a part, fewer where there are fewer workgroups than that
 constexpr unsigned AL_PROMPT = 1u << 31;               // beside the count of the output
 
 constexpr int AL_MASK_THREADS = 256, AL_MASK_BATCH = 4;
