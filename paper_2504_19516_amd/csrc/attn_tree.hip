@@ -125,10 +125,10 @@ __device__ __forceinline__ bool request_ok(const PlanCall& c, int cached, int fi
 
 __device__ void deal_out(const PlanCall& c) {
   constexpr int N = OP_MAX_REQUESTS;
-  // by request: first row; places on the lines of wide and narrow segments, and the first wide and narrow segment (16 bits each would do for one kind: up
-  // to 2^16 rows of 32 heads are 2^14 tiles)
+  // by request: first row; places on the lines of wide and narrow segments; the first wide and narrow segment (2^16 rows of 32 heads are 2^14 tiles and one for each
+  // request); tiles (none of one that is not computed) and nodes of a tile
   __shared__ int start[N + 1], line_at[2][N + 1], cached[N], waves[4][AT_PLAN_THREADS / 64];
-  __shared__ unsigned short seg0[2][N + 1];
+  __shared__ unsigned short seg0[2][N + 1], tiles_of[N], nodes_of[N];
   const int n = c.n, tid = threadIdx.x;
   bool malformed = false;
   for (int i = tid; i <= n; i += AT_PLAN_THREADS) {
@@ -140,26 +140,27 @@ __device__ void deal_out(const PlanCall& c) {
   const bool ordered = !__syncthreads_or(malformed);
   struct Shape { int rows, pages, per, tiles, kind; };
   auto shape = [&](int i) {
-    const int nodes = start[i + 1] - start[i];
-    Shape s{0, 0, 0, 0, 0};
-    if (!ordered || nodes == 0 || !request_ok(c, cached[i], start[i], start[i + 1])) return s;
-    s.rows = nodes * c.heads;
-    s.pages = (cached[i] + nodes + OP_PAGE - 1) / OP_PAGE;
-    s.kind = s.rows <= AT_ROWS;
-    // tiles of alike numbers of whole nodes
-    const int most = AT_TILE / c.heads, tiles = (nodes + most - 1) / most, of_tile = (nodes + tiles - 1) / tiles;
-    s.per = of_tile * c.heads;
-    s.tiles = (nodes + of_tile - 1) / of_tile;
-    return s;
+    const int nodes = start[i + 1] - start[i], rows = nodes * c.heads;
+    return Shape{rows, (cached[i] + nodes + OP_PAGE - 1) / OP_PAGE, nodes_of[i] * c.heads, tiles_of[i], rows <= AT_ROWS};
   };
   auto tile_cost = [&](const Shape& s) { return s.pages + (s.kind ? AT_NARROW_START : AT_WIDE_START); };
   const int per = (n + AT_PLAN_THREADS - 1) / AT_PLAN_THREADS, r0 = min(n, tid * per), r1 = min(n, r0 + per);
   int sums[4] = {0, 0, 0, 0}, all[4];            // cost and segments, wide and narrow
+  const int most = AT_TILE / c.heads;            // nodes of a tile; a request's tiles have alike numbers of them
   for (int i = r0; i < r1; i++) {
+    const int nodes = start[i + 1] - start[i];
+    int tiles = 0, of_tile = 1;
+    if (ordered && nodes > 0 && request_ok(c, cached[i], start[i], start[i + 1])) {
+      tiles = (nodes + most - 1) / most;
+      of_tile = (nodes + tiles - 1) / tiles;
+      tiles = (nodes + of_tile - 1) / of_tile;
+    }
+    tiles_of[i] = (unsigned short)tiles;
+    nodes_of[i] = (unsigned short)of_tile;
+    if (tiles == 0) continue;
     const Shape s = shape(i);
-    if (s.tiles == 0) continue;
-    sums[s.kind] += s.tiles * tile_cost(s);
-    sums[2 + s.kind] += s.tiles;
+    sums[s.kind] += tiles * tile_cost(s);
+    sums[2 + s.kind] += tiles;
   }
   plan_scan(sums, all, waves);
   const float wide_work = AT_WIDE_WEIGHT * all[0];
@@ -191,7 +192,7 @@ __device__ void deal_out(const PlanCall& c) {
     Parts p{0, -1, 0, 0};
     if (s.tiles > 0) {
       const Line& l = lines[s.kind];
-      const int at = line_at[s.kind][i] + (row - start[i]) * c.heads / s.per * tile_cost(s);
+      const int at = line_at[s.kind][i] + (row - start[i]) / nodes_of[i] * tile_cost(s);
       p.step = s.kind ? AT_ROWS : AT_TILE;
       p.count = l.pieces(at, s.pages);
       p.base = (s.kind ? narrow_part : 0) + row * c.heads + p.step * l.first(at, s.pages);
