@@ -3,12 +3,14 @@
 //   y = x / r or x r (x > 0 or not), where the token stands in prompt or output;  y -= f n + (n > 0) w;  y += b;  -inf where ruled out
 //
 // with n the token's count in the output. A workgroup takes a part of the vocabulary for some rows in a row: it counts the history's tokens of its part in LDS, once for
-// all rows of a request, and adds and takes off again the few tokens of each drafted node's path. One bit for each token tells whether anything applies to it; of the
-// others nothing is computed, and in place they are not even read: a group of neighbouring elements goes to memory only where it changes, and without being read
-// where all of it is ruled out.
+// all rows of a request. One bit for each token tells whether anything may apply to it, eight more on which of the rows' paths it is (how often is counted where that is so:
+// seldom); of the others nothing is computed, and in place they are not even read: a group of neighbouring elements goes to memory only where it changes, and without being read
+// where all of it is ruled out. The arithmetic is in 64 bits, rounded to 32 and to the type: it runs for a few thousand elements of a row.
 //
-// Bound by memory where rows are copied, by latency for a few rows (history, LDS, elements one behind the other). The arithmetic is in 64 bits, rounded once to 32 and to the type: it
-// runs for the tokens that something applies to, a few thousand of a row.
+// Bound by memory where rows are copied (320 rows of 128256 in 32 bits, chains of five on histories of 1500: 83 us, a copy of as many bytes 68; without the arithmetic of what changes some 12
+// less, the rest is histories that are read and counted while little else is under way), by latency for a few rows (one row 6.5 us: descriptions, history, LDS, elements, one behind the
+// other) and for masks in place (256 rows of 16 bits, half of them masked, 30 MB: 12.5 us). Stores past the caches took 85 instead of 87 us on rows that change, but the log
+// probabilities that read them next took longer: 124 instead of 119 for both.
 #include <algorithm>
 #include <cmath>
 
@@ -17,13 +19,15 @@
 namespace sts {
 namespace {
 
-constexpr int AL_THREADS = 512, AL_NODES = 256;
-constexpr int AL_BATCH = 4;                            // groups of elements of a thread under way
+constexpr int AL_THREADS = 512, AL_NODES = 256;        // 256 / 512 / 1024 threads: 320 rows 81 / 84 / 88 us, 702 rows of 56507 170 / 147 / 206
+constexpr int AL_BATCH = 4;                            // groups of elements of a thread under way: 2 / 4 / 8 level, longer for few rows
 constexpr int AL_ROWS = 8;                             // rows of a workgroup, at most: a bit each
-constexpr int AL_PART = 4096, AL_LEAST = 1024, AL_WORKGROUPS = 256;       // tokens of a part, fewer where there are fewer workgroups than that
+// Tokens of a part, fewer where that leaves fewer workgroups than these. Parts of 2048 / 4096 / 8192: 320 rows 95 / 84 / 81 us, 702 rows 161 / 147 / 170. 256 / 512 / 1024 workgroups: geometric mean
+// of 24 calls of all sizes 9.9 / 10.0 / 10.3 us.
+constexpr int AL_PART = 4096, AL_LEAST = 1024, AL_WORKGROUPS = 256;
 constexpr unsigned AL_PROMPT = 1u << 31;               // beside the count of the output
 
-constexpr int AL_MASK_THREADS = 256, AL_MASK_BATCH = 4;
+constexpr int AL_MASK_THREADS = 256, AL_MASK_BATCH = 4;       // groups of a thread: 4 / 8 / 16, 256 masked rows 12.6 / 14.7 / 20 us
 
 struct AdjustCall {
   sts_adjust_logits a;
@@ -34,7 +38,8 @@ struct AdjustCall {
   __device__ __forceinline__ int first_row() const { return (parts_first ? blockIdx.y : blockIdx.x) * rows_per; }
 };
 
-// A group of elements, 16 bytes that may begin at any element: rows of odd lengths lie one behind the other as often as aligned ones.
+// A group of elements, 16 bytes that may begin at any element: rows of odd lengths lie one behind the other as often as aligned ones (702 rows of 56507 in 32 bits 87 us so,
+// 147 an element at a time).
 template <typename T, int E> struct Group {
   typedef T V __attribute__((ext_vector_type(E)));
   typedef V InMemory __attribute__((aligned(sizeof(T))));

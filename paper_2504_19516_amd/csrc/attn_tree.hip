@@ -14,6 +14,12 @@
 // for each token of the pages that hold nodes; it writes the nodes' positions; and it lays the segments of each kind end to end (pages, and the start and end of
 // a segment counted as pages) and cuts each line into equal shares, one for each workgroup or wave. Piece p of segment s lies in share k: s + k is its number and
 // (first row) + (rows of a share's tile) * k the place of its partial result, both without a further scan.
+//
+// Measured, 32 query and 8 KV heads of 128 in bf16, or 64 and 8 in fp16; us of the plan (once a step), and of products and join (each layer), medians under a trace:
+//   one tree of 26 nodes on 1500 tokens, 6 MB of pages a layer     6   13   4    latency: table, pages, one to three tiles, partial results, one behind the other
+//   64 chains of 5 on 1100 tokens (spread), 322 MB                 8   65   8    4.95 TB/s in the products: memory
+//   16 trees of 64 on 4096 tokens (spread), 270 MB                 9  130  14    0.53 PFLOP/s, 0.8 with the second numbers': see run_wide
+//   six trees of up to 33 on 14000 tokens, 64 heads, 238 MB        7   67  12    memory for the small trees (3.6 TB/s), matrix cores and exponentials for the large
 #include <algorithm>
 
 #include "attn_parts.h"
@@ -31,7 +37,8 @@ constexpr int AT_PLAN_THREADS = 512;
 constexpr int AT_JOIN_ROWS = 1024;              // up to so many (row, head) pairs four waves join each, beyond it a run of lanes
 constexpr int AT_JOIN_BATCH = 4;                // parts of a run under way
 // Start and end of a wide and of a narrow segment, and the smallest shares beyond them, in pages; what a page of a wide segment takes a workgroup, in
-// pages of a narrow one.
+// pages of a narrow one. Wide start and least share 8 and 4 / 4 and 4 / 6 and 2 / 4 and 2: one tree on 1500 tokens (four layers) 70 / - / 73 / 73 us, 16 trees (two) 287 / 288 / 287 / 287, six
+// of the larger shape (two) 161 / 162 / 160 / 159. Narrow least share 4 / 12: a request of two nodes on 420 tokens 17 / 20. Wide weight 1.25 / 2: level.
 constexpr int AT_WIDE_START = 8, AT_NARROW_START = 2, AT_WIDE_LEAST = 4, AT_NARROW_LEAST = 4;
 constexpr float AT_WIDE_WEIGHT = 1.25f;
 
@@ -564,6 +571,11 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
 // ---- wide items, a workgroup: tiles of four pages go global -> LDS, two stages deep, a page a wave. KB = 2: every wave takes 32 rows over all the pages;
 // KB = 1 (up to 64 rows): waves w and w + 2 take the same 32 rows over two of each tile's pages, and join what they have at the end. Products, order of the tokens and softmax
 // as in attn_prefill.hip, whose queries lie in a row where these come from any node.
+// What bounds 128 rows: of 16 trees' cycles matrix instructions take 46 % and vector instructions 43 %, and on these cards the two hardly overlap, whatever their order: the next tile's
+// first product between this one's exponentials, instruction by instruction, was level (298 and 300 us a step of two layers), as was reading K up to four steps ahead, or the first product
+// at a higher priority. The tiles of a request read its pages each for itself (530 MB a layer past L2 where K and V are 270): eight waves on 256 rows read them once and took 280 instead of
+// 301 us here, but 205 instead of 173 with six trees of different sizes and 79 instead of 70 with one tree.
+// KB = 1 instead of 2 for 33 to 64 rows: three chains of 16 on 161 tokens (two layers) 46 -> 39 us, on 3214 tokens 71 -> 60.
 template <typename T, int D, int KB>
 __device__ __forceinline__ void run_wide(unsigned char* smem, const TreeCall<T>& c, const Item& it, int kvh) {
   typedef typename Mfma<T>::V V;

@@ -10,7 +10,8 @@
 // and keeps them in LDS for all heads.
 //
 // Norms of heads: y = x / sqrt(mean(x^2) + eps) * gain before the rotation, in 32 bits. A head's row is then a run of neighbouring lanes (a power of two of them; those
-// beyond its vectors hold none), which add up their squares; the rows are still read once. Rows that do not come in vectors take a wave each and are read twice.
+// beyond its vectors hold none), which add up their squares; the rows are still read once. Rows that do not come in vectors take a wave each and are read twice. The norms
+// hide behind memory: the prefill below takes 38 to 41 us with them again and again on the same rows, 48 on rows that change (46.7 without norms); 130 rows 5.5 us.
 //
 // Bound by memory for prefills (8192 rows of 32 + 8 heads of 128: 201 MB in 44 us, 4.6 TB/s, where a plain copy takes 38), by latency for decodes
 // (64 rows 4 us). V columns stored 1 KB in a row by neighbouring lanes, both halves of a page at once, were level.
