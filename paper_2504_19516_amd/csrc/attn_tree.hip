@@ -41,6 +41,9 @@ constexpr int AT_JOIN_BATCH = 4;                // parts of a run under way
 // of the larger shape (two) 161 / 162 / 160 / 159. Narrow least share 4 / 12: a request of two nodes on 420 tokens 17 / 20. Wide weight 1.25 / 2: level.
 constexpr int AT_WIDE_START = 8, AT_NARROW_START = 2, AT_WIDE_LEAST = 4, AT_NARROW_LEAST = 4;
 constexpr float AT_WIDE_WEIGHT = 1.25f;
+// Pages up to which segments are neither cut nor strung together where there is a workgroup or wave for each: none / 8 / 16, us: four trees of six nodes behind two tokens (64 heads, one layer)
+// 26.7 / 18.2 / 18.2, 25 requests of two nodes on 76 tokens (two layers) 25.0 / 21.7 / 21.7, four chains of 16 on 129 (two) 37.2 / 37.6 / 33.2, one of 7 on 45 (two) 28.7 / 30.6 / 30.6.
+constexpr int AT_APART = 16;
 
 // A piece of a segment: rows row0 .. row0 + rows - 1 (node row * heads of a group + head) over the pages [pg0, pg1) of a request's table. part: number of its
 // first row's partial result, -1: it finishes its rows.
@@ -136,6 +139,7 @@ __device__ void deal_out(const PlanCall& c) {
   // request); tiles (none of one that is not computed) and nodes of a tile
   __shared__ int start[N + 1], line_at[2][N + 1], cached[N], waves[4][AT_PLAN_THREADS / 64];
   __shared__ unsigned short seg0[2][N + 1], tiles_of[N], nodes_of[N];
+  __shared__ int longest_of_all;
   const int n = c.n, tid = threadIdx.x;
   bool malformed = false;
   for (int i = tid; i <= n; i += AT_PLAN_THREADS) {
@@ -150,9 +154,9 @@ __device__ void deal_out(const PlanCall& c) {
     const int nodes = start[i + 1] - start[i], rows = nodes * c.heads;
     return Shape{rows, (cached[i] + nodes + OP_PAGE - 1) / OP_PAGE, nodes_of[i] * c.heads, tiles_of[i], rows <= AT_ROWS};
   };
-  auto tile_cost = [&](const Shape& s) { return s.pages + (s.kind ? AT_NARROW_START : AT_WIDE_START); };
   const int per = (n + AT_PLAN_THREADS - 1) / AT_PLAN_THREADS, r0 = min(n, tid * per), r1 = min(n, r0 + per);
-  int sums[4] = {0, 0, 0, 0}, all[4];            // cost and segments, wide and narrow
+  int sums[4] = {0, 0, 0, 0}, all[4], longest = 0;      // cost and segments, wide and narrow
+  if (tid == 0) longest_of_all = 0;
   const int most = AT_TILE / c.heads;            // nodes of a tile; a request's tiles have alike numbers of them
   for (int i = r0; i < r1; i++) {
     const int nodes = start[i + 1] - start[i];
@@ -166,19 +170,32 @@ __device__ void deal_out(const PlanCall& c) {
     nodes_of[i] = (unsigned short)of_tile;
     if (tiles == 0) continue;
     const Shape s = shape(i);
-    sums[s.kind] += tiles * tile_cost(s);
+    sums[s.kind] += tiles * (s.pages + (s.kind ? AT_NARROW_START : AT_WIDE_START));
     sums[2 + s.kind] += tiles;
+    longest = max(longest, s.pages);
   }
+  __syncthreads();
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, 64));
+  if ((tid & 63) == 0) atomicMax(&longest_of_all, longest);
   plan_scan(sums, all, waves);
+  longest = longest_of_all;
+  // Short segments that all find a workgroup or wave of their own: each is as long on its line as a share.
+  const bool apart = longest <= AT_APART && all[2] + (all[3] + 3) / 4 <= c.slots;
   const float wide_work = AT_WIDE_WEIGHT * all[0];
   int wide = all[0] == 0 ? 0 : (int)(c.slots * (wide_work / (wide_work + all[1])) + 0.5f);
-  wide = min(max(wide, (int)(all[0] > 0)), c.slots - (all[1] > 0));
+  wide = apart ? all[2] : min(max(wide, (int)(all[0] > 0)), c.slots - (all[1] > 0));
   const int narrow = 4 * (c.slots - wide);
   auto line = [&](int total, int count, int start, int least, int granule) {
-    const int share = max((total + max(count, 1) - 1) / max(count, 1), start + least);
+    const int share = apart ? start + longest : max((total + max(count, 1) - 1) / max(count, 1), start + least);
     return Line{share, start, granule, 1.f / (float)share};
   };
   const Line lines[2] = {line(all[0], wide, AT_WIDE_START, AT_WIDE_LEAST, 4), line(all[1], narrow, AT_NARROW_START, AT_NARROW_LEAST, 2)};
+  auto tile_cost = [&](const Shape& s) { return (apart ? longest : s.pages) + (s.kind ? AT_NARROW_START : AT_WIDE_START); };
+  if (apart) {
+    sums[0] = sums[2] * lines[0].share; sums[1] = sums[3] * lines[1].share;
+    all[0] = all[2] * lines[0].share; all[1] = all[3] * lines[1].share;
+  }
   const int narrow_part = c.max_rows * c.heads + wide * AT_TILE;
   if (tid == 0) {
     *c.plan.header = Header{c.tag, ordered ? start[n] : -1, 0};
