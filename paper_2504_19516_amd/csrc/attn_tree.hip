@@ -48,7 +48,8 @@ constexpr int AT_APART = 16;
 // A piece of a segment: rows row0 .. row0 + rows - 1 (node row * heads of a group + head) over the pages [pg0, pg1) of a request's table. part: number of its
 // first row's partial result, -1: it finishes its rows.
 struct Item { int row0, rows, request, pg0, pg1, part, cached, len; };
-struct Range { Item first; int next, end, pad[2]; };              // items of a wave: the first, and next .. end - 1; none if its rows are 0. The four of a workgroup with wide ones have the same
+// Items of a wave: the first, and next .. end - 1; none if its rows are 0. The four of a workgroup with wide ones (whose last tile may have few rows) have the same.
+struct Range { Item first; int next, end, wide, pad; };
 // Where a node row's partial results are: head h of a group in base + h + j * step, j < count. One: its one piece finishes it. count -1: gives NaN.
 struct Parts { int base, count, step, pad; };
 struct Header {
@@ -229,6 +230,7 @@ __device__ void deal_out(const PlanCall& c) {
     const Line& l = lines[kind];
     const int begin = k * l.share, end = begin + l.share;
     Range r{};
+    r.wide = !kind;
     if (begin < all[kind]) {
       int i = last_up_to(line_at[kind], n, begin);                // has tiles there: the last of several at one place
       Shape s = shape(i);
@@ -586,7 +588,7 @@ __device__ __forceinline__ void run_narrow(unsigned char* smem, const TreeCall<T
 }
 
 // ---- wide items, a workgroup: tiles of four pages go global -> LDS, two stages deep, a page a wave. KB = 2: every wave takes 32 rows over all the pages;
-// KB = 1 (up to 64 rows): waves w and w + 2 take the same 32 rows over two of each tile's pages, and join what they have at the end. Products, order of the tokens and softmax
+// KB = 1 (up to 64 rows, a last tile's few ones too): waves w and w + 2 take the same 32 rows over two of each tile's pages, and join what they have at the end. Products, order of the tokens and softmax
 // as in attn_prefill.hip, whose queries lie in a row where these come from any node.
 // What bounds 128 rows: of 16 trees' cycles matrix instructions take 46 % and vector instructions 43 %, and on these cards the two hardly overlap, whatever their order: the next tile's
 // first product between this one's exponentials, instruction by instruction, was level (298 and 300 us a step of two layers), as was reading K up to four steps ahead, or the first product
@@ -856,12 +858,12 @@ __global__ void __launch_bounds__(256, 2) attn_tree_kernel(TreeCall<T> c) {
   auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   auto take = [&](const Item& x) { return Item{scalar(x.row0), scalar(x.rows), scalar(x.request), scalar(x.pg0), scalar(x.pg1), scalar(x.part), scalar(x.cached), scalar(x.len)}; };
   Item it = take(r.first);
-  const int next = scalar(r.next), end = scalar(r.end);
+  const int next = scalar(r.next), end = scalar(r.end), wide = scalar(r.wide);
   if (c.plan.header->tag != c.tag || it.rows == 0) return;
   for (int i = next;; i++) {
-    if (it.rows > 2 * AT_ROWS) run_wide<T, D, 2>(smem, c, it, kvh);
-    else if (it.rows > AT_ROWS) run_wide<T, D, 1>(smem, c, it, kvh);
-    else run_narrow<T, D>(smem, c, it, kvh);
+    if (!wide) run_narrow<T, D>(smem, c, it, kvh);
+    else if (it.rows > 2 * AT_ROWS) run_wide<T, D, 2>(smem, c, it, kvh);
+    else run_wide<T, D, 1>(smem, c, it, kvh);
     if (i >= end) break;
     it = take(c.plan.items[i]);
   }

@@ -517,6 +517,25 @@ def test_tree_attention_of_the_most_requests(sts, dtype, n_q, n_kv, requests):  
     assert np.isfinite(got).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n_q,n_kv,d,nodes,requests", [(32, 1, 64, 17, 150), (32, 1, 64, 13, 200), (64, 8, 128, 241, 6)])
+def test_tree_attention_of_last_tiles_with_few_rows(sts, dtype, n_q, n_kv, d, nodes, requests):  # noqa: F811
+    """Trees whose last tile has 8 or 32 rows, in workgroups that have another tile behind it: more tiles than there are workgroups for a head."""
+    rng = np.random.default_rng(41)
+    q, k, v, tables, pages, cached, trees = tree_inputs(rng, dtype, [(int(rng.integers(0, 90)), "tree", nodes) for _ in range(requests)], n_q, n_kv, d)
+    pool = pool_of(k, v, tables, [c + len(t) for c, t in zip(cached, trees)], pages, dtype)
+    with Device() as dev:
+        got, lse, positions, call, at = run_tree(sts, dev, dtype, q, pool, tables, cached, trees, n_q // n_kv)
+        for _ in range(20):
+            call()
+        dev.sync()
+        assert np.array_equal(dev.get(at[0], got.shape, dtype), got)
+    for r in range(0, requests, 5):
+        a, b = r * nodes, (r + 1) * nodes
+        check_tree(got[a:b], lse[a:b], tree_reference(q[a:b], [k[r]], [v[r]], [cached[r]], [trees[r]], n_q // n_kv, d ** -0.5, dtype), [cached[r]], [trees[r]], positions[a:b])
+    assert np.isfinite(got).all()
+
+
 # ------------------------------------------------------------------------------------------ logits
 def adjust_reference(x, requests, tokens, lens, prompts, penalties, trees, drafted, biases, masks, mask_rows):
     """x [rows, vocab] float64; biases: by request a list of (token, value)."""
