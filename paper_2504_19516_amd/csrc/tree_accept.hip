@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(256) tree_accept_kernel(sts_tree_accept a) {
 
 // Pages behind the paths, back onto the stack of free ones. One workgroup: a thread has neighbouring requests.
 __global__ void __launch_bounds__(TA_THREADS) tree_release_kernel(sts_tree_accept a) {
-  __shared__ int waves[TA_THREADS / 64];
+  __shared__ long long waves[TA_THREADS / 64];         // row_starts out of order may name a row in many requests: sums of 64 bits
   const int n = a.n_requests, tid = threadIdx.x, per = (n + TA_THREADS - 1) / TA_THREADS, i0 = min(n, tid * per), i1 = min(n, i0 + per);
   auto pages_of = [](int tokens) { return (tokens + OP_PAGE - 1) / OP_PAGE; };
   // of a request: the first page behind its path, and how many the nodes' rows had
@@ -81,18 +81,19 @@ __global__ void __launch_bounds__(TA_THREADS) tree_release_kernel(sts_tree_accep
     *page = pages_of(c + a.counts[i]);
     return pages_of(c + nodes) - *page;
   };
-  int sum = 0, page;
+  long long sum = 0;
+  int page;
   for (int i = i0; i < i1; i++) sum += behind(i, &page);
-  int x = sum;
+  long long x = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
+    const long long y = __shfl_up(x, o, 64);
     if ((tid & 63) >= o) x += y;
   }
   if ((tid & 63) == 63) waves[tid >> 6] = x;
   const int free = *a.n_free;
   __syncthreads();
-  int at = x - sum, total = 0;
+  long long at = x - sum, total = 0;
 #pragma unroll
   for (int w = 0; w < TA_THREADS / 64; w++) {
     if (w < tid >> 6) at += waves[w];
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(TA_THREADS) tree_release_kernel(sts_tree_accep
     const int m = behind(i, &page);
     for (int e = 0; e < m; e++) a.free_pages[free + at++] = a.tables[i * a.table_stride + page + e];
   }
-  if (tid == 0) *a.n_free = free + total;
+  if (tid == 0) *a.n_free = free + (int)total;
 }
 
 struct CompactCall { sts_tree_compact a; void* pools[TA_LAYERS]; };

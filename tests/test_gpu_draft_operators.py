@@ -809,6 +809,19 @@ def test_tree_accept_gives_pages_back(sts, sizes):  # noqa: F811
             assert dev.get(d["counts"], n, "i32").tolist() == counts
 
 
+def test_tree_accept_of_rows_in_many_requests(sts):  # noqa: F811
+    """row_starts up and down between 0 and 2^24: 2^31 pages seem to lie behind the paths, and none is given back."""
+    n, rows, width = 4096, 1 << 24, 1 << 20
+    with Device() as dev:
+        stack, number, counts, lens = dev.ints([-7] * 100), dev.ints([5]), dev.ints([777] * n), dev.ints([777] * n)
+        sts.op_tree_accept(sts.TreeAccept(n_requests=n, max_rows=rows, cached=dev.ints([0] * n), row_starts=dev.ints([0, rows] * (n // 2) + [0]), parents=dev.alloc(4 * rows), tokens=dev.alloc(4 * rows),
+                                          chosen=dev.alloc(4 * rows), lens=lens, counts=counts, path=dev.alloc(4 * rows), next_token=dev.alloc(4 * n), max_pages=width, free_capacity=50,
+                                          table_stride=width, tables=dev.alloc(4 * n * width), free_pages=stack + 100, n_free=number))
+        dev.sync()
+        assert dev.get(stack, 100, "i32").tolist() == [-7] * 100 and dev.get(number, 1, "i32")[0] == 5
+        assert dev.get(counts, n, "i32").tolist() == [0] * n and dev.get(lens, n, "i32").tolist() == [0] * n
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("n_kv,d,sizes,layers", [(8, 128, [26], 3), (2, 64, [5, 1, 0, 64, 40], 2), (4, 64, [256, 200], 1), (1, 128, [9] * 70, 2), (3, 64, [30] * 5, 4)])
 def test_tree_compact(sts, dtype, n_kv, d, sizes, layers):  # noqa: F811
