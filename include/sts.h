@@ -496,7 +496,8 @@ typedef struct {
   const int32_t *lens, *prompt_lens;    /* [n_requests]: tokens in all, up to token_stride (taken as that beyond it), and of the prompt (NULL: 0) */
   const float *repetition, *frequency, *presence;       /* [n_requests]; NULL: 1, 0 and 0 */
   const int32_t *row_starts, *parents, *drafted;        /* [n_requests + 1], [rows], [rows]: the nodes, as for sts_op_attn_tree, and their tokens; drafted NULL: no nodes */
-  const int32_t *bias_starts, *bias_tokens; const float* bias_values;       /* [n_requests + 1], entries of each request; of several of one token the last counts; NULL: none */
+  const int32_t *bias_starts, *bias_tokens; const float* bias_values;       /* [n_requests + 1], entries of each request (none outside 0 .. n_biases - 1); of several of one token the last counts;
+                                           NULL: none */
   const uint32_t* masks;                /* [n_masks][mask_stride]: bit t % 32 of word t / 32 is 0 where token t is ruled out; NULL: none */
   const int32_t* mask_rows;             /* [rows]: mask of each row; outside 0 .. n_masks - 1: none */
 } sts_adjust_logits;

@@ -178,10 +178,12 @@ __global__ void __launch_bounds__(AL_THREADS) adjust_logits_kernel(AdjustCall c)
       }
       for (i += tid; i < len; i += AL_THREADS) one(tokens[i], i);
     }
-    for (int i = max(bias0, 0) + tid; i < min(bias1, a.n_biases); i += AL_THREADS) {
-      const int t = (int)((unsigned)a.bias_tokens[i] - (unsigned)lo);
+    // both ends of the request's entries within the list before anything is added to them: counted from 0, as an end may be any number
+    const unsigned bias_first = min(max(bias0, 0), a.n_biases), bias_count = max(min(max(bias1, 0), a.n_biases) - (int)bias_first, 0);
+    for (unsigned i = tid; i < bias_count; i += AL_THREADS) {
+      const int t = (int)((unsigned)a.bias_tokens[bias_first + i] - (unsigned)lo);
       if ((unsigned)t >= (unsigned)size) continue;
-      atomicMax(&bias[t], (unsigned)i + 1);
+      atomicMax(&bias[t], bias_first + i + 1);
       mark(t);
     }
     if (tid < rows && row0 + tid >= first && row0 + tid < first + nodes)       // a thread for each row's path

@@ -704,6 +704,24 @@ def test_adjust_logits_of_odd_values_and_numbers(sts):  # noqa: F811
             assert np.isneginf(got[2]).all() and np.isneginf(got[9]).all()
 
 
+@pytest.mark.parametrize("starts", [[0, 2 ** 31 - 1, 3, 6], [2 ** 31 - 300, 2 ** 31 - 1, 2, 6], [-2 ** 31, 2, 2 ** 31 - 511, 2 ** 31 - 1], [6, 2, 5, 1], [-5, -1, 4, 2000], [2 ** 31 - 1, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1],
+                                    [7, 4001, 4002, 4003]])
+def test_adjust_logits_bias_starts_out_of_range(sts, starts):  # noqa: F811
+    """Of a request's entries, bias_starts[i] to bias_starts[i + 1], those that the list has count, whatever the numbers; the list may be longer than a workgroup."""
+    rng = np.random.default_rng(51)
+    c = adjust_case(rng, "f32", 5000, [random_tree(rng, m) for m in (2, 3, 1)], 20, 0, 0.0)
+    for n in (6, 3000):
+        flat = list(zip(rng.integers(0, 5000, n).tolist(), np.float32(5 * rng.standard_normal(n)).tolist()))
+        c["biases"] = [flat[max(a, 0):max(b, 0)] for a, b in zip(starts, starts[1:])]
+        with Device() as dev:
+            for in_place in (False, True):
+                a, out = adjust_description(sts, dev, "f32", c, in_place)
+                a.bias_starts, a.bias_tokens, a.bias_values, a.n_biases = dev.ints(starts), dev.ints([t for t, _ in flat]), dev.put(np.array([b for _, b in flat], np.float32)), n
+                sts.op_adjust_logits(a)
+                dev.sync()
+                check_adjusted(dev.get(out, c["x"].shape, "f32"), c, "f32")
+
+
 def test_adjust_logits_same_bits_again_and_in_a_graph(sts):  # noqa: F811
     rng = np.random.default_rng(6)
     c = adjust_case(rng, "bf16", 33000, [random_tree(rng, m) for m in (8, 30, 1)], 900, 9, 0.3)
