@@ -158,18 +158,19 @@ __global__ void __launch_bounds__(AL_THREADS) adjust_logits_kernel(AdjustCall c)
     __syncthreads();
     if (held > 0) {
       const int* tokens = a.tokens + (long long)request * a.token_stride;
-      const int len = (int)min((long long)held, (long long)a.token_stride);
-      auto one = [&](int t, int i) {
+      // up to 2^31 - 1 tokens: an index that the next step takes past them is still a number of 32 bits without a sign
+      const unsigned len = (unsigned)min((long long)held, (long long)a.token_stride);
+      auto one = [&](int t, unsigned i) {
         t = (int)((unsigned)t - (unsigned)lo);
         if ((unsigned)t >= (unsigned)size) return;
-        if (i < prompt) atomicOr(&count[t], AL_PROMPT); else atomicAdd(&count[t], 1u);
+        if ((int)i < prompt) atomicOr(&count[t], AL_PROMPT); else atomicAdd(&count[t], 1u);
         mark(t);
       };
-      int i = 0;
+      unsigned i = 0;
       if (c.tokens_vec) {
-        const int whole = len / 4;
+        const unsigned whole = len / 4;
 #pragma unroll 4
-        for (int v = tid; v < whole; v += AL_THREADS) {
+        for (unsigned v = tid; v < whole; v += AL_THREADS) {
           const i32x4 t = reinterpret_cast<const i32x4*>(tokens)[v];
 #pragma unroll
           for (int e = 0; e < 4; e++) one(t[e], 4 * v + e);

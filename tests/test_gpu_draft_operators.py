@@ -3,6 +3,8 @@ path) against plain implementations in 64 bits, on the same rounded inputs.
 
 Tolerances. u is half a step of the output's type (bf16 2^-8, fp16 2^-11, fp32 2^-24), relative to the value. Each test states its bound from the
 roundings that the kernels make; nothing is measured first."""
+import ctypes as C
+
 import numpy as np
 import pytest
 
@@ -720,6 +722,27 @@ def test_adjust_logits_bias_starts_out_of_range(sts, starts):  # noqa: F811
                 sts.op_adjust_logits(a)
                 dev.sync()
                 check_adjusted(dev.get(out, c["x"].shape, "f32"), c, "f32")
+
+
+@pytest.mark.parametrize("stride", [2 ** 31, 2 ** 31 - 1])
+def test_adjust_logits_of_the_longest_history(sts, stride):  # noqa: F811
+    """2^31 - 1 tokens, of which the first and last few are of the vocabulary: the last loads in vectors and one by one, with an index beside 2^31."""
+    n, vocab = 2 ** 31 - 1, 6
+    x = rounded(np.arange(1.0, 7.0)[None], "f32")
+    ends = np.full(600, -1, np.int32)
+    ends[:3] = [0, 1, 1]                                                   # of the prompt, but for the last of them
+    ends[-2:] = [3, 4]
+    with Device() as dev:
+        tokens = dev.alloc(4 * stride)
+        dev.ck(dev.rt.hipMemset(C.c_void_p(tokens), 0xFF, C.c_size_t(4 * stride)), "hipMemset")
+        dev.write(tokens, ends[:300])
+        dev.write(tokens + 4 * (n - 300), ends[300:])
+        logits, out = dev.put(x, "f32"), dev.put(np.zeros((1, vocab), np.float32))
+        sts.op_adjust_logits(sts.AdjustLogits(dtype=0, rows=1, vocab=vocab, n_requests=1, row_stride=vocab, out_stride=vocab, logits=logits, out=out, tokens=tokens, token_stride=stride, lens=dev.ints([n]),
+                                              prompt_lens=dev.ints([2]), repetition=dev.put(np.float32([2.0])), frequency=dev.put(np.float32([0.25])), presence=dev.put(np.float32([0.5]))))
+        dev.sync()
+        got = dev.get(out, vocab, "f32")
+    assert got.tolist() == [0.5, 1.0 - 0.75, 3.0, 2.0 - 0.75, 2.5 - 0.75, 6.0]
 
 
 def test_adjust_logits_same_bits_again_and_in_a_graph(sts):  # noqa: F811
