@@ -506,7 +506,7 @@ int sts_op_adjust_logits(const sts_adjust_logits* a, void* stream);
 /* The accepted path of each request: node 0, then as long as there is one the first child of the last node whose token is chosen[] of that node's row, which is what
  * the target takes behind it. */
 typedef struct {
-  int32_t n_requests, max_rows;
+  int32_t n_requests, max_rows;         /* max_rows up to 2^30 */
   const int32_t* cached;                /* [n_requests] */
   const int32_t *row_starts, *parents;  /* as for sts_op_attn_tree */
   const int32_t *tokens, *chosen;       /* [max_rows]: of each node, and the target's choice behind it */

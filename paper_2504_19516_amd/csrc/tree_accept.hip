@@ -171,7 +171,8 @@ __global__ void __launch_bounds__(256) tree_compact_kernel(CompactCall c) {
 using namespace sts;
 
 extern "C" int sts_op_tree_accept(const sts_tree_accept* a, void* stream) {
-  if (!a || a->n_requests < 0 || a->n_requests > OP_MAX_REQUESTS || a->max_rows < 0) return STS_EINVAL;
+  // rows as sts_op_block_tables makes them: a wave's steps over a request's path stay within 32 bits
+  if (!a || a->n_requests < 0 || a->n_requests > OP_MAX_REQUESTS || a->max_rows < 0 || a->max_rows > (1 << 30)) return STS_EINVAL;
   if (a->n_requests == 0) return STS_OK;
   if (!a->cached || !a->row_starts || !a->lens || !a->counts || !a->next_token) return STS_EINVAL;
   if (a->max_rows > 0 && (!a->parents || !a->tokens || !a->chosen || !a->path)) return STS_EINVAL;

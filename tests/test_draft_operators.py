@@ -89,6 +89,14 @@ def test_tree_accept_refuses(sts):  # noqa: F811
     assert sts.lib().sts_op_tree_accept(None, None) == sts.EINVAL
 
 
+def test_tree_accept_refuses_more_rows_than_block_tables_make(sts):  # noqa: F811
+    """Beyond 2^30 a step of 64 rows of a path would leave 32 bits near 2^31."""
+    good = dict(n_requests=0, max_rows=1 << 30, cached=A, row_starts=2 * A, parents=3 * A, tokens=4 * A, chosen=5 * A, lens=6 * A, counts=7 * A, path=8 * A, next_token=9 * A)
+    sts.op_tree_accept(sts.TreeAccept(**good))
+    for rows in ((1 << 30) + 1, (1 << 31) - 1):
+        refused(sts, sts.op_tree_accept, sts.TreeAccept, good, max_rows=rows)
+
+
 def test_tree_compact_refuses(sts):  # noqa: F811
     good = dict(n_requests=3, max_rows=20, n_kv=2, d=64, pool_pages=9, max_pages=5, table_stride=5, tables=A, cached=2 * A, row_starts=3 * A, counts=4 * A, path=5 * A)
     call = lambda a: sts.op_tree_compact(a, [6 * A, 7 * A])  # noqa: E731
