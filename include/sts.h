@@ -510,7 +510,8 @@ typedef struct {
   const int32_t* cached;                /* [n_requests] */
   const int32_t *row_starts, *parents;  /* as for sts_op_attn_tree */
   const int32_t *tokens, *chosen;       /* [max_rows]: of each node, and the target's choice behind it */
-  int32_t *lens, *counts;               /* [n_requests]: cached + count, and the nodes on the path (0: no rows, more than 256, or node 0 is none; lens then cached) */
+  int32_t *lens, *counts;               /* [n_requests]: cached + count, and the nodes on the path (0: no rows, more than 256, or node 0 is none; lens then cached). lens = cached: in
+                                           place, where no rows are moved behind it (paths of chains lie right as they are): sts_op_tree_compact reads the lengths before */
   int32_t* path;                        /* [max_rows]: numbers of a request's nodes on the path, from its first row on, -1 behind them; rows of no request are left as they were */
   int32_t* next_token;                  /* [n_requests]: chosen[] of the last; -1 without one */
   /* The pages behind the path, which sts_op_block_tables gave to the nodes, go back onto the end of free_pages in the requests' order (tables NULL: they stay with

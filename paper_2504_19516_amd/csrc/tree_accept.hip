@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(256) tree_accept_kernel(sts_tree_accept a) {
   for (int j = count + lane; j < nodes; j += 64) a.path[first + j] = -1;
   if (lane == 0) {
     a.counts[request] = count;
-    a.lens[request] = a.cached[request] + count;
+    a.lens[request] = (int)((unsigned)a.cached[request] + (unsigned)count);
     a.next_token[request] = next;
   }
 }
@@ -75,10 +75,11 @@ __global__ void __launch_bounds__(TA_THREADS) tree_release_kernel(sts_tree_accep
   // of a request: the first page behind its path, and how many the nodes' rows had
   auto behind = [&](int i, int* page) {
     int first;
-    const int nodes = nodes_of(a.row_starts, i, a.max_rows, &first), c = a.cached[i];
+    // lens may have taken the place of cached by now
+    const int nodes = nodes_of(a.row_starts, i, a.max_rows, &first), count = a.counts[i], c = (int)((unsigned)a.lens[i] - (unsigned)count);
     *page = 0;
     if (c < 0 || c > a.max_pages * (long long)OP_PAGE - nodes) return 0;
-    *page = pages_of(c + a.counts[i]);
+    *page = pages_of(c + count);
     return pages_of(c + nodes) - *page;
   };
   long long sum = 0;
@@ -177,6 +178,15 @@ extern "C" int sts_op_tree_accept(const sts_tree_accept* a, void* stream) {
   if (!a->cached || !a->row_starts || !a->lens || !a->counts || !a->next_token) return STS_EINVAL;
   if (a->max_rows > 0 && (!a->parents || !a->tokens || !a->chosen || !a->path)) return STS_EINVAL;
   if (a->tables && (!a->free_pages || !a->n_free || a->max_pages < 0 || a->max_pages > (1 << 26) || a->free_capacity < 0 || a->table_stride < a->max_pages)) return STS_EINVAL;
+  // What is written is read by other waves or by the second kernel: arrays of their own, but for lens in place of cached, and a path in place of the rows that its own wave has read.
+  const bool rows = a->max_rows > 0, pages = a->tables != nullptr;
+  const void* written[] = {a->lens, a->counts, a->next_token, rows ? a->path : nullptr, pages ? a->free_pages : nullptr, pages ? a->n_free : nullptr};
+  const void* read[] = {a->row_starts, a->cached, a->tables, rows ? a->parents : nullptr, rows ? a->tokens : nullptr, rows ? a->chosen : nullptr};
+  for (int i = 0; i < 6; i++)
+    for (int j = 0; j < 6 && written[i]; j++) {
+      if (j > i && written[i] == written[j]) return STS_EINVAL;
+      if (written[i] == read[j] && !(i == 0 && j == 1) && !(i == 3 && j >= 3)) return STS_EINVAL;
+    }
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   OnStreamDevice dev(s);
   if (dev.error() != hipSuccess) return op_result(dev.error());

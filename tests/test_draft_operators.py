@@ -97,6 +97,17 @@ def test_tree_accept_refuses_more_rows_than_block_tables_make(sts):  # noqa: F81
         refused(sts, sts.op_tree_accept, sts.TreeAccept, good, max_rows=rows)
 
 
+def test_tree_accept_refuses_outputs_in_each_others_place(sts):  # noqa: F811
+    """Or in that of what is read: all but lens = cached, whose test runs on the GPU."""
+    good = dict(n_requests=3, max_rows=20, cached=A, row_starts=2 * A, parents=3 * A, tokens=4 * A, chosen=5 * A, lens=6 * A, counts=7 * A, path=8 * A, next_token=9 * A, max_pages=4,
+                free_capacity=9, table_stride=4, tables=10 * A, free_pages=11 * A, n_free=12 * A)
+    written, read = ("lens", "counts", "next_token", "path", "free_pages", "n_free"), ("row_starts", "cached", "tables", "parents", "tokens", "chosen")
+    for i, w in enumerate(written):
+        for other in written[i + 1:] + read:
+            if (w, other) != ("lens", "cached") and not (w == "path" and other in ("parents", "tokens", "chosen")):
+                refused(sts, sts.op_tree_accept, sts.TreeAccept, good, **{w: good[other]})
+
+
 def test_tree_compact_refuses(sts):  # noqa: F811
     good = dict(n_requests=3, max_rows=20, n_kv=2, d=64, pool_pages=9, max_pages=5, table_stride=5, tables=A, cached=2 * A, row_starts=3 * A, counts=4 * A, path=5 * A)
     call = lambda a: sts.op_tree_compact(a, [6 * A, 7 * A])  # noqa: E731

@@ -850,6 +850,31 @@ def test_tree_accept_gives_pages_back(sts, sizes):  # noqa: F811
             assert dev.get(d["counts"], n, "i32").tolist() == counts
 
 
+def test_tree_accept_takes_lengths_in_place(sts):  # noqa: F811
+    """lens = cached: the pages behind the paths are those of the lengths before."""
+    rng = np.random.default_rng(12)
+    sizes = [18, 40, 0, 1, 200, 16, 256, 300] + [3] * 100
+    cached = [30] + rng.integers(0, 100, len(sizes) - 1).tolist()
+    trees, n = [chain(m) for m in sizes], len(sizes)
+    tokens = [list(range(m)) for m in sizes]
+    chosen = [[j + 1 if j < m // 6 else -9 for j in range(m)] for m in sizes]        # the first request's path has four nodes
+    width = max(-(-(c + m) // 16) for c, m in zip(cached, sizes))
+    tables = np.arange(n * width, dtype=np.int32).reshape(n, width) + 1000
+    counts = [len(accept_reference(*x)[0]) for x in zip(trees, tokens, chosen)]
+    back = [int(p) for c, m, k, row in zip(cached, sizes, counts, tables) for p in row[-(-(c + k) // 16):-(-(c + m) // 16)]]
+    with Device() as dev:
+        for in_place in (False, True):
+            _, d, a = run_accept(sts, dev, cached, trees, tokens, chosen)
+            stack, number = dev.ints([-7] * (len(back) + 9)), dev.ints([0])
+            a.max_pages, a.table_stride, a.tables, a.free_pages, a.free_capacity, a.n_free = width, width, dev.ints(tables), stack, len(back) + 9, number
+            if in_place:
+                a.lens = d["cached"]
+            sts.op_tree_accept(a)
+            dev.sync()
+            assert dev.get(a.lens, n, "i32").tolist() == [c + k for c, k in zip(cached, counts)] and dev.get(d["counts"], n, "i32").tolist() == counts
+            assert dev.get(number, 1, "i32")[0] == len(back) and dev.get(stack, len(back) + 9, "i32").tolist() == back + [-7] * 9
+
+
 def test_tree_accept_of_rows_in_many_requests(sts):  # noqa: F811
     """row_starts up and down between 0 and 2^24: 2^31 pages seem to lie behind the paths, and none is given back."""
     n, rows, width = 4096, 1 << 24, 1 << 20
