@@ -451,7 +451,7 @@ typedef struct {
   int32_t dtype;                        /* of the gains */
   int32_t offset_one;                   /* 1: gains are stored less 1 */
   float eps;                            /* not negative */
-  const void *q_gain, *k_gain;          /* [d]; NULL: all 1 */
+  const void *q_gain, *k_gain;          /* [d]; NULL: all 1; not read where there are no such heads */
 } sts_head_norm;
 int sts_op_norm_rope(const sts_head_norm* norm, const sts_rope* rope, const sts_rope_rows* a, void* stream);
 

@@ -474,6 +474,8 @@ extern "C" int sts_op_rope(const sts_rope* rope, const sts_rope_rows* a, void* s
 
 extern "C" int sts_op_norm_rope(const sts_head_norm* norm, const sts_rope* rope, const sts_rope_rows* a, void* stream) {
   if (!norm || !a || norm->dtype < STS_F32 || norm->dtype > STS_F16 || (norm->offset_one != 0 && norm->offset_one != 1) || !(norm->eps >= 0.f) || !std::isfinite(norm->eps) || a->d > RP_NORM_D) return STS_EINVAL;
-  if (!aligned(norm->q_gain, dtype_bytes(norm->dtype)) || !aligned(norm->k_gain, dtype_bytes(norm->dtype))) return STS_EINVAL;
-  return rope_rows(rope, a, stream, HeadNorms{norm->q_gain, norm->k_gain, norm->dtype, 0, norm->eps, norm->offset_one ? 1.f : 0.f});
+  // of heads that are none nothing is read, their gains neither
+  const void *q_gain = a->n_q > 0 ? norm->q_gain : nullptr, *k_gain = a->n_kv > 0 ? norm->k_gain : nullptr;
+  if (!aligned(q_gain, dtype_bytes(norm->dtype)) || !aligned(k_gain, dtype_bytes(norm->dtype))) return STS_EINVAL;
+  return rope_rows(rope, a, stream, HeadNorms{q_gain, k_gain, norm->dtype, 0, norm->eps, norm->offset_one ? 1.f : 0.f});
 }

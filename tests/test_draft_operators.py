@@ -29,6 +29,17 @@ def test_norm_rope_refuses(sts):  # noqa: F811
     sts.op_norm_rope(sts.HeadNorm(), rope, sts.RopeRows(**{**ROWS, "rows": 0}))
 
 
+def test_norm_rope_looks_at_no_gains_of_heads_that_are_none(sts):  # noqa: F811
+    """Wherever their pointer leads."""
+    rope, odd = sts.Rope(rotary_dim=64, theta=1e4), 8 * A + 1
+    call = lambda a, **g: sts.op_norm_rope(sts.HeadNorm(dtype=1, eps=1e-6, **g), rope, sts.RopeRows(**{**ROWS, "rows": 0, "pool": None, "k_out": 10 * A, "k_out_stride": 128, **a}))  # noqa: E731
+    call(dict(n_q=0), q_gain=odd)
+    call(dict(n_kv=0), k_gain=odd)
+    for heads, gain in (("n_kv", "q_gain"), ("n_q", "k_gain")):
+        with pytest.raises(sts.StsError):
+            call({heads: 0}, **{gain: odd})
+
+
 def test_tree_attention_refuses(sts):  # noqa: F811
     size = sts.attn_tree_workspace(6, 40, 8, 2, 64)
     good = dict(dtype=1, n_requests=6, max_rows=40, n_q=8, n_kv=2, d=64, pool_pages=9, max_pages=5, table_stride=5, tables=A, cached=2 * A, row_starts=3 * A, parents=4 * A,

@@ -139,6 +139,23 @@ def test_norm_rope_of_zeros_infinities_and_nan(sts):  # noqa: F811
                 assert np.isfinite(got[r, h]).all()
 
 
+@pytest.mark.parametrize("rows", [3, 700])
+def test_norm_rope_of_one_kind_of_heads(sts, rows):  # noqa: F811
+    """Q without K, or K without Q: the other's pointers, its gains among them, are not followed."""
+    rng = np.random.default_rng(rows)
+    heads, d, eps = 3, 128, 1e-6
+    rope, positions = rope_of(sts, "plain", d, 0), np.arange(rows) % 40
+    x, gain = rounded(rng.standard_normal((rows, heads, d)), "bf16"), gains_of(rng, d, "bf16", 0)[0]
+    want, size = norm_rope_reference(sts, rope, x.astype(np.float64), gain, np.float64(np.float32(eps)), 0, positions)
+    with Device() as dev:
+        for kind, other in (("q", "k"), ("k", "q")):
+            buf, out, g, nowhere = dev.put(x, "bf16"), dev.alloc(x.size * 2), dev.put(gain, "bf16"), 1 << 20
+            a = {kind: buf, kind + "_stride": heads * d, kind + "_out": out, kind + "_out_stride": heads * d, "n_q" if kind == "q" else "n_kv": heads, other: nowhere, other + "_out": nowhere}
+            sts.op_norm_rope(sts.HeadNorm(dtype=1, eps=eps, **{kind + "_gain": g, other + "_gain": nowhere}), rope, sts.RopeRows(dtype=1, rows=rows, d=d, positions=dev.ints(positions), **a))
+            dev.sync()
+            near(dev.get(out, x.shape, "bf16"), want, norm_rope_bound(want, size, "bf16"))
+
+
 # ------------------------------------------------------------------------------------------ attention of drafted trees
 def chain(m):
     return list(range(-1, m - 1))
