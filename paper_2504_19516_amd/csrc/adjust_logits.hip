@@ -5,7 +5,7 @@
 // with n the token's count in the output. A workgroup takes a part of the vocabulary for some rows in a row: it counts the history's tokens of its part in LDS, once for
 // all rows of a request. One bit for each token tells whether anything may apply to it, eight more on which of the rows' paths it is (how often is counted where that is so:
 // seldom); of the others nothing is computed, and in place they are not even read: a group of neighbouring elements goes to memory only where it changes, and without being read
-// where all of it is ruled out. The arithmetic is in 64 bits, rounded to 32 and to the type: it runs for a few thousand elements of a row.
+// where all of it is ruled out. The arithmetic is in 64 bits, rounded once, to the type: it runs for a few thousand elements of a row.
 //
 // Bound by memory where rows are copied (320 rows of 128256 in 32 bits, chains of five on histories of 1500: 83 us, a copy of as many bytes 68; without the arithmetic of what changes some 12
 // less, the rest is histories that are read and counted while little else is under way), by latency for a few rows (one row 6.5 us: descriptions, history, LDS, elements, one behind the
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(AL_THREADS) adjust_logits_kernel(AdjustCall c)
       if (n) y *= y > 0.0 ? inverse : (double)r;
       if (n & ~AL_PROMPT) y -= (double)f * (n & ~AL_PROMPT) + w;
       if (b) y += a.bias_values[b - 1];
-      return (T)(float)y;
+      return (T)y;                                     // one rounding, from 64 bits to the type
     };
     auto group = [&](const At& at) {                   // bits of its elements: something may apply; ruled out
       const int m = __builtin_amdgcn_readfirstlane(mask_of[at.row]);

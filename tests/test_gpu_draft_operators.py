@@ -741,6 +741,52 @@ def test_adjust_logits_bias_starts_out_of_range(sts, starts):  # noqa: F811
                 check_adjusted(dev.get(out, c["x"].shape, "f32"), c, "f32")
 
 
+def to_type(y, dtype):
+    """y (float64) in the type, as float64: one rounding, to the nearest, ties to even."""
+    bits, least, most = (8, -133, float(np.uint32(0x7F7F0000).view(np.float32))) if dtype == "bf16" else (11, -24, 65504.0)
+    step = np.exp2(np.maximum(np.frexp(y)[1] - bits, least).astype(np.float64))
+    z = np.rint(y / step) * step
+    return np.where(np.abs(z) > most, np.copysign(np.inf, y), z)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_adjust_logits_rounds_once(sts, dtype):  # noqa: F811
+    """Sums that lie 2^-20 of half a step of the type beside the middle between two of its numbers, where 32 bits would round them onto the middle, at both ends of the type's range and in
+    between: they are exact in 64 bits, so the outputs are known to the bit."""
+    bits, least = (8, -126) if dtype == "bf16" else (11, -14)
+    top = 127 if dtype == "bf16" else 15
+    x, b = [], []
+    for e in (least, -3, 0, 1, 6, top - 1, top):
+        for m in list(range(2 ** (bits - 1), 2 ** (bits - 1) + 6)) + [2 ** bits - 3, 2 ** bits - 2, 2 ** bits - 1]:
+            for side in (-1, 0, 1):
+                for sign in (-1.0, 1.0):
+                    x.append(sign * np.ldexp(float(m), e + 1 - bits))
+                    b.append(sign * np.ldexp(1.0 + side * 2.0 ** -20, e - bits))
+    for m in (0, 1, 2, 3, 7):                                               # numbers below the smallest with all its digits
+        for side in (-1, 0, 1):
+            x.append(np.ldexp(float(m), least + 1 - bits))
+            b.append(np.ldexp(1.0 + side * 2.0 ** -20, least - bits))
+    x, b = np.array(x), np.array(b)
+    b32 = b.astype(np.float32)
+    vocab = len(x)
+    assert np.array_equal(rounded(x, dtype), x)
+    y = x + b32.astype(np.float64)
+    want = to_type(y, dtype)
+    with np.errstate(over="ignore"):
+        twice = rounded(y.astype(np.float32), dtype)
+    assert (twice != want).sum() > 20
+    with Device() as dev:
+        for in_place in (False, True):
+            logits = dev.put(x[None], dtype)
+            out = logits if in_place else dev.alloc(2 * vocab)
+            sts.op_adjust_logits(sts.AdjustLogits(dtype=sts.DTYPES[dtype], rows=1, vocab=vocab, n_requests=1, row_stride=vocab, out_stride=vocab, logits=logits, out=out, n_biases=vocab,
+                                                  bias_starts=dev.ints([0, vocab]), bias_tokens=dev.ints(np.arange(vocab)), bias_values=dev.put(b32)))
+            dev.sync()
+            got = dev.get(out, vocab, dtype).astype(np.float64)
+            bad = got != want
+            assert not bad.any(), (bad.sum(), x[bad][:5], b[bad][:5], got[bad][:5], want[bad][:5])
+
+
 @pytest.mark.parametrize("stride", [2 ** 31, 2 ** 31 - 1])
 def test_adjust_logits_of_the_longest_history(sts, stride):  # noqa: F811
     """2^31 - 1 tokens, of which the first and last few are of the vocabulary: the last loads in vectors and one by one, with an index beside 2^31."""
