@@ -459,7 +459,7 @@ int sts_op_norm_rope(const sts_head_norm* norm, const sts_rope* rope, const sts_
  * sts_op_block_tables numbers them. A row whose parent is no earlier node of its request (-1: it follows the context) is no node, nor are those below it:
  * their rows are padding, which gives zeros and an lse of -inf, and which nobody sees. Rows from row_starts[n_requests] on are left as they were. A request
  * of more than 256 rows, one with cached < 0 or cached + rows behind max_pages, one whose table names a page outside the pool, and all rows if row_starts does not
- * lead from 0 to at most max_rows in order, give NaN. What lies in a page behind the nodes is not looked at, and infinities and NaN in a node's K or V stay with those
+ * lead from 0 to at most max_rows in order, give NaN (for a page outside the pool the nodes alone: padding gives zeros there too). What lies in a page behind the nodes is not looked at, and infinities and NaN in a node's K or V stay with those
  * who see it.
  * The plan is made once a step and serves all layers, as for sts_op_attn_shared; a workspace that holds no plan, or one of a batch of other sizes, gives NaN for
  * all max_rows rows. Calls that may run at the same time need workspaces of their own. */
@@ -484,7 +484,8 @@ int sts_op_attn_tree(const sts_tree_batch* b, const void* q, int64_t q_stride, c
 /* Logits before a token is chosen. With n the times that a token stands in the output of the row's request, and s whether it stands in its prompt or output:
  *   y = x / repetition (x > 0) or x * repetition, where s;  y -= frequency * n;  y -= presence, where n > 0;  y += bias;  -inf, where the row's mask has a 0
  * in 64 bits, rounded once. Elements that nothing applies to keep their bits. The output: tokens[prompt_len .. len) of the request, and of a drafted node's row the
- * tokens of the node and its ancestors (of a request's first 256 rows). */
+ * tokens of the node and its ancestors (of a request's first 256 rows). A row that is no node, which nobody looks at, counts its own token and those above it, as far as
+ * each row's parent is an earlier one. */
 typedef struct {
   int32_t dtype, rows, vocab, n_requests;      /* rows up to 65535, vocab up to 2^30 */
   int64_t row_stride, out_stride;       /* elements from row to row */

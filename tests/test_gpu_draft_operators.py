@@ -388,6 +388,26 @@ def test_tree_attention_pages_and_lengths_out_of_range_are_nan(sts):  # noqa: F8
         assert (check(0, cached=c) == -1).all()
 
 
+def test_tree_attention_padding_of_a_request_with_a_bad_page_gives_zeros(sts):  # noqa: F811
+    """Its nodes NaN, its padding zeros and an lse of -inf as everywhere."""
+    rng = np.random.default_rng(14)
+    q, k, v, tables, pages, cached, trees = tree_inputs(rng, "bf16", SMALL, 8, 2, 64)
+    trees[0][3], trees[2][1], trees[2][20] = -2, 1, 99
+    pool = pool_of(k, v, tables, [c + len(t) for c, t in zip(cached, trees)], pages, "bf16")
+    want, starts = tree_reference(q, k, v, cached, trees, 4, 0.125, "bf16"), starts_of(trees)
+    node = np.array([up is not None for t in trees for up in ancestors(t)])
+    for hit, at in ((0, 1), (2, 0), (2, 4)):
+        t = tables.copy()
+        t[hit, at] = pages
+        with Device() as dev:
+            got, lse, positions, _, _ = run_tree(sts, dev, "bf16", q, pool, t, cached, trees, 4)
+        bad = np.zeros(len(q), bool)
+        bad[starts[hit]:starts[hit + 1]] = True
+        assert np.isnan(got[bad & node]).all() and np.isnan(lse[bad & node]).all()
+        assert (got[~node] == 0.0).all() and np.isneginf(lse[~node]).all() and (positions[~node] == -1).all()
+        near(got[~bad & node], want[0][~bad & node], want[1][~bad & node])
+
+
 def test_tree_attention_of_more_nodes_than_a_request_may_have_is_nan(sts):  # noqa: F811
     rng = np.random.default_rng(9)
     q, k, v, tables, pages, cached, trees = tree_inputs(rng, "bf16", [(20, "chain", 7), (5, "chain", 257), (31, "tree", 12)], 4, 2, 64)
@@ -692,6 +712,22 @@ def test_adjust_logits_without_requests_or_prompts(sts):  # noqa: F811
         sts.op_adjust_logits(a)
         dev.sync()
         check_adjusted(dev.get(out, c["x"].shape, "f32"), c, "f32")
+
+
+def test_adjust_logits_paths_of_rows_that_are_no_nodes(sts):  # noqa: F811
+    """Such a row's path ends where a parent is no earlier row."""
+    rng = np.random.default_rng(15)
+    c = adjust_case(rng, "f32", 3000, [random_tree(rng, 9), random_tree(rng, 4)], 30, 2, 0.3)
+    odd = {2: -2, 4: 4, 5: 2, 6: 2 ** 31 - 1, 8: 6}
+    first = list(c["trees"][0])
+    c["trees"][0] = [-1 if odd.get(j, p) < -1 or odd.get(j, p) >= j else odd.get(j, p) for j, p in enumerate(first)]
+    with Device() as dev:
+        for in_place in (False, True):
+            a, out = adjust_description(sts, dev, "f32", c, in_place)
+            a.parents = dev.ints([odd.get(j, p) for j, p in enumerate(first)] + c["trees"][1])
+            sts.op_adjust_logits(a)
+            dev.sync()
+            check_adjusted(dev.get(out, c["x"].shape, "f32"), c, "f32")
 
 
 def test_adjust_logits_of_odd_values_and_numbers(sts):  # noqa: F811
