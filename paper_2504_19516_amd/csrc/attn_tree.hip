@@ -939,7 +939,7 @@ __global__ void __launch_bounds__(256) attn_tree_join_few_kernel(TreeCall<T> c) 
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attn_tree_join_kernel(TreeCall<T> c) {
   constexpr int LANES = D / 4, RUNS = 256 / LANES;
-  const int lane = threadIdx.x % LANES, at = blockIdx.x * RUNS + threadIdx.x / LANES;
+  const int lane = threadIdx.x % LANES, at = (int)(blockIdx.y * gridDim.x + blockIdx.x) * RUNS + threadIdx.x / LANES;
   if (at >= c.max_rows * c.n_q) return;
   const int row = at / c.n_q, head = at % c.n_q, kvh = head / c.heads;
   const Pieces p = pieces_of(c, row, head % c.heads);
@@ -991,8 +991,10 @@ hipError_t launch_attn(hipStream_t s, const TreeCall<T>& c) {
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)c.max_rows * c.n_q;
   if (rows <= AT_JOIN_ROWS) return launch(attn_tree_join_few_kernel<T, D>, dim3((unsigned)rows), dim3(256), 0, s, c);
+  // a launch's x ends below 2^32 threads: the most rows of the most heads are 2^34
   constexpr int RUNS = 256 / (D / 4);
-  return launch(attn_tree_join_kernel<T, D>, dim3((unsigned)((rows + RUNS - 1) / RUNS)), dim3(256), 0, s, c);
+  const unsigned groups = (unsigned)((rows + RUNS - 1) / RUNS), x = std::min(groups, 1u << 20);
+  return launch(attn_tree_join_kernel<T, D>, dim3(x, (groups + x - 1) / x), dim3(256), 0, s, c);
 }
 
 bool sizes_ok(int n, int max_rows, int n_q, int n_kv, int d) {

@@ -520,6 +520,30 @@ def test_tree_attention_without_a_plan_of_its_sizes_is_nan(sts):  # noqa: F811
         assert np.isfinite(layer(batch())[:60]).all() and (layer(batch())[60:] == 7.0).all()
 
 
+def test_tree_attention_of_the_most_rows_and_many_heads(sts):  # noqa: F811
+    """65536 rows of 2048 query heads: 2^27 rows of heads to join, 137 GB of workspace. Few of the rows are there; the others stay as they are."""
+    rng = np.random.default_rng(61)
+    n_q, n_kv, d, rows = 2048, 256, 128, 65536
+    q, k, v, tables, pages, cached, trees = tree_inputs(rng, "bf16", [(35, "tree", 3), (0, "chain", 2), (7, "tree", 5)], n_q, n_kv, d)
+    pool = pool_of(k, v, tables, [c + len(t) for c, t in zip(cached, trees)], pages, "bf16")
+    want, n, size = tree_reference(q, k, v, cached, trees, n_q // n_kv, d ** -0.5, "bf16"), len(q), sts.attn_tree_workspace(3, rows, n_q, n_kv, d)
+    assert size > 1 << 37
+    with Device() as dev:
+        fields = dict(tables=dev.ints(tables), cached=dev.ints(cached), row_starts=dev.ints(starts_of(trees)), parents=dev.ints([p for t in trees for p in t] + [-1] * (rows - n)),
+                      positions=dev.ints([777] * rows), workspace=dev.alloc(size), workspace_bytes=size)
+        batch = sts.TreeBatch(dtype=1, n_requests=3, max_rows=rows, n_q=n_q, n_kv=n_kv, d=d, pool_pages=pages, max_pages=tables.shape[1], table_stride=tables.shape[1], **fields)
+        dev_q, out, lse = dev.alloc(rows * n_q * d * 2), dev.alloc(rows * n_q * d * 2), dev.alloc(rows * n_q * 4)
+        dev.write(dev_q, stored(q.reshape(n, -1), "bf16"))
+        for row in (n, rows - 1):
+            dev.write(out + row * n_q * d * 2, np.full(n_q * d, 0x7FC0, np.uint16))
+        sts.op_attn_tree_plan(batch)
+        sts.op_attn_tree(batch, dev_q, n_q * d, dev.put(pool, "bf16"), out, n_q * d, lse)
+        dev.sync()
+        check_tree(dev.get(out, (n, n_q, d), "bf16"), dev.get(lse, (n, n_q), "f32"), want, cached, trees, dev.get(fields["positions"], rows, "i32")[:n])
+        for row in (n, rows - 1):
+            assert np.isnan(dev.get(out + row * n_q * d * 2, n_q * d, "bf16")).all()
+
+
 def test_tree_attention_of_two_streams_at_once(sts):  # noqa: F811
     """Workspaces of their own: calls under way together do not see each other."""
     rng = np.random.default_rng(21)
