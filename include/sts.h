@@ -445,7 +445,7 @@ int sts_op_logprobs(const sts_logprobs* a, void* stream);
  * sts_op_tree_accept, sts_op_tree_compact. */
 
 /* sts_op_rope of heads that are first divided by their root mean square: x / sqrt(mean(x^2) + eps) times the gain of each element, over the d elements of a head of
- * Q and of K; V passes. All in 32 bits (squares and their sum too: elements below 2^60, and with an eps of 0 a root
+ * Q and of K; V passes. All in 32 bits (squares and their sum too: elements below 2^60, and with an eps below 2^-120 a root
  * above 2^-60), rounded once, behind the rotation. d up to 512. */
 typedef struct {
   int32_t dtype;                        /* of the gains */

@@ -19,15 +19,19 @@
 namespace sts {
 namespace {
 
-constexpr int AL_THREADS = 512, AL_NODES = 256;        // 256 / 512 / 1024 threads: 320 rows 81 / 84 / 88 us, 702 rows of 56507 170 / 147 / 206
-constexpr int AL_BATCH = 4;                            // groups of elements of a thread under way: 2 / 4 / 8 level, longer for few rows
+// Figures of the constants: rows that change, in 32 bits unless stated, with histories of up to 2000 tokens and 8 biases a request; runs differ by up to 2 %.
+// "24 calls" is the geometric mean of 24 calls with penalties or biases, of all sizes and types.
+// 256 / 512 / 1024 threads: 320 rows in chains of five 86 / 88 / 112 us, 702 rows of 56507 in chains of three 103 / 96 / 132, 256 single rows of 16 bits 81 / 94 / 153, 24 calls 12.3 / 11.5 / 12.7.
+constexpr int AL_THREADS = 512, AL_NODES = 256;
+// Groups of elements of a thread under way. 2 / 4 / 8: 320 rows 88 / 88 / 103 us, 702 rows 95 / 96 / 115, one row 6.2 / 6.4 / 7.0, 24 calls 11.1 / 11.5 / 12.5: 2 would do as well, and gain some 0.3 us of the small ones.
+constexpr int AL_BATCH = 4;
 constexpr int AL_ROWS = 8;                             // rows of a workgroup, at most: a bit each
-// Tokens of a part, fewer where that leaves fewer workgroups than these. Parts of 2048 / 4096 / 8192: 320 rows 95 / 84 / 81 us, 702 rows 161 / 147 / 170. 256 / 512 / 1024 workgroups: geometric mean
-// of 24 calls of all sizes 9.9 / 10.0 / 10.3 us.
+// Tokens of a part, fewer where that leaves fewer workgroups than these. Parts of 2048 / 4096 / 8192: 320 rows 97 / 88 / 86 us, 702 rows of 56507 111 / 96 / 102, 38 chains of 15 and 10586 tokens of vocabulary
+// 44 / 38 / 48, 256 single rows of 16 bits 147 / 94 / 82 (each part counts the history for itself), 24 calls 12.3 / 11.5 / 11.3. 256 / 512 / 1024 workgroups: 24 calls 11.5 / 11.0 / 11.4, the large ones level.
 constexpr int AL_PART = 4096, AL_LEAST = 1024, AL_WORKGROUPS = 256;
 constexpr unsigned AL_PROMPT = 1u << 31;               // beside the count of the output
 
-constexpr int AL_MASK_THREADS = 256, AL_MASK_BATCH = 4;       // groups of a thread: 4 / 8 / 16, 256 masked rows 12.6 / 14.7 / 20 us
+constexpr int AL_MASK_THREADS = 256, AL_MASK_BATCH = 4;       // groups of a thread: 4 / 8 / 16, 256 rows, half of them masked, 13.4 / 18.5 / 17.5 us, 1000 of 32000, all masked, 19 / 22 / 22
 
 struct AdjustCall {
   sts_adjust_logits a;

@@ -18,8 +18,8 @@
 // Measured, 32 query and 8 KV heads of 128 in bf16, or 64 and 8 in fp16; us of the plan (once a step), and of products and join (each layer), medians under a trace:
 //   one tree of 26 nodes on 1500 tokens, 6 MB of pages a layer     6   13   4    latency: table, pages, one to three tiles, partial results, one behind the other
 //   64 chains of 5 on 1100 tokens (spread), 322 MB                 8   65   8    4.95 TB/s in the products: memory
-//   16 trees of 64 on 4096 tokens (spread), 270 MB                 9  130  14    0.53 PFLOP/s, 0.8 with the second numbers': see run_wide
-//   six trees of up to 33 on 14000 tokens, 64 heads, 238 MB        7   67  12    memory for the small trees (3.6 TB/s), matrix cores and exponentials for the large
+//   16 trees of 64 on 4096 tokens (spread), 270 MB                10  143  15    0.48 PFLOP/s; without the trace 129, 0.53 and 0.8 with the second numbers': see run_wide
+//   six trees of up to 33 on 14000 tokens, 64 heads, 238 MB        8   69  12    memory for the small trees (3.6 TB/s), matrix cores and exponentials for the large
 #include <algorithm>
 
 #include "attn_parts.h"
